@@ -395,6 +395,83 @@ int cgconv_plan_enable_timing(cgconv_plan_t plan, int32_t max_calls);
 int cgconv_plan_stage_times(cgconv_plan_t plan, double* ms, int32_t cap, int32_t* n_stages, int32_t* n_calls);
 const char* cgconv_plan_stage_name(cgconv_plan_t plan, int32_t stage);
 
+/*
+ * ---- Sequence operators ----------------------------------------------------
+ *
+ * What a block has around the convolution: layer norm by degree and activation
+ * checkpoints in 8 bits.  Features are [batch][N][(L_max+1)^2][C] as above, in
+ * fp32 or bfloat16 (CGCONV_F32, CGCONV_BF16: the features and their gradients;
+ * parameters, statistics and all arithmetic are fp32, an output is rounded once,
+ * to nearest, ties to even).  L_max = 0 is the ordinary layout of scalars.
+ *
+ * A sequence plan holds the sizes and the workspace.  1 <= batch <= 65535, N >= 1
+ * (any), batch * N <= CGCONV_SEQ_TOKENS, 0 <= L_max <= CGCONV_LMAX, C >= 1 with
+ * (2 L_max + 1) C <= CGCONV_SEQ_SEGMENT, 0 <= states <= CGCONV_SEQ_STATES.  As for
+ * the other plans: created synchronously, its device must be current at every
+ * call, calls only enqueue kernels (capturable), and calls of one plan share its
+ * workspace, so two of them must not be in flight on different streams (nor in
+ * two captured graphs that run at once).  Arrays are 16-byte aligned and
+ * contiguous; what a call writes overlaps none of its other arrays.
+ */
+typedef struct cgconv_seq_plan* cgconv_seq_plan_t;
+enum cgconv_dtype { CGCONV_F32 = 0, CGCONV_BF16 = 1 };
+#define CGCONV_SEQ_TOKENS 2147483647
+#define CGCONV_SEQ_SEGMENT 16384
+#define CGCONV_SEQ_STATES 32
+
+cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states);
+void cgconv_seq_plan_destroy(cgconv_seq_plan_t plan); /* NULL is a no-op */
+int cgconv_seq_plan_info(cgconv_seq_plan_t plan, size_t* workspace_bytes);
+
+/*
+ * Layer norm by degree (token by token):
+ *
+ *   d = x - [l = 0] mean_c x,   rstd_l = 1 / sqrt(mean_{m,c} d^2 + eps)
+ *   y[(l,m),c] = weight[l,c] d[(l,m),c] rstd_l + [l = 0] bias[c]
+ *
+ * Only the invariants (l = 0) are shifted, so the norm commutes with rotations;
+ * L_max = 0 is the ordinary layer norm.  x, y: [batch][N][K][C] of dtype; weight
+ * [L_max+1][C] and bias [C], fp32, may be NULL (ones, zeros); eps >= 0.
+ * mean [batch][N] and rstd [batch][N][L_max+1], fp32, receive the statistics for
+ * the backward (both, or NULL for inference).  codes and scales (both, or NULL)
+ * receive the 8-bit checkpoint of x in the same pass, rows of C channels
+ * (cgconv_pack8).
+ */
+int cgconv_seq_norm(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const float* weight, const float* bias,
+                    float eps, void* y, float* mean, float* rstd, int8_t* codes, uint8_t* scales,
+                    hipStream_t stream);
+
+/*
+ * Backward of cgconv_seq_norm, with h = d rstd_l and g = weight grad_y:
+ *
+ *   grad_x = rstd_l (g - [l = 0] mean_c g - h mean_{m,c}(g h))
+ *   grad_weight[l,c] = sum_{b,n,m} grad_y h,   grad_bias[c] = sum_{b,n} grad_y[(0,0),c]
+ *
+ * The input is x, or its checkpoint (codes and scales; x NULL): h is then formed
+ * from the values that the 8 bits hold, with the mean and rstd of x itself.
+ * mean and rstd are the forward's.  Any of grad_x (dtype), grad_weight, grad_bias
+ * (fp32) may be NULL, not all.  The sums over tokens have a fixed order.
+ */
+int cgconv_seq_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const int8_t* codes,
+                             const uint8_t* scales, const float* weight, const float* mean, const float* rstd,
+                             const void* grad_y, void* grad_x, float* grad_weight, float* grad_bias,
+                             hipStream_t stream);
+
+/*
+ * Activation checkpoint in 8 bits of `rows` rows of C channels: codes int8
+ * [rows][C], scales uint8 [rows][ceil(C/32)].  Of every 32 channels of a row (the
+ * last group shorter) the scale is s = 2^(byte - 127), the smallest power of two
+ * (at least 2^-126) with max |x| <= 127 s; a code is x / s to the nearest whole
+ * number, ties to even.  Every step is exact in fp32, so |x - code s| <= s/2 and
+ * the codes are the same on any machine; a value of a bfloat16 tensor comes back
+ * as a bfloat16 without another rounding.  A group with an infinity or NaN gets
+ * the byte 255 and comes back as NaN.  x is of dtype; no plan, no workspace.
+ */
+int cgconv_pack8(int32_t dtype, int64_t rows, int64_t C, const void* x, int8_t* codes, uint8_t* scales,
+                 hipStream_t stream);
+int cgconv_unpack8(int32_t dtype, int64_t rows, int64_t C, const int8_t* codes, const uint8_t* scales, void* x,
+                   hipStream_t stream);
+
 /* Thread-local message describing the last error on this thread ("" if none). */
 const char* cgconv_last_error(void);
 

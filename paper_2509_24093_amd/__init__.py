@@ -15,6 +15,26 @@ from __future__ import annotations
 import ctypes
 import os
 
+from . import sequence
+from .sequence import (  # noqa: F401
+    CGCONV_BF16,
+    CGCONV_F32,
+    CGCONV_SEQ_SEGMENT,
+    CGCONV_SEQ_STATES,
+    CGCONV_SEQ_TOKENS,
+    SequencePlan,
+    cgconv_norm,
+    cgconv_pack8,
+    cgconv_seq_norm,
+    cgconv_seq_norm_backward,
+    cgconv_seq_plan_create,
+    cgconv_seq_plan_destroy,
+    cgconv_seq_plan_info,
+    cgconv_unpack8,
+    checkpoint_pack,
+    checkpoint_unpack,
+)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcgconv.so")
 
@@ -99,6 +119,7 @@ def library() -> ctypes.CDLL:
     lib.cgconv_plan_stage_name.restype = ctypes.c_char_p
     lib.cgconv_last_error.argtypes = []
     lib.cgconv_last_error.restype = ctypes.c_char_p
+    sequence.bind(lib)
     _lib = lib
     return lib
 
@@ -441,29 +462,33 @@ class Plan:
 _autograd_fn = None
 
 
-def cgconv(q, k, plan: Plan):
+def cgconv(q, k, plan: Plan, checkpoint=None):
     """Differentiable CG convolution of fp32 tensors: the forward and the
-    backward are the plan's cgconv_forward and cgconv_backward."""
+    backward are the plan's cgconv_forward and cgconv_backward.
+    checkpoint="int8": q and k are kept for the backward in 8 bits
+    (:func:`checkpoint_pack`), 1.03 bytes a value instead of 4."""
     global _autograd_fn
+    packed = sequence._want_checkpoint(checkpoint) and sequence._grad_wanted(q, k)
     if _autograd_fn is None:
         import torch
 
         class _CgconvFn(torch.autograd.Function):
             @staticmethod
-            def forward(ctx, q, k, plan):
-                ctx.save_for_backward(q, k)
+            def forward(ctx, q, k, plan, packed):
+                out = plan.forward(q, k)  # checks q and k
+                sequence.keep(ctx, packed, (q, k))
                 ctx.plan = plan
-                return plan.forward(q, k)
+                return out
 
             @staticmethod
             def backward(ctx, grad_out):
-                q, k = ctx.saved_tensors
+                (q, k), _ = sequence.kept(ctx)
                 gq, gk = ctx.plan.backward(q, k, grad_out.contiguous(), need_q=ctx.needs_input_grad[0],
                                            need_k=ctx.needs_input_grad[1])
-                return gq, gk, None
+                return gq, gk, None, None
 
         _autograd_fn = _CgconvFn
-    return _autograd_fn.apply(q, k, plan)
+    return _autograd_fn.apply(q, k, plan, packed)
 
 
 class GraphPlan(Plan):
@@ -511,40 +536,45 @@ class GraphPlan(Plan):
 _gate_fn = None
 
 
-def cgconv_gate(u, v, plan: Plan):
+def cgconv_gate(u, v, plan: Plan, checkpoint=None):
     """Differentiable gating + value tensor product of fp32 tensors in u and
     v: the forward and the backward are the plan's cgconv_gate_value and
-    cgconv_gate_value_backward."""
+    cgconv_gate_value_backward.  checkpoint="int8": u and v are kept for the
+    backward in 8 bits."""
     global _gate_fn
+    packed = sequence._want_checkpoint(checkpoint) and sequence._grad_wanted(u, v)
     if _gate_fn is None:
         import torch
 
         class _GateFn(torch.autograd.Function):
             @staticmethod
-            def forward(ctx, u, v, plan):
-                ctx.save_for_backward(u, v)
+            def forward(ctx, u, v, plan, packed):
+                f = plan.gate_value(u, v)
+                sequence.keep(ctx, packed, (u, v))
                 ctx.plan = plan
-                return plan.gate_value(u, v)
+                return f
 
             @staticmethod
             def backward(ctx, grad_f):
-                u, v = ctx.saved_tensors
+                (u, v), _ = sequence.kept(ctx)
                 gu, gv = ctx.plan.gate_value_backward(u, v, grad_f.contiguous(), need_u=ctx.needs_input_grad[0],
                                                       need_v=ctx.needs_input_grad[1])
-                return gu, gv, None
+                return gu, gv, None, None
 
         _gate_fn = _GateFn
-    return _gate_fn.apply(u, v, plan)
+    return _gate_fn.apply(u, v, plan, packed)
 
 
 _graph_fn = None
 
 
-def cgconv_graph(U, q, k, plan: GraphPlan):
+def cgconv_graph(U, q, k, plan: GraphPlan, checkpoint=None):
     """Differentiable graph CG convolution of fp32 tensors in q and k: the
     forward and the backward are the plan's cgconv_forward_graph and
-    cgconv_backward_graph.  U is a constant here (no gradient flows to it)."""
+    cgconv_backward_graph.  U is a constant here (no gradient flows to it).
+    checkpoint="int8": q and k (not U) are kept for the backward in 8 bits."""
     global _graph_fn
+    packed = sequence._want_checkpoint(checkpoint) and sequence._grad_wanted(q, k)
     if getattr(U, "requires_grad", False):
         raise ValueError("cgconv_graph gives no gradient with respect to U; pass U.detach()")
     if _graph_fn is None:
@@ -552,17 +582,18 @@ def cgconv_graph(U, q, k, plan: GraphPlan):
 
         class _GraphFn(torch.autograd.Function):
             @staticmethod
-            def forward(ctx, U, q, k, plan):
-                ctx.save_for_backward(U, q, k)
+            def forward(ctx, U, q, k, plan, packed):
+                out = plan.forward(U, q, k)
+                sequence.keep(ctx, packed, (q, k), (U,))
                 ctx.plan = plan
-                return plan.forward(U, q, k)
+                return out
 
             @staticmethod
             def backward(ctx, grad_out):
-                U, q, k = ctx.saved_tensors
+                (q, k), (U,) = sequence.kept(ctx)
                 gq, gk = ctx.plan.backward(U, q, k, grad_out.contiguous(), need_q=ctx.needs_input_grad[1],
                                            need_k=ctx.needs_input_grad[2])
-                return None, gq, gk, None
+                return None, gq, gk, None, None
 
         _graph_fn = _GraphFn
-    return _graph_fn.apply(U, q, k, plan)
+    return _graph_fn.apply(U, q, k, plan, packed)

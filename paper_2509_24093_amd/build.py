@@ -60,6 +60,9 @@ def build(jobs: int | None = None, verbose: bool = True) -> str:
         ([HIPCC, "-c"] + HIP_FLAGS, "fft.hip", "fft.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "cg.hip", "cg.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "gft.hip", "gft.o", []),
+        ([HIPCC, "-x", "hip", "-c"] + HIP_FLAGS, "sequence.cpp", "sequence.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "norm.hip", "norm.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "pack.hip", "pack.o", []),
     ]
     for P in (3, 5, 7):
         units.append(([HIPCC, "-c"] + HIP_FLAGS, "fft_odd.hip", "fft_odd_P%d.o" % P, ["-DCGCONV_TU_P=%d" % P]))

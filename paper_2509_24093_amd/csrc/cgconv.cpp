@@ -32,6 +32,7 @@
 #include "gate_bwd.h"
 #include "gft.h"
 #include "kernels.h"
+#include "seq.h"
 
 using namespace cgconv;
 
@@ -39,13 +40,17 @@ namespace {
 
 thread_local std::string g_last_error;
 
-void set_error(const char* fmt, ...) {
+void set_error_list(const char* fmt, va_list ap) {
   char buf[512];
+  std::vsnprintf(buf, sizeof buf, fmt, ap);
+  g_last_error = buf;
+}
+
+void set_error(const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
-  std::vsnprintf(buf, sizeof buf, fmt, ap);
+  set_error_list(fmt, ap);
   va_end(ap);
-  g_last_error = buf;
 }
 
 bool is_pow2(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
@@ -173,6 +178,15 @@ SmallShape small_shape(int64_t B, int64_t rows, int64_t Nf, int L, int64_t C, in
 }
 
 }  // namespace
+
+void cgconv::set_last_error(const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  set_error_list(fmt, ap);
+  va_end(ap);
+}
+
+void cgconv::clear_last_error() { g_last_error.clear(); }
 
 struct cgconv_plan {
   int64_t B = 0, N = 0, C = 0, Cp = 0;  // N: length of the token DFTs

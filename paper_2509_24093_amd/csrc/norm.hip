@@ -1,0 +1,666 @@
+// Layer norm by degree, forward and backward, for gfx950.  For a token's
+// features x[(l,m),c] (K = (L+1)^2 components of C channels, the degrees'
+// (2l+1) C values contiguous):
+//
+//   d = x - [l = 0] mean_c x                      only invariants may be shifted
+//   r_l = 1 / sqrt(mean_{m,c} d^2 + eps)
+//   y = w[l,c] d r_l + [l = 0] bias[c]
+//
+// L = 0 is the ordinary layer norm over C.  Backward, with h = d r (the
+// normalised values) and g = w gy:
+//
+//   gx = r_l (g - [l = 0] mean g - h mean(g h)),   gw[l,c] = sum_{t,m} gy h,   gb[c] = sum_t gy_0
+//
+// Two forms.  Rows (one component's C channels) of at most 64 vectors are
+// shared by 1..64 lanes, and a block takes whole tokens of several rows per
+// pass, all of them in registers: the sum of a row is a lane reduction, the sum
+// of a degree adds the sums of its rows through LDS.  Longer rows: a block per
+// degree of a token.  Either way every input is read once and every output
+// written once.  In the backward the threads keep their columns from token to
+// token, so gw and gb grow in registers over all tokens of a block; the blocks'
+// sums are added by a second kernel in a fixed order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "seq_common.h"
+
+namespace cgconv {
+
+namespace {
+
+using namespace seqdev;
+
+// Launch shape of the row form.
+struct RowShape {
+  int lanes;    // per row (a power of two)
+  int threads;  // per block
+  int passes;   // rows per thread: a multiple of kPassStep
+  int tokens;   // per block
+};
+
+__device__ __forceinline__ int degree_of(int comp) { return (int)__builtin_sqrtf((float)comp + 0.5f); }
+
+// Dynamic LDS: a row's sums, then a degree's.
+template <class T, int V, int R, bool CODES>
+__global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
+  extern __shared__ float lds[];
+  const int tid = threadIdx.x, per = sh.threads / sh.lanes;  // rows per pass
+  const int j = tid & (sh.lanes - 1), rg = tid / sh.lanes;
+  const int c = j * V;
+  const bool col = c < a.C;
+  const long long t0 = (long long)blockIdx.x * sh.tokens;
+  const int toks = (int)min((long long)sh.tokens, a.tokens - t0);
+  const int rows = toks * a.K;
+  float* rowsum = lds;
+  float* rs = lds + sh.tokens * a.K;
+  const T* x = static_cast<const T*>(a.x) + t0 * a.K * a.C;
+  float v[R][V];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = i * per + rg;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[i][e] = 0.f;
+    if (col && r < rows) load_vec(x + (long long)r * a.C + c, v[i]);
+  }
+  const int nb = (a.C + kPackBlock - 1) / kPackBlock;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = i * per + rg;
+    if (CODES) {
+      constexpr int kLanes = kPackBlock / V;
+      const uint32_t scale = pack_scale(group_max_bits(max_bits(v[i]), min(kLanes, sh.lanes)));
+      if (col && r < rows) {
+        const long long row = t0 * a.K + r;
+        store_codes(a.codes + row * a.C + c, v[i], scale);
+        if (j % kLanes == 0) a.scales[row * nb + c / kPackBlock] = (uint8_t)scale;
+      }
+    }
+    const int tok = r / a.K;
+    if (r - tok * a.K == 0) {  // the invariants' row
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < V; ++e) s += v[i][e];
+      const float mean = group_sum(s, sh.lanes) / (float)a.C;
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i][e] = col ? v[i][e] - mean : 0.f;
+      if (a.mean && j == 0 && r < rows) a.mean[t0 + tok] = mean;
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) q = fmaf(v[i][e], v[i][e], q);
+    q = group_sum(q, sh.lanes);
+    if (j == 0 && r < rows) rowsum[r] = q;
+  }
+  __syncthreads();
+  const int degs = a.L + 1;
+  for (int i = tid; i < toks * degs; i += sh.threads) {
+    const int tok = i / degs, l = i - tok * degs;
+    const float* p = rowsum + tok * a.K + l * l;
+    float s = 0.f;
+    for (int m = 0; m < 2 * l + 1; ++m) s += p[m];
+    const float r = 1.f / __builtin_sqrtf(s / (float)((2 * l + 1) * a.C) + a.eps);
+    rs[i] = r;
+    if (a.rstd) a.rstd[t0 * degs + i] = r;
+  }
+  __syncthreads();
+  T* y = static_cast<T*>(a.y) + t0 * a.K * a.C;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = i * per + rg;
+    if (!col || r >= rows) continue;
+    const int tok = r / a.K, comp = r - tok * a.K, l = degree_of(comp);
+    const float m = rs[tok * degs + l];
+    float w[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[e] = m;
+    if (a.weight) {
+      load_vec(a.weight + l * a.C + c, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[e] *= m;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[i][e] *= w[e];
+    if (comp == 0 && a.bias) {
+      float b[V];
+      load_vec(a.bias + c, b);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i][e] += b[e];
+    }
+    store_vec(y + (long long)r * a.C + c, v[i]);
+  }
+}
+
+// Sum over the block (up to 16 waves), the same in every thread.
+__device__ __forceinline__ float block_sum(float v, float* lds, int threads) {
+  v = group_sum(v, 64);
+  if (threads == 64) return v;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = 0.f;
+  for (int w = 0; w < threads / 64; ++w) s += lds[w];
+  return s;
+}
+
+// Wide rows: block (token, degree), the degree's (2l+1) C values in registers.
+// CODES only where C is a multiple of 32 (a scale's lanes are then neighbours).
+template <class T, int V, int R, bool CODES>
+__global__ void norm_wide_kernel(NormArgs a) {
+  __shared__ float lds[16];
+  const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
+  const int n = (2 * l + 1) * a.C;
+  const long long t = blockIdx.x;
+  const long long base = (t * a.K + l * l) * a.C;
+  const T* x = static_cast<const T*>(a.x) + base;
+  float v[R][V];
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int e0 = (i * threads + tid) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[i][e] = 0.f;
+    if (e0 < n) load_vec(x + e0, v[i]);
+    if (CODES) {
+      constexpr int kLanes = kPackBlock / V;
+      const uint32_t scale = pack_scale(group_max_bits(max_bits(v[i]), kLanes));
+      if (e0 < n) {
+        store_codes(a.codes + base + e0, v[i], scale);
+        if (tid % kLanes == 0) a.scales[(base + e0) / kPackBlock] = (uint8_t)scale;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) s += v[i][e];
+  }
+  if (l == 0) {
+    const float mean = block_sum(s, lds, threads) / (float)a.C;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const bool here = (i * threads + tid) * V < n;
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i][e] = here ? v[i][e] - mean : 0.f;
+    }
+    if (a.mean && tid == 0) a.mean[t] = mean;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int e = 0; e < V; ++e) q = fmaf(v[i][e], v[i][e], q);
+  const float r = 1.f / __builtin_sqrtf(block_sum(q, lds, threads) / (float)n + a.eps);
+  if (a.rstd && tid == 0) a.rstd[t * (a.L + 1) + l] = r;
+  T* y = static_cast<T*>(a.y) + base;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int e0 = (i * threads + tid) * V;
+    if (e0 >= n) continue;
+    const int c = e0 % a.C;
+    float w[V], b[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[e] = 1.f, b[e] = 0.f;
+    if (a.weight) load_vec(a.weight + (long long)l * a.C + c, w);
+    if (l == 0 && a.bias) load_vec(a.bias + c, b);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[i][e] = fmaf(v[i][e] * r, w[e], b[e]);
+    store_vec(y + e0, v[i]);
+  }
+}
+
+// ---- backward --------------------------------------------------------------------
+
+// Input values of a row vector: x itself, or its 8-bit checkpoint.
+template <class T, int V, bool CODES>
+__device__ __forceinline__ void load_input(const NormBwdArgs& a, long long row, int c, int nb, float (&v)[V]) {
+  if (CODES)
+    load_codes(a.codes + row * a.C + c, a.scales[row * nb + c / kPackBlock], v);
+  else
+    load_vec(static_cast<const T*>(a.x) + row * a.C + c, v);
+}
+
+// Block b takes tiles b, b + gridDim.x, ... of sh.tokens tokens.  Dynamic LDS:
+// sums of rows and of degrees while the tiles run, then the staging of gw.
+// Partial sums of block b: part[b][L+1 degrees, then gb][C].
+constexpr int kBwdRowThreads = 512;
+
+template <class T, int V, int R, bool CODES>
+__global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdArgs a, RowShape sh, long long tiles) {
+  extern __shared__ float lds[];
+  const int tid = threadIdx.x, per = sh.threads / sh.lanes;
+  const int j = tid & (sh.lanes - 1), rg = tid / sh.lanes;
+  const int c = j * V;
+  const bool col = c < a.C;
+  const int nb = (a.C + kPackBlock - 1) / kPackBlock, degs = a.L + 1;
+  float* rowsum = lds;
+  float* ds = lds + sh.tokens * a.K;  // mean(g h) of every degree
+  float gw[R][V], gb[V];
+  int tok[R], comp[R], deg[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = i * per + rg;
+    tok[i] = r / a.K;
+    comp[i] = r - tok[i] * a.K;
+    deg[i] = degree_of(comp[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) gw[i][e] = 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) gb[e] = 0.f;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const long long t0 = tile * sh.tokens;
+    const int toks = (int)min((long long)sh.tokens, a.tokens - t0);
+    const T* gy = static_cast<const T*>(a.gy) + t0 * a.K * a.C;
+    float h[R][V], g[R][V], m0[R], r0[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[i][e] = g[i][e] = 0.f;
+      m0[i] = r0[i] = 0.f;
+      if (col && tok[i] < toks) {
+        const int r = i * per + rg;
+        load_input<T, V, CODES>(a, t0 * a.K + r, c, nb, h[i]);
+        load_vec(gy + (long long)r * a.C + c, g[i]);
+        r0[i] = a.rstd[(t0 + tok[i]) * degs + deg[i]];
+        if (comp[i] == 0) m0[i] = a.mean[t0 + tok[i]];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float w[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[e] = 1.f;
+      if (a.weight && col) load_vec(a.weight + deg[i] * a.C + c, w);
+      float q = 0.f, s = 0.f;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        h[i][e] = (h[i][e] - m0[i]) * r0[i];
+        gw[i][e] = fmaf(g[i][e], h[i][e], gw[i][e]);
+        if (comp[i] == 0) gb[e] += g[i][e];
+        g[i][e] *= w[e];
+        q = fmaf(g[i][e], h[i][e], q);
+        s += g[i][e];
+      }
+      q = group_sum(q, sh.lanes);
+      if (comp[i] == 0) {
+        s = group_sum(s, sh.lanes) / (float)a.C;
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[i][e] -= s;
+      }
+      if (j == 0 && tok[i] < toks) rowsum[i * per + rg] = q;
+    }
+    __syncthreads();
+    for (int i = tid; i < toks * degs; i += sh.threads) {
+      const int t = i / degs, l = i - t * degs;
+      const float* p = rowsum + t * a.K + l * l;
+      float s = 0.f;
+      for (int m = 0; m < 2 * l + 1; ++m) s += p[m];
+      ds[i] = s / (float)((2 * l + 1) * a.C);
+    }
+    __syncthreads();
+    if (a.gx) {
+      T* gx = static_cast<T*>(a.gx) + t0 * a.K * a.C;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        if (!col || tok[i] >= toks) continue;
+        const float d = ds[tok[i] * degs + deg[i]];
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = r0[i] * fmaf(-h[i][e], d, g[i][e]);
+        store_vec(gx + (long long)(i * per + rg) * a.C + c, o);
+      }
+    }
+    // the next tile writes rowsum only, which every thread has read before the
+    // second barrier, and ds after its own first barrier
+  }
+  if (!a.part) return;
+  // gw of the block: all rows through LDS, each output adds its degree's rows
+  float* part = a.part + (long long)blockIdx.x * (degs + 1) * a.C;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (col) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) lds[(i * per + rg) * a.C + c + e] = gw[i][e];
+    }
+  __syncthreads();
+  for (int o = tid; o < degs * a.C; o += sh.threads) {
+    const int l = o / a.C, ch = o - l * a.C;
+    float s = 0.f;
+    for (int t = 0; t < sh.tokens; ++t)
+      for (int m = 0; m < 2 * l + 1; ++m) s += lds[(t * a.K + l * l + m) * a.C + ch];
+    part[o] = s;
+  }
+  __syncthreads();
+  if (col) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) lds[rg * a.C + c + e] = gb[e];
+  }
+  __syncthreads();
+  for (int ch = tid; ch < a.C; ch += sh.threads) {
+    float s = 0.f;
+    for (int r = 0; r < per; ++r) s += lds[r * a.C + ch];
+    part[degs * a.C + ch] = s;
+  }
+}
+
+// Wide rows: block (slot, degree) takes tokens slot, slot + gridDim.x, ...
+// Partial sums: part[slot][K components, then gb][C].
+template <class T, int V, int R, bool CODES>
+__global__ void norm_wide_bwd_kernel(NormBwdArgs a) {
+  __shared__ float lds[16];
+  const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
+  const int n = (2 * l + 1) * a.C, nb = (a.C + kPackBlock - 1) / kPackBlock;
+  float gw[R][V], gb[R][V];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int e = 0; e < V; ++e) gw[i][e] = gb[i][e] = 0.f;
+  for (long long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+    const long long row0 = t * a.K + l * l;
+    const float r0 = a.rstd[t * (a.L + 1) + l], m0 = l == 0 ? a.mean[t] : 0.f;
+    float h[R][V], g[R][V];
+    float q = 0.f, s = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int e0 = (i * threads + tid) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[i][e] = m0, g[i][e] = 0.f;
+      if (e0 < n) {
+        const int m = e0 / a.C;
+        load_input<T, V, CODES>(a, row0 + m, e0 - m * a.C, nb, h[i]);
+        load_vec(static_cast<const T*>(a.gy) + row0 * a.C + e0, g[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int e0 = (i * threads + tid) * V;
+      float w[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[e] = 1.f;
+      if (a.weight && e0 < n) load_vec(a.weight + (long long)l * a.C + e0 % a.C, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        h[i][e] = (h[i][e] - m0) * r0;
+        gw[i][e] = fmaf(g[i][e], h[i][e], gw[i][e]);
+        gb[i][e] += g[i][e];
+        g[i][e] *= w[e];
+        q = fmaf(g[i][e], h[i][e], q);
+        s += g[i][e];
+      }
+    }
+    if (!a.gx) continue;
+    const float d = block_sum(q, lds, threads) / (float)n;
+    const float m1 = l == 0 ? block_sum(s, lds, threads) / (float)n : 0.f;
+    T* gx = static_cast<T*>(a.gx) + row0 * a.C;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int e0 = (i * threads + tid) * V;
+      if (e0 >= n) continue;
+      float o[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] = r0 * fmaf(-h[i][e], d, g[i][e] - m1);
+      store_vec(gx + e0, o);
+    }
+  }
+  if (!a.part) return;
+  float* part = a.part + (long long)blockIdx.x * (a.K + 1) * a.C;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int e0 = (i * threads + tid) * V;
+    if (e0 >= n) continue;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      part[(long long)l * l * a.C + e0 + e] = gw[i][e];
+      if (l == 0) part[(long long)a.K * a.C + e0 + e] = gb[i][e];
+    }
+  }
+}
+
+// Adds the blocks' partial sums: block of 16 slices x 64 outputs, a slice adds
+// every 16th block's sum, in a fixed order.  per_degree: rows of part are the
+// degrees (row form), else the K components.
+constexpr int kSumSlices = 16;
+__global__ __launch_bounds__(64 * kSumSlices) void norm_sum_kernel(const float* __restrict__ part, int blocks, int L,
+                                                                   int K, int C, int per_degree, float* gw, float* gb) {
+  __shared__ float lds[kSumSlices][64];
+  const int o = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+  const int l = o / C, c = o - l * C;  // l = L + 1: gb
+  const int rows = (per_degree ? L + 1 : K) + 1;
+  float s = 0.f;
+  if (l <= L + 1) {
+    const bool bias = l == L + 1;
+    const int first = bias ? rows - 1 : (per_degree ? l : l * l), n = bias || per_degree ? 1 : 2 * l + 1;
+    for (int m = 0; m < n; ++m) {
+      const float* p = part + (long long)(first + m) * C + c;
+#pragma unroll 4
+      for (int b = slice; b < blocks; b += kSumSlices) s += p[(long long)b * rows * C];
+    }
+  }
+  lds[slice][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (slice == 0 && l <= L + 1) {
+    float t = 0.f;
+    for (int i = 0; i < kSumSlices; ++i) t += lds[i][threadIdx.x];
+    if (l == L + 1) {
+      if (gb) gb[c] = t;
+    } else if (gw) {
+      gw[o] = t;
+    }
+  }
+}
+
+// ---- launch shapes -----------------------------------------------------------------
+
+constexpr int kPassStep = 2;
+
+// Row form: the block and pass count that leave the fewest lanes without a row,
+// at most max_passes rows per thread and max_values values per block; 0 tokens
+// if a token does not fit.
+RowShape row_shape(int C, int K, int V, int max_passes, int max_threads, int max_values) {
+  RowShape best{1, 0, 0, 0};
+  const int vecs = (C + V - 1) / V;
+  if (vecs > 64) return best;
+  while (best.lanes < vecs) best.lanes *= 2;
+  double score = 0;
+  for (int threads = 256; threads <= max_threads; threads *= 2) {
+    const int per = threads / best.lanes;
+    for (int passes = kPassStep; passes <= max_passes; passes += kPassStep) {
+      const int tokens = per * passes / K;
+      if (tokens < 1 || threads * passes * V > max_values) continue;
+      const double use = (double)(tokens * K) / (per * passes) - (threads > 512 ? 0.1 : 0.0);
+      if (use > score + 0.02) {
+        score = use;
+        best.threads = threads;
+        best.passes = passes;
+        best.tokens = tokens;
+      }
+    }
+  }
+  return best;
+}
+
+struct WideShape {
+  int threads = 0, vecs = 0;  // vecs: per thread, a power of two
+};
+// Wide form: about 4 vectors a thread (8 for the largest rows).
+WideShape wide_shape(int n, int V, int max_vecs) {
+  WideShape w;
+  const int total = (n + V - 1) / V;
+  for (w.threads = 64; w.threads < 1024; w.threads *= 2)
+    if (total <= w.threads * std::min(4, max_vecs)) break;
+  w.vecs = 1;
+  while (w.vecs * w.threads < total) w.vecs *= 2;
+  return w;
+}
+
+constexpr int kBwdBlocks = 1024;
+int row_bwd_blocks(long long tokens, const RowShape& sh) {
+  const long long tiles = (tokens + sh.tokens - 1) / sh.tokens;
+  return (int)std::min<long long>(tiles, kBwdBlocks * 256 / sh.threads);
+}
+int wide_bwd_blocks(long long tokens, int L) {
+  return (int)std::min<long long>(tokens, std::max(64, 1024 / (L + 1)));
+}
+
+size_t row_lds_floats(const RowShape& sh, int K, int L) { return (size_t)sh.tokens * (K + L + 1); }
+
+template <class T, int V, int R>
+hipError_t norm_rows(const NormArgs& a, const RowShape& sh, hipStream_t s) {
+  const long long blocks = (a.tokens + sh.tokens - 1) / sh.tokens;
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const size_t lds = row_lds_floats(sh, a.K, a.L) * sizeof(float);
+  if (lds > 64 * 1024) return hipErrorInvalidValue;
+  if (a.codes)
+    hipLaunchKernelGGL((norm_rows_kernel<T, V, R, true>), dim3((unsigned)blocks), dim3(sh.threads), lds, s, a, sh);
+  else
+    hipLaunchKernelGGL((norm_rows_kernel<T, V, R, false>), dim3((unsigned)blocks), dim3(sh.threads), lds, s, a, sh);
+  return hipGetLastError();
+}
+
+template <class T, int V, int R>
+hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
+  if (a.tokens > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)a.tokens, a.L + 1);
+  if (a.codes && a.C % kPackBlock == 0) {
+    hipLaunchKernelGGL((norm_wide_kernel<T, V, R, true>), grid, dim3(threads), 0, s, a);
+    return hipGetLastError();
+  }
+  if (a.codes) {  // a scale's channels would straddle the lanes: a pass of its own
+    const hipError_t e = launch_pack(a.type, a.x, a.codes, a.scales, a.tokens * a.K, a.C, s);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((norm_wide_kernel<T, V, R, false>), grid, dim3(threads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class T, int V, int R>
+hipError_t norm_rows_bwd(const NormBwdArgs& a, const RowShape& sh, hipStream_t s) {
+  const long long tiles = (a.tokens + sh.tokens - 1) / sh.tokens;
+  const int blocks = row_bwd_blocks(a.tokens, sh);
+  const int per = sh.threads / sh.lanes;
+  const size_t lds = std::max(row_lds_floats(sh, a.K, a.L), a.part ? (size_t)per * R * a.C : 0) * sizeof(float);
+  if (lds > 64 * 1024) return hipErrorInvalidValue;
+  if (a.codes)
+    hipLaunchKernelGGL((norm_rows_bwd_kernel<T, V, R, true>), dim3(blocks), dim3(sh.threads), lds, s, a, sh, tiles);
+  else
+    hipLaunchKernelGGL((norm_rows_bwd_kernel<T, V, R, false>), dim3(blocks), dim3(sh.threads), lds, s, a, sh, tiles);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.part) return e;
+  hipLaunchKernelGGL(norm_sum_kernel, dim3(((a.L + 2) * a.C + 63) / 64), dim3(64 * kSumSlices), 0, s, a.part, blocks,
+                     a.L, a.K, a.C, 1, a.gw, a.gb);
+  return hipGetLastError();
+}
+
+template <class T, int V, int R>
+hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
+  const int blocks = wide_bwd_blocks(a.tokens, a.L);
+  const dim3 grid(blocks, a.L + 1);
+  if (a.codes)
+    hipLaunchKernelGGL((norm_wide_bwd_kernel<T, V, R, true>), grid, dim3(threads), 0, s, a);
+  else
+    hipLaunchKernelGGL((norm_wide_bwd_kernel<T, V, R, false>), grid, dim3(threads), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.part) return e;
+  hipLaunchKernelGGL(norm_sum_kernel, dim3(((a.L + 2) * a.C + 63) / 64), dim3(64 * kSumSlices), 0, s, a.part, blocks,
+                     a.L, a.K, a.C, 0, a.gw, a.gb);
+  return hipGetLastError();
+}
+
+// Values a thread holds of one array: 32 in the forward, 16 in the backward
+// (which holds four arrays).
+constexpr int kFwdPasses = 8;
+constexpr int fwd_values(int V) { return V >= 4 ? 32 : 16; }
+constexpr int kBwdValues = 16;
+constexpr int bwd_passes(int V) { return V >= 4 ? kBwdValues / V : 4; }
+// a block's gw is staged in at most 64 KiB of LDS
+RowShape bwd_row_shape(int C, int K, int V) { return row_shape(C, K, V, bwd_passes(V), kBwdRowThreads, 16384); }
+
+template <class T, int V>
+hipError_t norm_any(const NormArgs& a, hipStream_t s) {
+  const RowShape sh = row_shape(a.C, a.K, V, kFwdPasses, 1024, 1024 * 32);
+  if (sh.tokens) {
+    switch (sh.passes) {
+      case 2: return norm_rows<T, V, 2>(a, sh, s);
+      case 4: return norm_rows<T, V, 4>(a, sh, s);
+      case 6: return norm_rows<T, V, 6>(a, sh, s);
+      case 8: return norm_rows<T, V, 8>(a, sh, s);
+      default: return hipErrorInvalidValue;
+    }
+  }
+  constexpr int kMax = fwd_values(V) / V;
+  const WideShape w = wide_shape((2 * a.L + 1) * a.C, V, kMax);
+  if (w.vecs <= kMax) {
+    if (w.vecs <= 1) return norm_wide<T, V, 1>(a, w.threads, s);
+    if (w.vecs <= 4) return norm_wide<T, V, 4>(a, w.threads, s);
+    return norm_wide<T, V, kMax>(a, w.threads, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <class T, int V>
+hipError_t norm_bwd_any(const NormBwdArgs& a, hipStream_t s) {
+  const RowShape sh = bwd_row_shape(a.C, a.K, V);
+  if (sh.tokens) {
+    switch (sh.passes) {
+      case 2: return norm_rows_bwd<T, V, 2>(a, sh, s);
+      case 4: return norm_rows_bwd<T, V, V == 8 ? 2 : 4>(a, sh, s);
+      default: return hipErrorInvalidValue;
+    }
+  }
+  constexpr int kMax = kBwdValues / V;
+  const WideShape w = wide_shape((2 * a.L + 1) * a.C, V, kMax);
+  if (w.vecs <= kMax) {
+    if (w.vecs <= 1) return norm_wide_bwd<T, V, 1>(a, w.threads, s);
+    if (w.vecs <= 2) return norm_wide_bwd<T, V, 2>(a, w.threads, s);
+    return norm_wide_bwd<T, V, kMax>(a, w.threads, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t norm_bwd_part_bytes(long long tokens, int L, int C) {
+  const int K = (L + 1) * (L + 1);
+  size_t rows = 0;
+  for (int type : {SEQ_F32, SEQ_BF16}) {
+    const RowShape sh = bwd_row_shape(C, K, seq_vec(type, C));
+    rows = std::max(rows, sh.tokens ? (size_t)row_bwd_blocks(tokens, sh) * (L + 2)
+                                    : (size_t)wide_bwd_blocks(tokens, L) * (K + 1));
+  }
+  return rows * C * sizeof(float);
+}
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  const int v = seq_vec(a.type, a.C);
+  if (a.type == SEQ_BF16) {
+    switch (v) {
+      case 8: return norm_any<bf16, 8>(a, s);
+      case 4: return norm_any<bf16, 4>(a, s);
+      case 2: return norm_any<bf16, 2>(a, s);
+      default: return norm_any<bf16, 1>(a, s);
+    }
+  }
+  switch (v) {
+    case 4: return norm_any<float, 4>(a, s);
+    case 2: return norm_any<float, 2>(a, s);
+    default: return norm_any<float, 1>(a, s);
+  }
+}
+
+hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t s) {
+  const int v = seq_vec(a.type, a.C);
+  if (a.type == SEQ_BF16) {
+    switch (v) {
+      case 8: return norm_bwd_any<bf16, 8>(a, s);
+      case 4: return norm_bwd_any<bf16, 4>(a, s);
+      case 2: return norm_bwd_any<bf16, 2>(a, s);
+      default: return norm_bwd_any<bf16, 1>(a, s);
+    }
+  }
+  switch (v) {
+    case 4: return norm_bwd_any<float, 4>(a, s);
+    case 2: return norm_bwd_any<float, 2>(a, s);
+    default: return norm_bwd_any<float, 1>(a, s);
+  }
+}
+
+}  // namespace cgconv

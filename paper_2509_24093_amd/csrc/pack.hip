@@ -1,0 +1,87 @@
+// Activation checkpoints in 8 bits (format: seq_common.h): rows of C channels
+// of any tensor to int8 codes and one power-of-two scale byte per 32 channels,
+// and back.  Both directions are streams, bound by HBM.
+#include <hip/hip_runtime.h>
+
+#include "seq_common.h"
+
+namespace cgconv {
+
+namespace {
+
+using namespace seqdev;
+
+constexpr int kThreads = 256;
+
+// One group of V lanes-worth of elements per thread: the 32 / V lanes of a
+// scale's channels are neighbours, and a row's last group leaves lanes idle.
+template <class T, int V, bool PACK>
+__global__ __launch_bounds__(kThreads) void pack_kernel(const T* __restrict__ x, const int8_t* __restrict__ codes_in,
+                                                        const uint8_t* __restrict__ scales_in, T* __restrict__ out,
+                                                        int8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                        long long groups, int C, int nb) {
+  constexpr int kLanes = kPackBlock / V;
+  const long long thread = (long long)blockIdx.x * kThreads + threadIdx.x;
+  const long long g = thread / kLanes;
+  if (g >= groups) return;
+  const int j = (int)(thread % kLanes);
+  const long long row = g / nb;
+  const int c = (int)(g - row * nb) * kPackBlock + j * V;
+  const bool here = c < C;
+  const long long at = row * C + c;
+  float v[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = 0.f;
+  if (PACK) {
+    if (here) load_vec(x + at, v);
+    const uint32_t scale = pack_scale(group_max_bits(max_bits(v), kLanes));
+    if (here) store_codes(codes + at, v, scale);
+    if (j == 0) scales[g] = (uint8_t)scale;
+  } else if (here) {
+    load_codes(codes_in + at, scales_in[g], v);
+    store_vec(out + at, v);
+  }
+}
+
+template <class T, int V, bool PACK>
+hipError_t launch(const void* x, int8_t* codes, uint8_t* scales, void* out, long long rows, int C, hipStream_t s) {
+  const int nb = (int)pack_blocks(C);
+  const long long groups = rows * nb;
+  const long long blocks = (groups * (kPackBlock / V) + kThreads - 1) / kThreads;
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((pack_kernel<T, V, PACK>), dim3((unsigned)blocks), dim3(kThreads), 0, s,
+                     static_cast<const T*>(x), codes, scales, static_cast<T*>(out), codes, scales, groups, C, nb);
+  return hipGetLastError();
+}
+
+template <bool PACK>
+hipError_t launch_any(int type, const void* x, int8_t* codes, uint8_t* scales, void* out, long long rows, int C,
+                      hipStream_t s) {
+  const int v = seq_vec(type, C);
+  if (type == SEQ_BF16) {
+    switch (v) {
+      case 8: return launch<bf16, 8, PACK>(x, codes, scales, out, rows, C, s);
+      case 4: return launch<bf16, 4, PACK>(x, codes, scales, out, rows, C, s);
+      case 2: return launch<bf16, 2, PACK>(x, codes, scales, out, rows, C, s);
+      default: return launch<bf16, 1, PACK>(x, codes, scales, out, rows, C, s);
+    }
+  }
+  switch (v) {
+    case 4: return launch<float, 4, PACK>(x, codes, scales, out, rows, C, s);
+    case 2: return launch<float, 2, PACK>(x, codes, scales, out, rows, C, s);
+    default: return launch<float, 1, PACK>(x, codes, scales, out, rows, C, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_pack(int type, const void* x, int8_t* codes, uint8_t* scales, long long rows, int C, hipStream_t s) {
+  return launch_any<true>(type, x, codes, scales, nullptr, rows, C, s);
+}
+
+hipError_t launch_unpack(int type, const int8_t* codes, const uint8_t* scales, void* x, long long rows, int C,
+                         hipStream_t s) {
+  return launch_any<false>(type, nullptr, const_cast<int8_t*>(codes), const_cast<uint8_t*>(scales), x, rows, C, s);
+}
+
+}  // namespace cgconv

@@ -1,0 +1,316 @@
+"""Operators around the convolution on [batch, tokens, (L+1)^2, C] features:
+layer norm by degree and activation checkpoints in 8 bits (``include/cgconv.h``,
+"Sequence operators").  As in the package's main module, every step runs in the
+library's HIP kernels; this module checks and marshals arguments.
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+CGCONV_F32 = 0
+CGCONV_BF16 = 1
+CGCONV_SEQ_TOKENS = 2147483647
+CGCONV_SEQ_SEGMENT = 16384
+CGCONV_SEQ_STATES = 32
+
+_vp, _i64, _i32, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
+
+# name: (argument types, result type); bound when the library is loaded
+SIGNATURES = {
+    "cgconv_seq_plan_create": ([_i64, _i64, _i32, _i64, _i32], _vp),
+    "cgconv_seq_plan_destroy": ([_vp], None),
+    "cgconv_seq_plan_info": ([_vp, ctypes.POINTER(ctypes.c_size_t)], ctypes.c_int),
+    "cgconv_seq_norm": ([_vp, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
+    "cgconv_seq_norm_backward": ([_vp, _i32] + [_vp] * 11, ctypes.c_int),
+    "cgconv_pack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
+    "cgconv_unpack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
+}
+
+
+def bind(lib) -> None:
+    for name, (args, res) in SIGNATURES.items():
+        f = getattr(lib, name)
+        f.argtypes = args
+        f.restype = res
+
+
+def _main():
+    import paper_2509_24093_amd as P
+    return P
+
+
+# ---- C ABI, same names -------------------------------------------------------
+
+def cgconv_seq_plan_create(batch: int, N: int, L_max: int, C: int, states: int = 0) -> int:
+    P = _main()
+    h = P.library().cgconv_seq_plan_create(batch, N, L_max, C, states)
+    if not h:
+        raise P.CgconvError(P.CGCONV_ERR_INVALID_ARG, P.cgconv_last_error())
+    return h
+
+
+def cgconv_seq_plan_destroy(plan: int) -> None:
+    _main().library().cgconv_seq_plan_destroy(plan)
+
+
+def cgconv_seq_plan_info(plan: int) -> int:
+    """Workspace bytes."""
+    P = _main()
+    n = ctypes.c_size_t()
+    P._check(P.library().cgconv_seq_plan_info(plan, ctypes.byref(n)))
+    return n.value
+
+
+def cgconv_seq_norm(plan, dtype, x, weight, bias, eps, y, mean, rstd, codes, scales, stream) -> int:
+    """Layer norm by degree (device pointers; weight, bias, the statistics and
+    the checkpoint may be None)."""
+    P = _main()
+    return P._check(P.library().cgconv_seq_norm(plan, dtype, x, weight, bias, eps, y, mean, rstd, codes, scales,
+                                                stream))
+
+
+def cgconv_seq_norm_backward(plan, dtype, x, codes, scales, weight, mean, rstd, grad_y, grad_x, grad_weight,
+                             grad_bias, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_norm_backward(plan, dtype, x, codes, scales, weight, mean, rstd, grad_y,
+                                                         grad_x, grad_weight, grad_bias, stream))
+
+
+def cgconv_pack8(dtype, rows, C, x, codes, scales, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_pack8(dtype, rows, C, x, codes, scales, stream))
+
+
+def cgconv_unpack8(dtype, rows, C, codes, scales, x, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_unpack8(dtype, rows, C, codes, scales, x, stream))
+
+
+# ---- tensors -------------------------------------------------------------------
+
+def _dtype_code(name, dtype) -> int:
+    import torch
+    if dtype == torch.float32:
+        return CGCONV_F32
+    if dtype == torch.bfloat16:
+        return CGCONV_BF16
+    raise ValueError(f"{name} must be float32 or bfloat16")
+
+
+def _tensor(name, t, shape, dtype, device):
+    """t's address after its checks; None stays None."""
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.device.index != device:
+        raise ValueError(f"{name} is on GPU {t.device.index}, expected GPU {device}")
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _scale_shape(shape):
+    return tuple(shape[:-1]) + ((shape[-1] + 31) // 32,)
+
+
+def checkpoint_pack(x):
+    """8-bit checkpoint of a contiguous fp32 or bf16 GPU tensor of any shape
+    [..., C]: int8 codes of its shape and one power-of-two scale byte per 32
+    channels, [..., ceil(C / 32)]; 1.03 bytes a value instead of 4 or 2."""
+    import torch
+    P = _main()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.ndim < 1 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous GPU tensor")
+    code = _dtype_code("x", x.dtype)
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty(_scale_shape(x.shape), dtype=torch.uint8, device=x.device)
+    if x.numel() == 0:
+        return codes, scales
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError(f"x is on GPU {x.device.index}, which is not current")
+    C = x.shape[-1]
+    cgconv_pack8(code, x.numel() // C, C, x.data_ptr(), codes.data_ptr(), scales.data_ptr(), P._current_stream(torch))
+    return codes, scales
+
+
+def checkpoint_unpack(codes, scales, dtype=None, out=None):
+    """The values of a checkpoint, in float32 (default) or bfloat16."""
+    import torch
+    P = _main()
+    dtype = (out.dtype if out is not None else torch.float32) if dtype is None else dtype
+    code = _dtype_code("dtype", dtype)
+    if not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.ndim < 1:
+        raise ValueError("codes must be a GPU tensor")
+    device = codes.device.index
+    if out is None:
+        out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    args = (_tensor("codes", codes, codes.shape, torch.int8, device),
+            _tensor("scales", scales, _scale_shape(codes.shape), torch.uint8, device),
+            _tensor("out", out, codes.shape, dtype, device))
+    if codes.numel() == 0:
+        return out
+    if device != torch.cuda.current_device():
+        raise ValueError(f"codes is on GPU {device}, which is not current")
+    C = codes.shape[-1]
+    cgconv_unpack8(code, codes.numel() // C, C, *args, P._current_stream(torch))
+    return out
+
+
+def _want_checkpoint(checkpoint) -> bool:
+    if checkpoint not in (None, "int8"):
+        raise ValueError("checkpoint must be None or 'int8'")
+    return checkpoint == "int8"
+
+
+def keep(ctx, checkpoint: bool, tensors, others=()):
+    """Saves tensors for the backward pass, whole or as 8-bit checkpoints, and
+    others as they are."""
+    if checkpoint:
+        saved = [s for t in tensors for s in checkpoint_pack(t)]
+        ctx.kept_dtypes = [t.dtype for t in tensors]
+    else:
+        saved = list(tensors)
+        ctx.kept_dtypes = None
+    ctx.n_kept = len(tensors)
+    ctx.save_for_backward(*saved, *others)
+
+
+def kept(ctx):
+    """(the tensors, the others) of :func:`keep`, unpacked."""
+    saved = ctx.saved_tensors
+    if ctx.kept_dtypes is None:
+        return saved[:ctx.n_kept], saved[ctx.n_kept:]
+    n = 2 * ctx.n_kept
+    return [checkpoint_unpack(saved[2 * i], saved[2 * i + 1], dtype) for i, dtype in enumerate(ctx.kept_dtypes)], saved[n:]
+
+
+class SequencePlan:
+    """Sizes and workspace of the sequence operators for features
+    [batch, N, (L_max+1)^2, C] (fp32 or bf16) on the current GPU."""
+
+    def __init__(self, batch: int, N: int, L_max: int, C: int, states: int = 0):
+        self._h = None
+        self._h = cgconv_seq_plan_create(int(batch), int(N), int(L_max), int(C), int(states))
+        import torch
+        self.device = torch.cuda.current_device()
+        self.batch, self.N, self.L_max, self.C, self.states = int(batch), int(N), int(L_max), int(C), int(states)
+        self.shape = (self.batch, self.N, (self.L_max + 1) ** 2, self.C)
+
+    def info(self) -> int:
+        """Workspace bytes."""
+        return cgconv_seq_plan_info(self._h)
+
+    def _features(self, name, t, dtype):
+        return _tensor(name, t, self.shape, dtype, self.device)
+
+    def _empty(self, shape, dtype):
+        import torch
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", self.device))
+
+    def norm(self, x, weight=None, bias=None, eps: float = 1e-5, checkpoint: bool = False, out=None):
+        """Layer norm by degree (L_max = 0: the ordinary layer norm): weight
+        [L_max+1, C] and bias [C], fp32 or None.  Returns (y, mean [batch, N],
+        rstd [batch, N, L_max+1]), and the 8-bit checkpoint (codes, scales) of x
+        behind them if asked for."""
+        import torch
+        P = _main()
+        code = _dtype_code("x", x.dtype)
+        f32 = torch.float32
+        px = self._features("x", x, x.dtype)
+        if out is None:
+            out = self._empty(self.shape, x.dtype)
+        mean, rstd = self._empty(self.shape[:2], f32), self._empty(self.shape[:2] + (self.L_max + 1,), f32)
+        codes = scales = None
+        if checkpoint:
+            codes = self._empty(self.shape, torch.int8)
+            scales = self._empty(_scale_shape(self.shape), torch.uint8)
+        cgconv_seq_norm(self._h, code, px, _tensor("weight", weight, (self.L_max + 1, self.C), f32, self.device),
+                        _tensor("bias", bias, (self.C,), f32, self.device), eps, self._features("out", out, x.dtype),
+                        mean.data_ptr(), rstd.data_ptr(), codes.data_ptr() if checkpoint else None,
+                        scales.data_ptr() if checkpoint else None, P._current_stream(torch))
+        return (out, mean, rstd, codes, scales) if checkpoint else (out, mean, rstd)
+
+    def norm_backward(self, x, weight, mean, rstd, grad_y, need_x: bool = True, need_weight: bool = True,
+                      need_bias: bool = True):
+        """(grad_x, grad_weight, grad_bias) given grad_y and the forward's
+        statistics; x is the input or its checkpoint (codes, scales).  A
+        gradient that is not needed is None."""
+        import torch
+        P = _main()
+        if not (need_x or need_weight or need_bias):
+            return None, None, None
+        f32, dtype = torch.float32, grad_y.dtype
+        code = _dtype_code("grad_y", dtype)
+        px = pc = ps = None
+        if isinstance(x, (tuple, list)):
+            codes, scales = x
+            pc = _tensor("codes", codes, self.shape, torch.int8, self.device)
+            ps = _tensor("scales", scales, _scale_shape(self.shape), torch.uint8, self.device)
+        else:
+            px = self._features("x", x, dtype)
+        args = (self._h, code, px, pc, ps, _tensor("weight", weight, (self.L_max + 1, self.C), f32, self.device),
+                _tensor("mean", mean, self.shape[:2], f32, self.device),
+                _tensor("rstd", rstd, self.shape[:2] + (self.L_max + 1,), f32, self.device),
+                self._features("grad_y", grad_y, dtype))
+        gx = self._empty(self.shape, dtype) if need_x else None
+        gw = self._empty((self.L_max + 1, self.C), f32) if need_weight else None
+        gb = self._empty((self.C,), f32) if need_bias else None
+        cgconv_seq_norm_backward(*args, *(None if t is None else t.data_ptr() for t in (gx, gw, gb)),
+                                 P._current_stream(torch))
+        return gx, gw, gb
+
+    def close(self):
+        if getattr(self, "_h", None):
+            cgconv_seq_plan_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_functions = {}
+
+
+def _grad_wanted(*tensors) -> bool:
+    import torch
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
+def _norm_function():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _NormFn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, plan, eps, checkpoint):
+            y, *rest = plan.norm(x, weight, bias, eps, checkpoint=checkpoint)
+            stats, held = rest[:2], rest[2:] if checkpoint else [x]
+            ctx.save_for_backward(weight, *stats, *held)
+            ctx.plan = plan
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_y):
+            weight, mean, rstd, *held = ctx.saved_tensors
+            need = ctx.needs_input_grad
+            return ctx.plan.norm_backward(held if len(held) == 2 else held[0], weight, mean, rstd,
+                                          grad_y.contiguous(), need[0], need[1], need[2]) + (None, None, None)
+
+    return _NormFn
+
+
+def cgconv_norm(x, weight, bias, plan: SequencePlan, eps: float = 1e-5, checkpoint=None):
+    """Differentiable layer norm by degree in x, weight and bias (weight and
+    bias may be None).  checkpoint="int8": the input is kept for the backward
+    pass in 8 bits, written by the forward kernel and read by the backward."""
+    wanted = _want_checkpoint(checkpoint) and _grad_wanted(x, weight, bias)
+    if "norm" not in _functions:
+        _functions["norm"] = _norm_function()
+    return _functions["norm"].apply(x, weight, bias, plan, eps, wanted)

@@ -1,0 +1,119 @@
+"""Refusals of the sequence plan's entry points, on the CPU with stand-ins for
+the HIP runtime (tests/host_runtime.py): nothing is launched for a bad call."""
+
+import os
+
+import pytest
+
+import paper_2509_24093_amd as P
+from tests.host_runtime import run
+
+pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libcgconv.so not built")
+
+HEAD = """
+lib = P.library()
+def refused(status, word, want):
+    got = status, P.cgconv_last_error()
+    assert status == want and word in got[1], (got, word, want)
+    assert launches() == []
+INVALID, UNSUPPORTED, ALIGNMENT = P.CGCONV_ERR_INVALID_ARG, P.CGCONV_ERR_UNSUPPORTED, P.CGCONV_ERR_ALIGNMENT
+"""
+
+
+def test_plan_create_refuses_bad_sizes(tmp_path):
+    run(tmp_path, HEAD + """
+for args, word in (((0, 4, 1, 8, 0), "invalid sizes"), ((65536, 4, 1, 8, 0), "invalid sizes"),
+                   ((1, 0, 1, 8, 0), "invalid sizes"), ((1, 4, 1, 0, 0), "invalid sizes"),
+                   ((1, 4, 1, 8, -1), "invalid sizes"), ((1, 4, -1, 8, 0), "unsupported L_max"),
+                   ((1, 4, 9, 8, 0), "unsupported L_max"), ((1, 4, 1, 8, 33), "unsupported states"),
+                   ((1, 4, 0, 16385, 0), "unsupported C"), ((1, 4, 8, 964, 0), "unsupported C"),
+                   ((1, 4, 8, 2**62, 0), "unsupported C"), ((2, 2**31, 0, 1, 0), "batch*N"),
+                   ((65535, 2**62, 0, 1, 0), "batch*N")):
+    assert not lib.cgconv_seq_plan_create(*args), args
+    assert word in P.cgconv_last_error(), (args, P.cgconv_last_error())
+plan = P.cgconv_seq_plan_create(2, 8, 1, 16)
+assert P.cgconv_seq_plan_info(plan) > 0
+refused(lib.cgconv_seq_plan_info(None, None), "NULL", INVALID)
+P.cgconv_seq_plan_destroy(plan)
+P.cgconv_seq_plan_destroy(None)
+""")
+
+
+def test_norm_refuses_bad_calls(tmp_path):
+    run(tmp_path, HEAD + """
+plan = P.cgconv_seq_plan_create(2, 8, 1, 16)
+names = ("x", "weight", "bias", "eps", "y", "mean", "rstd", "codes", "scales")
+def norm(plan=plan, dtype=0, **kw):
+    a = dict(x=ptr(0), weight=ptr(1), bias=ptr(2), eps=1e-5, y=ptr(3), mean=ptr(4), rstd=ptr(5), codes=ptr(6), scales=ptr(7))
+    a.update(kw)
+    return lib.cgconv_seq_norm(plan, dtype, *(a[n] for n in names), None)
+assert norm() == 0 and len(launches()) == 1
+assert norm(weight=None, bias=None, mean=None, rstd=None, codes=None, scales=None) == 0 and len(launches()) == 1
+refused(norm(plan=None), "plan is NULL", INVALID)
+refused(norm(dtype=2), "dtype", INVALID)
+refused(norm(x=None), "x must", INVALID)
+refused(norm(y=None), "y must", INVALID)
+refused(norm(mean=None), "together", INVALID)
+refused(norm(codes=None), "together", INVALID)
+refused(norm(eps=-1.0), "eps", INVALID)
+refused(norm(eps=float("nan")), "eps", INVALID)
+refused(norm(x=ptr(0) + 4), "aligned", ALIGNMENT)
+refused(norm(scales=ptr(7) + 8), "aligned", ALIGNMENT)
+refused(norm(y=ptr(0)), "overlap", INVALID)
+refused(norm(y=ptr(0) + 2 * 8 * 4 * 16 * 4 - 16), "overlap", INVALID)
+refused(norm(rstd=ptr(4)), "overlap", INVALID)
+assert norm(y=ptr(0) + 2 * 8 * 4 * 16 * 4) == 0
+launches()
+names2 = ("x", "codes", "scales", "weight", "mean", "rstd", "grad_y", "grad_x", "grad_weight", "grad_bias")
+def back(plan=plan, dtype=0, **kw):
+    a = dict(x=ptr(0), codes=None, scales=None, weight=ptr(1), mean=ptr(2), rstd=ptr(3), grad_y=ptr(4), grad_x=ptr(5),
+             grad_weight=ptr(6), grad_bias=ptr(7))
+    a.update(kw)
+    return lib.cgconv_seq_norm_backward(plan, dtype, *(a[n] for n in names2), None)
+assert back() == 0 and len(launches()) == 2
+assert back(grad_weight=None, grad_bias=None) == 0 and len(launches()) == 1
+assert back(x=None, codes=ptr(8), scales=ptr(9)) == 0 and len(launches()) == 2
+refused(back(plan=None), "plan is NULL", INVALID)
+refused(back(x=None), "either x", INVALID)
+refused(back(codes=ptr(8), scales=ptr(9)), "either x", INVALID)
+refused(back(x=None, codes=ptr(8)), "either x", INVALID)
+refused(back(mean=None), "mean must", INVALID)
+refused(back(rstd=None), "rstd must", INVALID)
+refused(back(grad_y=None), "grad_y must", INVALID)
+refused(back(grad_x=None, grad_weight=None, grad_bias=None), "at least one", INVALID)
+refused(back(grad_x=ptr(4)), "overlap", INVALID)
+refused(back(grad_bias=ptr(6)), "overlap", INVALID)
+""")
+
+
+def test_pack_refuses_bad_calls(tmp_path):
+    run(tmp_path, HEAD + """
+for f in (lib.cgconv_pack8, lib.cgconv_unpack8):
+    assert f(0, 10, 40, ptr(0), ptr(1), ptr(2), None) == 0 and len(launches()) == 1
+    refused(f(3, 10, 40, ptr(0), ptr(1), ptr(2), None), "dtype", INVALID)
+    refused(f(0, 0, 40, ptr(0), ptr(1), ptr(2), None), "invalid sizes", INVALID)
+    refused(f(0, 10, 0, ptr(0), ptr(1), ptr(2), None), "invalid sizes", INVALID)
+    refused(f(0, 2**62, 2, ptr(0), ptr(1), ptr(2), None), "invalid sizes", INVALID)
+    refused(f(0, 2**40, 32, ptr(0), ptr(1), ptr(2), None), "too many", UNSUPPORTED)
+    refused(f(0, 10, 40, None, ptr(1), ptr(2), None), "non-NULL", INVALID)
+    refused(f(0, 10, 40, ptr(0), ptr(1) + 8, ptr(2), None), "aligned", ALIGNMENT)
+    refused(f(0, 10, 40, ptr(0), ptr(1), ptr(1), None), "overlap", INVALID)
+""")
+
+
+def test_norm_launches_are_within_limits(tmp_path):
+    run(tmp_path, """
+for L in range(9):
+    for C in (1, 2, 3, 4, 7, 8, 16, 20, 32, 33, 64, 100, 128, 250, 256, 257, 500, 512, 963, 1000, 4096, 16384):
+        if (2 * L + 1) * C > 16384:
+            continue
+        for B, N in ((1, 1), (3, 70), (8, 16384)):
+            plan = P.cgconv_seq_plan_create(B, N, L, C)
+            for dtype in (0, 1):
+                big = lambda i: 1 << (44 + i) if i else 1 << 43
+                assert P.library().cgconv_seq_norm(plan, dtype, big(0), big(1), big(2), 0.0, big(3), big(4), big(5), big(6), big(7), None) == 0, P.cgconv_last_error()
+                assert P.library().cgconv_seq_norm_backward(plan, dtype, big(0), None, None, big(1), big(2), big(3), big(4), big(5), big(6), big(7), None) == 0, P.cgconv_last_error()
+                for grid, block, lds, allowed in launches():
+                    assert block[0] <= 1024 and block[0] % 64 == 0 and lds <= allowed and grid[1] <= 65535, (L, C, grid, block, lds)
+            P.cgconv_seq_plan_destroy(plan)
+""")
