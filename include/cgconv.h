@@ -398,15 +398,18 @@ const char* cgconv_plan_stage_name(cgconv_plan_t plan, int32_t stage);
 /*
  * ---- Sequence operators ----------------------------------------------------
  *
- * What a block has around the convolution: layer norm by degree and activation
+ * What a block has around the convolution: layer norm by degree, a short causal
+ * convolution and a selective state space scan (the causal mixer with a state of
+ * constant size, for whole sequences and single tokens), and activation
  * checkpoints in 8 bits.  Features are [batch][N][(L_max+1)^2][C] as above, in
  * fp32 or bfloat16 (CGCONV_F32, CGCONV_BF16: the features and their gradients;
  * parameters, statistics and all arithmetic are fp32, an output is rounded once,
  * to nearest, ties to even).  L_max = 0 is the ordinary layout of scalars.
  *
  * A sequence plan holds the sizes and the workspace.  1 <= batch <= 65535, N >= 1
- * (any), batch * N <= CGCONV_SEQ_TOKENS, 0 <= L_max <= CGCONV_LMAX, C >= 1 with
- * (2 L_max + 1) C <= CGCONV_SEQ_SEGMENT, 0 <= states <= CGCONV_SEQ_STATES.  As for
+ * (any), batch * N <= CGCONV_SEQ_TOKENS, batch * N * K * C <= CGCONV_SEQ_VALUES, 0 <=
+ * L_max <= CGCONV_LMAX, C >= 1 with (2 L_max + 1) C <= CGCONV_SEQ_SEGMENT; states:
+ * S of the scans, 0 (no scans: a smaller workspace) .. CGCONV_SEQ_STATES.  As for
  * the other plans: created synchronously, its device must be current at every
  * call, calls only enqueue kernels (capturable), and calls of one plan share its
  * workspace, so two of them must not be in flight on different streams (nor in
@@ -415,9 +418,11 @@ const char* cgconv_plan_stage_name(cgconv_plan_t plan, int32_t stage);
  */
 typedef struct cgconv_seq_plan* cgconv_seq_plan_t;
 enum cgconv_dtype { CGCONV_F32 = 0, CGCONV_BF16 = 1 };
-#define CGCONV_SEQ_TOKENS 2147483647
+#define CGCONV_SEQ_TOKENS (1 << 30)
+#define CGCONV_SEQ_VALUES (1LL << 38)
 #define CGCONV_SEQ_SEGMENT 16384
 #define CGCONV_SEQ_STATES 32
+#define CGCONV_SEQ_WIDTH 8
 
 cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states);
 void cgconv_seq_plan_destroy(cgconv_seq_plan_t plan); /* NULL is a no-op */
@@ -455,6 +460,64 @@ int cgconv_seq_norm(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const 
 int cgconv_seq_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const int8_t* codes,
                              const uint8_t* scales, const float* weight, const float* mean, const float* rstd,
                              const void* grad_y, void* grad_x, float* grad_weight, float* grad_bias,
+                             hipStream_t stream);
+
+/*
+ * Short causal convolution of every component and channel over the tokens,
+ * width W = 2..CGCONV_SEQ_WIDTH, depthwise, one filter per degree and channel:
+ *
+ *   z[t,(l,m),c] = sum_{j<W} weight[j,l,c] x[t-j,(l,m),c] + [l = 0] bias[c]
+ *   y = z, with activation != 0: the invariants y[(0,0)] = z sigmoid(z)
+ *
+ * weight [W][L_max+1][C], bias [C] (or NULL), fp32.  lengths: int32 [batch] or NULL
+ * (N): tokens at and behind a sequence's length are not read, their outputs are
+ * zero (values outside 0..N count as the nearest of them).  state_in: the W - 1
+ * inputs before the first token, oldest first, [batch][W-1][K][C] of dtype, or
+ * NULL (zeros); state_out (or NULL) receives the W - 1 inputs before every
+ * sequence's end.  A prompt in pieces, each with the state of the one before, is
+ * the prompt.  cgconv_seq_conv_step: one token of every sequence, x and y
+ * [batch][K][C], the state moved on in place.  The backward is from the zero
+ * state; any of its outputs may be NULL, not all.
+ */
+int cgconv_seq_conv(cgconv_seq_plan_t plan, int32_t dtype, int32_t width, const void* x, const float* weight,
+                    const float* bias, int32_t activation, const int32_t* lengths, const void* state_in, void* y,
+                    void* state_out, hipStream_t stream);
+int cgconv_seq_conv_step(cgconv_seq_plan_t plan, int32_t dtype, int32_t width, const void* x, const float* weight,
+                         const float* bias, int32_t activation, void* state, void* y, hipStream_t stream);
+int cgconv_seq_conv_backward(cgconv_seq_plan_t plan, int32_t dtype, int32_t width, const void* x,
+                             const float* weight, const float* bias, int32_t activation, const int32_t* lengths,
+                             const void* grad_y, void* grad_x, float* grad_weight, float* grad_bias,
+                             hipStream_t stream);
+
+/*
+ * Selective state space scan, S = the plan's states per component and channel;
+ * its coefficients are invariants, so it commutes with rotations:
+ *
+ *   step_t[c] = log(1 + exp(delta_t[c] + delta_bias[c]))
+ *   h_t[s,k,c] = exp(step_t[c] A[c,s]) h_{t-1}[s,k,c] + step_t[c] Bt_t[s] x_t[k,c]
+ *   y_t[k,c] = sum_s Ct_t[s] h_t[s,k,c] + D[c] x_t[k,c]
+ *
+ * x, y [batch][N][K][C], delta [batch][N][C], Bt, Ct [batch][N][S] of dtype; A [C][S],
+ * D and delta_bias [C] (or NULL: zeros), fp32; the states are fp32.  A should not
+ * be positive (the decays then are at most 1; a positive A may overflow).
+ * lengths as for the convolution.  state_in [batch][S][K][C] (or NULL: zeros) is
+ * the state before the first token, state_out (or NULL) receives the one after
+ * every sequence's last token.  cgconv_seq_scan_step: one token of every sequence
+ * (x, y [batch][K][C], delta [batch][C], Bt, Ct [batch][S]), the state in place.
+ * The backward is from the zero state and takes no gradient of the final state;
+ * any of its outputs (grad_A, grad_D, grad_delta_bias fp32) may be NULL, not all.
+ * All its sums have a fixed order.
+ */
+int cgconv_seq_scan(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* delta, const float* A,
+                    const void* Bt, const void* Ct, const float* D, const float* delta_bias, const int32_t* lengths,
+                    const float* state_in, void* y, float* state_out, hipStream_t stream);
+int cgconv_seq_scan_step(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* delta, const float* A,
+                         const void* Bt, const void* Ct, const float* D, const float* delta_bias, float* state,
+                         void* y, hipStream_t stream);
+int cgconv_seq_scan_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* delta, const float* A,
+                             const void* Bt, const void* Ct, const float* D, const float* delta_bias,
+                             const int32_t* lengths, const void* grad_y, void* grad_x, void* grad_delta,
+                             float* grad_A, void* grad_Bt, void* grad_Ct, float* grad_D, float* grad_delta_bias,
                              hipStream_t stream);
 
 /*

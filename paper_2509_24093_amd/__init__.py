@@ -22,14 +22,24 @@ from .sequence import (  # noqa: F401
     CGCONV_SEQ_SEGMENT,
     CGCONV_SEQ_STATES,
     CGCONV_SEQ_TOKENS,
+    CGCONV_SEQ_VALUES,
+    CGCONV_SEQ_WIDTH,
     SequencePlan,
     cgconv_norm,
     cgconv_pack8,
+    cgconv_scan,
+    cgconv_seq_conv,
+    cgconv_seq_conv_backward,
+    cgconv_seq_conv_step,
     cgconv_seq_norm,
     cgconv_seq_norm_backward,
     cgconv_seq_plan_create,
     cgconv_seq_plan_destroy,
     cgconv_seq_plan_info,
+    cgconv_seq_scan,
+    cgconv_seq_scan_backward,
+    cgconv_seq_scan_step,
+    cgconv_short_conv,
     cgconv_unpack8,
     checkpoint_pack,
     checkpoint_unpack,

@@ -63,6 +63,9 @@ def build(jobs: int | None = None, verbose: bool = True) -> str:
         ([HIPCC, "-x", "hip", "-c"] + HIP_FLAGS, "sequence.cpp", "sequence.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "norm.hip", "norm.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "pack.hip", "pack.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "conv.hip", "conv.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "scan.hip", "scan.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "scan_bwd.hip", "scan_bwd.o", []),
     ]
     for P in (3, 5, 7):
         units.append(([HIPCC, "-c"] + HIP_FLAGS, "fft_odd.hip", "fft_odd_P%d.o" % P, ["-DCGCONV_TU_P=%d" % P]))

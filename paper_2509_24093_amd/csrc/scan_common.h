@@ -1,0 +1,88 @@
+// Device side shared by the selective scan's forward (scan.hip) and backward
+// (scan_bwd.hip).
+//
+//   delta = softplus(raw[t,c] + bias[c])
+//   h_t[s,k,c] = exp(delta A[c,s]) h_{t-1}[s,k,c] + delta B_t[s] x_t[k,c]
+//   y_t[k,c] = sum_s C_t[s] h_t[s,k,c] + D[c] x_t[k,c]
+//
+// Lanes are channels (of one or several components), so B_t and C_t are the
+// same for a whole wave: a preparing kernel writes them as fp32 rows of SP
+// states each (SP = S rounded up, zeros behind S), and the scans read them
+// through the scalar cache as scalar operands.  The states stay in registers.
+#pragma once
+
+#include "seq_common.h"
+
+namespace cgconv {
+namespace seqdev {
+
+typedef const __attribute__((address_space(4))) float* ConstFloats;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// exp(v) as 2^(v log2 e) of the hardware.  a is pre-scaled by log2 e.
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|) in (0, 1]; log1p(e) = 2
+// atanh(u), u = e / (2 + e) <= 1/3, by its series in u^2 <= 1/9: the first term
+// left out is u^17 2/17, below 2^-30 of the sum.
+__device__ __forceinline__ float softplus(float v) {
+  const float e = exp2_fast(-fabsf(v) * kLog2e);
+  const float u = e * __builtin_amdgcn_rcpf(2.f + e), q = u * u;
+  float p = 2.f / 15.f;
+  p = fmaf(p, q, 2.f / 13.f);
+  p = fmaf(p, q, 2.f / 11.f);
+  p = fmaf(p, q, 2.f / 9.f);
+  p = fmaf(p, q, 2.f / 7.f);
+  p = fmaf(p, q, 2.f / 5.f);
+  p = fmaf(p, q, 2.f / 3.f);
+  p = fmaf(p, q, 2.f);
+  return fmaxf(v, 0.f) + p * u;
+}
+
+__device__ __forceinline__ int scan_length(const int* lengths, int b, int N) {
+  return lengths ? min(max(lengths[b], 0), N) : N;
+}
+
+template <class T>
+__device__ __forceinline__ float load1(const void* p, long long i) {
+  return widen(static_cast<const T*>(p)[i]);
+}
+
+}  // namespace seqdev
+
+constexpr int kScanThreads = 256;
+
+// Tokens in chunks; a chunk's states at its start are [B][chunks][S][K C].
+struct ScanChunks {
+  int chunk, chunks;
+};
+inline int scan_padded(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : 32; }
+
+// Workspace: parts of one allocation, 256-byte aligned.
+struct ScanSpace {
+  float* bc = nullptr;   // [B][N][2 SP]: B_t, C_t
+  float* hs = nullptr;   // [B][chunks][S][K C]: states at the chunks' ends, then starts
+  float* ds = nullptr;   // [B][chunks][C]: sum of delta over a chunk
+  // backward
+  float* rs = nullptr;   // [B][chunks][S][K C]: gradients of the states behind a chunk
+  float* gbc = nullptr;  // [column blocks][B][N][2 SP]: of B_t, C_t
+  float* gd = nullptr;   // [B][N][K][C]: the components' parts of delta's
+  float* ga = nullptr;   // [B][chunks][S + 1][K C]: of A and (last) D over a chunk
+  float* gbp = nullptr;  // [token blocks][C]: of the bias
+  size_t bytes = 0;
+  void place(void* base, float** p, size_t floats) {
+    *p = reinterpret_cast<float*>(static_cast<char*>(base) + bytes);
+    bytes += (floats * sizeof(float) + 255) / 256 * 256;
+  }
+};
+
+size_t scan_forward_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
+size_t scan_backward_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
+
+hipError_t launch_scan_prepare(const ScanArgs& a, float* bc, hipStream_t s);
+hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const float* first, float* hs, const float* ds,
+                             bool reverse, hipStream_t s);
+hipError_t launch_scan_local(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, hipStream_t s);
+
+}  // namespace cgconv

@@ -70,4 +70,68 @@ hipError_t launch_pack(int type, const void* x, int8_t* codes, uint8_t* scales, 
 hipError_t launch_unpack(int type, const int8_t* codes, const uint8_t* scales, void* x, long long rows, int C,
                          hipStream_t s);
 
+// ---- short causal convolution --------------------------------------------------
+
+constexpr int kConvMaxWidth = 8;
+struct ConvArgs {
+  int type;
+  const void* x;        // [B][N][K][C] (a step: [B][K][C])
+  const float* weight;  // [W][L+1][C]
+  const float* bias;    // [C] or nullptr
+  const int* lengths;   // [B] or nullptr
+  const void* state_in;  // [B][W-1][K][C] or nullptr (zeros)
+  void* y;
+  void* state_out;       // or nullptr; a step's state, in place
+  int B, N, L, K, C, W;
+  int activation;
+};
+struct ConvBwdArgs {
+  ConvArgs a;  // y and the states unused
+  const void* gy;
+  void* gx;    // or nullptr
+  float* gw;   // [W][L+1][C] or nullptr
+  float* gb;   // [C] or nullptr
+  float* part;  // conv_bwd_part_bytes, or nullptr if neither gw nor gb is wanted
+};
+hipError_t launch_conv(const ConvArgs& a, hipStream_t s);
+hipError_t launch_conv_step(const ConvArgs& a, hipStream_t s);
+hipError_t launch_conv_backward(const ConvBwdArgs& g, hipStream_t s);
+size_t conv_bwd_part_bytes(int64_t B, int64_t N, int K, int64_t C);
+
+// ---- selective scan --------------------------------------------------------------
+
+constexpr int kScanMaxStates = 32;
+struct ScanArgs {
+  int type;
+  const void* x;      // [B][N][K][C] (a step: [B][K][C])
+  const void* delta;  // [B][N][C]
+  const float* A;     // [C][S]
+  const void* Bt;     // [B][N][S]
+  const void* Ct;
+  const float* D;     // [C] or nullptr
+  const float* bias;  // [C] or nullptr
+  const int* lengths;  // [B] or nullptr
+  const float* state_in;  // [B][S][K][C] or nullptr (zeros)
+  void* y;
+  float* state_out;  // or nullptr; a step's state, in place
+  int B, N, K, C, S;
+  float* ws;  // scan_workspace_bytes
+};
+struct ScanBwdArgs {
+  ScanArgs a;  // y and the states unused
+  const void* gy;
+  void* gx;      // the gradients, in the inputs' types (fp32 for A, D, bias);
+  void* gdelta;  // any may be nullptr
+  float* gA;
+  void* gB;
+  void* gC;
+  float* gD;
+  float* gbias;
+};
+hipError_t launch_scan(const ScanArgs& a, hipStream_t s);
+hipError_t launch_scan_step(const ScanArgs& a, hipStream_t s);
+hipError_t launch_scan_backward(const ScanBwdArgs& g, hipStream_t s);
+// workspace of both directions
+size_t scan_workspace_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
+
 }  // namespace cgconv

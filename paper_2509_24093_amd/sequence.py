@@ -1,6 +1,7 @@
 """Operators around the convolution on [batch, tokens, (L+1)^2, C] features:
-layer norm by degree and activation checkpoints in 8 bits (``include/cgconv.h``,
-"Sequence operators").  As in the package's main module, every step runs in the
+layer norm by degree, the short causal convolution and the selective state space
+scan (whole sequences and single tokens), and activation checkpoints in 8 bits
+(``include/cgconv.h``, "Sequence operators").  As in the package's main module, every step runs in the
 library's HIP kernels; this module checks and marshals arguments.
 """
 
@@ -10,9 +11,11 @@ import ctypes
 
 CGCONV_F32 = 0
 CGCONV_BF16 = 1
-CGCONV_SEQ_TOKENS = 2147483647
+CGCONV_SEQ_TOKENS = 1 << 30
+CGCONV_SEQ_VALUES = 1 << 38
 CGCONV_SEQ_SEGMENT = 16384
 CGCONV_SEQ_STATES = 32
+CGCONV_SEQ_WIDTH = 8
 
 _vp, _i64, _i32, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
 
@@ -23,6 +26,12 @@ SIGNATURES = {
     "cgconv_seq_plan_info": ([_vp, ctypes.POINTER(ctypes.c_size_t)], ctypes.c_int),
     "cgconv_seq_norm": ([_vp, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
     "cgconv_seq_norm_backward": ([_vp, _i32] + [_vp] * 11, ctypes.c_int),
+    "cgconv_seq_conv": ([_vp, _i32, _i32, _vp, _vp, _vp, _i32] + [_vp] * 5, ctypes.c_int),
+    "cgconv_seq_conv_step": ([_vp, _i32, _i32, _vp, _vp, _vp, _i32] + [_vp] * 3, ctypes.c_int),
+    "cgconv_seq_conv_backward": ([_vp, _i32, _i32, _vp, _vp, _vp, _i32] + [_vp] * 6, ctypes.c_int),
+    "cgconv_seq_scan": ([_vp, _i32] + [_vp] * 12, ctypes.c_int),
+    "cgconv_seq_scan_step": ([_vp, _i32] + [_vp] * 10, ctypes.c_int),
+    "cgconv_seq_scan_backward": ([_vp, _i32] + [_vp] * 17, ctypes.c_int),
     "cgconv_pack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
     "cgconv_unpack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
 }
@@ -75,6 +84,46 @@ def cgconv_seq_norm_backward(plan, dtype, x, codes, scales, weight, mean, rstd, 
     P = _main()
     return P._check(P.library().cgconv_seq_norm_backward(plan, dtype, x, codes, scales, weight, mean, rstd, grad_y,
                                                          grad_x, grad_weight, grad_bias, stream))
+
+
+def cgconv_seq_conv(plan, dtype, width, x, weight, bias, activation, lengths, state_in, y, state_out, stream) -> int:
+    """Short causal convolution (bias, lengths and the states may be None)."""
+    P = _main()
+    return P._check(P.library().cgconv_seq_conv(plan, dtype, width, x, weight, bias, activation, lengths, state_in, y,
+                                                state_out, stream))
+
+
+def cgconv_seq_conv_step(plan, dtype, width, x, weight, bias, activation, state, y, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_conv_step(plan, dtype, width, x, weight, bias, activation, state, y, stream))
+
+
+def cgconv_seq_conv_backward(plan, dtype, width, x, weight, bias, activation, lengths, grad_y, grad_x, grad_weight,
+                             grad_bias, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_conv_backward(plan, dtype, width, x, weight, bias, activation, lengths,
+                                                         grad_y, grad_x, grad_weight, grad_bias, stream))
+
+
+def cgconv_seq_scan(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, lengths, state_in, y, state_out, stream) -> int:
+    """Selective scan (D, delta_bias, lengths and the states may be None)."""
+    P = _main()
+    return P._check(P.library().cgconv_seq_scan(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, lengths, state_in, y,
+                                                state_out, stream))
+
+
+def cgconv_seq_scan_step(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, state, y, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_scan_step(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, state, y,
+                                                     stream))
+
+
+def cgconv_seq_scan_backward(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, lengths, grad_y, grad_x, grad_delta,
+                             grad_A, grad_Bt, grad_Ct, grad_D, grad_delta_bias, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_scan_backward(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, lengths,
+                                                         grad_y, grad_x, grad_delta, grad_A, grad_Bt, grad_Ct, grad_D,
+                                                         grad_delta_bias, stream))
 
 
 def cgconv_pack8(dtype, rows, C, x, codes, scales, stream) -> int:
@@ -262,6 +311,146 @@ class SequencePlan:
                                  P._current_stream(torch))
         return gx, gw, gb
 
+    # ---- short causal convolution
+
+    def _conv_args(self, x, weight, bias, shape):
+        import torch
+        f32 = torch.float32
+        code = _dtype_code("x", x.dtype)
+        if not isinstance(weight, torch.Tensor) or weight.ndim != 3:
+            raise ValueError(f"weight must be a GPU tensor of shape [width, {self.L_max + 1}, {self.C}]")
+        width = int(weight.shape[0])
+        return (self._h, code, width, _tensor("x", x, shape, x.dtype, self.device),
+                _tensor("weight", weight, (width, self.L_max + 1, self.C), f32, self.device),
+                _tensor("bias", bias, (self.C,), f32, self.device))
+
+    def _lengths(self, lengths):
+        import torch
+        return _tensor("lengths", lengths, (self.batch,), torch.int32, self.device)
+
+    def conv_state(self, width: int, dtype=None):
+        """The state before the first token: zeros [batch, width - 1, K, C]."""
+        import torch
+        return self._empty((self.batch, width - 1) + self.shape[2:], dtype or torch.float32).zero_()
+
+    def conv(self, x, weight, bias=None, lengths=None, state=None, activation: bool = True, out=None):
+        """Short causal convolution over the tokens: weight [width, L_max+1, C]
+        and bias [C], fp32; the invariants pass z sigmoid(z) unless activation
+        is False.  lengths (int32 [batch]): tokens behind them are not read,
+        their outputs are zero.  Returns (y, state): the width - 1 inputs before
+        every sequence's end, [batch, width - 1, K, C], for conv_step or the
+        next piece (state=)."""
+        import torch
+        P = _main()
+        args = self._conv_args(x, weight, bias, self.shape)
+        if out is None:
+            out = self._empty(self.shape, x.dtype)
+        state_shape = (self.batch, max(args[2] - 1, 0)) + self.shape[2:]
+        last = self._empty(state_shape, x.dtype)
+        cgconv_seq_conv(*args, int(bool(activation)), self._lengths(lengths),
+                        _tensor("state", state, state_shape, x.dtype, self.device),
+                        self._features("out", out, x.dtype), last.data_ptr(), P._current_stream(torch))
+        return out, last
+
+    def conv_step(self, x, weight, bias, state, activation: bool = True, out=None):
+        """One token of every sequence: x [batch, K, C]; state is moved on in
+        place.  Returns y [batch, K, C]."""
+        import torch
+        P = _main()
+        shape = (self.batch,) + self.shape[2:]
+        args = self._conv_args(x, weight, bias, shape)
+        if out is None:
+            out = self._empty(shape, x.dtype)
+        cgconv_seq_conv_step(*args, int(bool(activation)),
+                             _tensor("state", state, (self.batch, max(args[2] - 1, 0)) + self.shape[2:], x.dtype,
+                                     self.device),
+                             _tensor("out", out, shape, x.dtype, self.device), P._current_stream(torch))
+        return out
+
+    def conv_backward(self, x, weight, bias, grad_y, lengths=None, activation: bool = True, need_x: bool = True,
+                      need_weight: bool = True, need_bias: bool = True):
+        """(grad_x, grad_weight, grad_bias) given grad_y, from the zero state; a
+        gradient that is not needed is None."""
+        import torch
+        P = _main()
+        if not (need_x or need_weight or need_bias):
+            return None, None, None
+        args = self._conv_args(x, weight, bias, self.shape) + (
+            int(bool(activation)), self._lengths(lengths), self._features("grad_y", grad_y, x.dtype))
+        gx = self._empty(self.shape, x.dtype) if need_x else None
+        gw = self._empty(weight.shape, torch.float32) if need_weight else None
+        gb = self._empty((self.C,), torch.float32) if need_bias else None
+        cgconv_seq_conv_backward(*args, *(None if t is None else t.data_ptr() for t in (gx, gw, gb)),
+                                 P._current_stream(torch))
+        return gx, gw, gb
+
+    # ---- selective scan
+
+    def _scan_args(self, x, delta, A, Bt, Ct, D, delta_bias, tokens):
+        import torch
+        f32 = torch.float32
+        code = _dtype_code("x", x.dtype)
+        lead = (self.batch,) + tokens
+        S, C, dev = self.states, self.C, self.device
+        return (self._h, code, _tensor("x", x, lead + self.shape[2:], x.dtype, dev),
+                _tensor("delta", delta, lead + (C,), x.dtype, dev), _tensor("A", A, (C, S), f32, dev),
+                _tensor("Bt", Bt, lead + (S,), x.dtype, dev), _tensor("Ct", Ct, lead + (S,), x.dtype, dev),
+                _tensor("D", D, (C,), f32, dev), _tensor("delta_bias", delta_bias, (C,), f32, dev))
+
+    def scan_state(self):
+        """The state before the first token: fp32 zeros [batch, S, K, C]."""
+        import torch
+        return self._empty((self.batch, self.states) + self.shape[2:], torch.float32).zero_()
+
+    def scan(self, x, delta, A, Bt, Ct, D=None, delta_bias=None, lengths=None, state=None, out=None):
+        """Selective scan of whole sequences: delta [batch, N, C], Bt and Ct
+        [batch, N, S] of x's type, A [C, S], D and delta_bias [C] in fp32.
+        Returns (y, state): the state [batch, S, K, C] (fp32) after every
+        sequence's last token, for scan_step or the next piece (state=)."""
+        import torch
+        P = _main()
+        args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, (self.N,))
+        if out is None:
+            out = self._empty(self.shape, x.dtype)
+        state_shape = (self.batch, self.states) + self.shape[2:]
+        last = self._empty(state_shape, torch.float32)
+        cgconv_seq_scan(*args, self._lengths(lengths),
+                        _tensor("state", state, state_shape, torch.float32, self.device),
+                        self._features("out", out, x.dtype), last.data_ptr(), P._current_stream(torch))
+        return out, last
+
+    def scan_step(self, x, delta, A, Bt, Ct, D, state, delta_bias=None, out=None):
+        """One token of every sequence: x [batch, K, C], delta [batch, C], Bt
+        and Ct [batch, S]; state is moved on in place.  Returns y [batch, K, C]."""
+        import torch
+        P = _main()
+        args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, ())
+        shape = (self.batch,) + self.shape[2:]
+        if out is None:
+            out = self._empty(shape, x.dtype)
+        cgconv_seq_scan_step(*args, _tensor("state", state, (self.batch, self.states) + self.shape[2:],
+                                            torch.float32, self.device),
+                             _tensor("out", out, shape, x.dtype, self.device), P._current_stream(torch))
+        return out
+
+    def scan_backward(self, x, delta, A, Bt, Ct, D, grad_y, delta_bias=None, lengths=None, need=(True,) * 7):
+        """Gradients of (x, delta, A, Bt, Ct, D, delta_bias) given grad_y, from
+        the zero state; None where ``need`` is False."""
+        import torch
+        P = _main()
+        if not any(need):
+            return (None,) * 7
+        f32 = torch.float32
+        args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, (self.N,)) + (
+            self._lengths(lengths), self._features("grad_y", grad_y, x.dtype))
+        lead = (self.batch, self.N)
+        shapes = ((self.shape, x.dtype), (lead + (self.C,), x.dtype), ((self.C, self.states), f32),
+                  (lead + (self.states,), x.dtype), (lead + (self.states,), x.dtype), ((self.C,), f32), ((self.C,), f32))
+        grads = tuple(self._empty(*s) if n else None for s, n in zip(shapes, need))
+        cgconv_seq_scan_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
+                                 P._current_stream(torch))
+        return grads
+
     def close(self):
         if getattr(self, "_h", None):
             cgconv_seq_plan_destroy(self._h)
@@ -314,3 +503,70 @@ def cgconv_norm(x, weight, bias, plan: SequencePlan, eps: float = 1e-5, checkpoi
     if "norm" not in _functions:
         _functions["norm"] = _norm_function()
     return _functions["norm"].apply(x, weight, bias, plan, eps, wanted)
+
+
+def _conv_function():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _ConvFn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, lengths, plan, activation, packed):
+            y, _ = plan.conv(x, weight, bias, lengths, activation=activation)
+            keep(ctx, packed, (x,), (weight, bias, lengths))
+            ctx.plan, ctx.activation = plan, activation
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_y):
+            (x,), (weight, bias, lengths) = kept(ctx)
+            need = ctx.needs_input_grad
+            return ctx.plan.conv_backward(x, weight, bias, grad_y.contiguous(), lengths, ctx.activation, need[0],
+                                          need[1], need[2]) + (None,) * 4
+
+    return _ConvFn
+
+
+def cgconv_short_conv(x, weight, bias, plan: SequencePlan, lengths=None, activation: bool = True, checkpoint=None):
+    """Differentiable short causal convolution (:meth:`SequencePlan.conv`, from
+    the zero state) in x, weight and bias (may be None).  checkpoint="int8": x
+    is kept for the backward pass in 8 bits."""
+    packed = _want_checkpoint(checkpoint) and _grad_wanted(x, weight, bias)
+    if "conv" not in _functions:
+        _functions["conv"] = _conv_function()
+    return _functions["conv"].apply(x, weight, bias, lengths, plan, activation, packed)
+
+
+def _scan_function():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _ScanFn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, delta, A, Bt, Ct, D, delta_bias, lengths, plan, packed):
+            y, _ = plan.scan(x, delta, A, Bt, Ct, D, delta_bias, lengths)
+            keep(ctx, packed, (x,), (delta, A, Bt, Ct, D, delta_bias, lengths))
+            ctx.plan = plan
+            return y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_y):
+            (x,), (delta, A, Bt, Ct, D, delta_bias, lengths) = kept(ctx)
+            need = tuple(n and t is not None
+                         for n, t in zip(ctx.needs_input_grad, (x, delta, A, Bt, Ct, D, delta_bias)))
+            return ctx.plan.scan_backward(x, delta, A, Bt, Ct, D, grad_y.contiguous(), delta_bias, lengths,
+                                          need) + (None,) * 3
+
+    return _ScanFn
+
+
+def cgconv_scan(x, delta, A, Bt, Ct, D, plan: SequencePlan, delta_bias=None, lengths=None, checkpoint=None):
+    """Differentiable selective scan (:meth:`SequencePlan.scan`, from the zero
+    state) in all its inputs; D and delta_bias may be None.  checkpoint="int8":
+    x is kept for the backward pass in 8 bits (delta, Bt and Ct whole)."""
+    packed = _want_checkpoint(checkpoint) and _grad_wanted(x, delta, A, Bt, Ct, D, delta_bias)
+    if "scan" not in _functions:
+        _functions["scan"] = _scan_function()
+    return _functions["scan"].apply(x, delta, A, Bt, Ct, D, delta_bias, lengths, plan, packed)
