@@ -36,9 +36,10 @@ struct Column {
   }
 };
 
-constexpr int kAhead = 4;  // tokens loaded ahead of their use
+// Tokens whose x and delta are loaded while the ones before are computed.
+constexpr int kAhead = 4;
 
-// LOCAL: pass (1), else pass (3) from `starts` (or the caller's state, or zero).
+// LOCAL: pass (1), else pass (3) from pass (2)'s states (or the caller's, or zero).
 template <class T, int KG, int SP, bool LOCAL>
 __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChunks sh, ScanSpace ws, int colblocks) {
   const int ch = blockIdx.x / colblocks, b = blockIdx.y;
@@ -47,10 +48,30 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
   const int t0 = ch * sh.chunk, t1 = min(a.N, t0 + sh.chunk), t2 = min(t1, len);
   const long long KC = (long long)a.K * a.C;
   const long long col = (long long)q.k0 * a.C + q.c;
+  const long long row0 = (long long)b * a.N;
+  const T* xp = static_cast<const T*>(a.x) + row0 * KC + col;
+  T* yp = static_cast<T*>(a.y) + row0 * KC + col;
+  const T* dp = static_cast<const T*>(a.delta) + row0 * a.C + q.c;
+  const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
+  float dn[kAhead], xn[kAhead][KG];
+  auto fetch = [&](int tb) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = min(tb + u, t2 - 1);
+      dn[u] = widen(dp[(long long)t * a.C]);
+#pragma unroll
+      for (int i = 0; i < KG; ++i) xn[u][i] = i < q.nk ? widen(xp[t * KC + (long long)i * a.C]) : 0.f;
+    }
+  };
+  TokenRow<SP> p;
+  if (t0 < t2) {
+    fetch(t0);
+    p.load(bc + (long long)t0 * 2 * SP);
+  }
   float A2[SP], h[SP][KG];
 #pragma unroll
   for (int s = 0; s < SP; ++s) {
-    A2[s] = s < a.S ? a.A[(long long)q.c * a.S + s] * kLog2e : 0.f;
+    A2[s] = ws.A2[s * a.C + q.c];
 #pragma unroll
     for (int i = 0; i < KG; ++i) h[s][i] = 0.f;
   }
@@ -65,41 +86,37 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
         if (s < a.S && i < q.nk) h[s][i] = start[s * KC + col + (long long)i * a.C];
   }
   const float bias = a.bias ? a.bias[q.c] : 0.f, D = !LOCAL && a.D ? a.D[q.c] : 0.f;
-  const long long row0 = (long long)b * a.N;
-  const T* xp = static_cast<const T*>(a.x) + row0 * KC + col;
-  T* yp = static_cast<T*>(a.y) + row0 * KC + col;
-  const T* dp = static_cast<const T*>(a.delta) + row0 * a.C + q.c;
-  const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
   float total = 0.f;
   for (int tb = t0; tb < t2; tb += kAhead) {
-    float dn[kAhead], xn[kAhead][KG];
+    float dc[kAhead], xc[kAhead][KG];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int t = min(tb + u, t2 - 1);
-      dn[u] = widen(dp[(long long)t * a.C]);
+      dc[u] = dn[u];
 #pragma unroll
-      for (int i = 0; i < KG; ++i) xn[u][i] = i < q.nk ? widen(xp[t * KC + (long long)i * a.C]) : 0.f;
+      for (int i = 0; i < KG; ++i) xc[u][i] = xn[u][i];
     }
+    if (tb + kAhead < t2) fetch(tb + kAhead);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int t = tb + u;
       if (t >= t2) break;
-      const float d = softplus(dn[u] + bias);
+      TokenRow<SP> next;
+      next.load(bc + (long long)min(t + 1, t2 - 1) * 2 * SP);
+      const float d = softplus(dc[u] + bias);
       if (LOCAL) total += d;
       float dx[KG], y[KG];
 #pragma unroll
       for (int i = 0; i < KG; ++i) {
-        dx[i] = d * xn[u][i];
-        y[i] = D * xn[u][i];
+        dx[i] = d * xc[u][i];
+        y[i] = D * xc[u][i];
       }
-      const ConstFloats p = bc + (long long)t * 2 * SP;
 #pragma unroll
       for (int s = 0; s < SP; ++s) {
         const float e = exp2_fast(d * A2[s]);
 #pragma unroll
         for (int i = 0; i < KG; ++i) {
-          h[s][i] = fmaf(e, h[s][i], p[s] * dx[i]);
-          if (!LOCAL) y[i] = fmaf(p[SP + s], h[s][i], y[i]);
+          h[s][i] = fmaf(e, h[s][i], p.v[s] * dx[i]);
+          if (!LOCAL) y[i] = fmaf(p.v[SP + s], h[s][i], y[i]);
         }
       }
       if (!LOCAL && q.here) {
@@ -107,6 +124,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
         for (int i = 0; i < KG; ++i)
           if (i < q.nk) yp[t * KC + (long long)i * a.C] = (T)y[i];
       }
+      p = next;
     }
   }
   if (!q.here) return;
@@ -128,50 +146,78 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
   if (LOCAL && q.k0 == 0) ws.ds[((long long)b * sh.chunks + ch) * a.C + q.c] = total;
 }
 
-// Pass (2): one thread per state, from chunk to chunk (backwards for the
-// gradients).  hs: in, what a chunk adds; out, what it starts with.
-template <bool REVERSE>
-__global__ __launch_bounds__(kScanThreads) void carry_kernel(ScanArgs a, ScanChunks sh, const float* first, float* hs,
-                                                             const float* ds) {
+// Pass (2): h <- exp(A ds) h + add from chunk to chunk, for 64 states per block;
+// each of its kCarrySlices waves first composes its own run of chunks, then
+// starts from the runs before it.  The arrays hold, in, what a chunk adds and,
+// out, what it starts with; y = 1 of the grid goes through rs backwards.  The
+// chunk at the far end adds to nobody and need not be formed.
+constexpr int kCarrySlices = 8;
+__global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, ScanChunks sh, ScanSpace ws,
+                                                                  const float* first) {
+  __shared__ float scale[kCarrySlices][64], shift[kCarrySlices][64];
   const long long KC = (long long)a.K * a.C;
-  const long long id = (long long)blockIdx.x * kScanThreads + threadIdx.x;
-  const int b = blockIdx.y;
-  if (id >= a.S * KC) return;
+  const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, b = blockIdx.z;
+  const bool reverse = blockIdx.y;
+  const long long col = (long long)blockIdx.x * 64 + lane;
+  const bool here = col < a.S * KC;
+  const long long id = here ? col : 0;
   const int s = (int)(id / KC), c = (int)((id - s * KC) % a.C);
-  const float A2 = a.A[(long long)c * a.S + s] * kLog2e;
-  float h = first ? first[(long long)b * a.S * KC + id] : 0.f;
-  float* p = hs + (long long)b * sh.chunks * a.S * KC + id;
-  const float* d = ds + (long long)b * sh.chunks * a.C + c;
+  const float A2 = ws.A2[s * a.C + c];
+  float* p = (reverse ? ws.rs : ws.hs) + (long long)b * sh.chunks * a.S * KC + id;
+  const float* d = ws.ds + (long long)b * sh.chunks * a.C + c;
+  const int run = (sh.chunks + kCarrySlices - 1) / kCarrySlices;
+  const int n0 = slice * run, n1 = min(n0 + run, sh.chunks);
   constexpr int kBatch = 8;
-  for (int n = 0; n < sh.chunks; n += kBatch) {
-    float add[kBatch], e[kBatch];
+  auto load = [&](int n, float (&add)[kBatch], float (&e)[kBatch]) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int ch = REVERSE ? sh.chunks - 1 - (n + i) : n + i;
-      // the chunk at the far end adds to nobody and was not formed
-      const bool last = n + i >= sh.chunks - 1;
-      add[i] = last ? 0.f : p[ch * a.S * KC];
-      e[i] = last ? 1.f : exp2_fast(A2 * d[(long long)ch * a.C]);
+      const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
+      const bool in = n + i < n1 && n + i < sh.chunks - 1;
+      add[i] = in ? p[ch * a.S * KC] : 0.f;
+      e[i] = in ? exp2_fast(A2 * d[(long long)ch * a.C]) : 1.f;
     }
+  };
+  float E = 1.f, H = 0.f;
+  for (int n = n0; n < n1; n += kBatch) {
+    float add[kBatch], e[kBatch];
+    load(n, add, e);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      if (n + i >= sh.chunks) break;
-      const int ch = REVERSE ? sh.chunks - 1 - (n + i) : n + i;
+      H = fmaf(e[i], H, add[i]);
+      E *= e[i];
+    }
+  }
+  scale[slice][lane] = E;
+  shift[slice][lane] = H;
+  __syncthreads();
+  float h = first && !reverse ? first[(long long)b * a.S * KC + id] : 0.f;
+  for (int i = 0; i < slice; ++i) h = fmaf(scale[i][lane], h, shift[i][lane]);
+  if (!here) return;
+  for (int n = n0; n < n1; n += kBatch) {
+    float add[kBatch], e[kBatch];
+    load(n, add, e);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (n + i >= n1) break;
+      const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
       p[ch * a.S * KC] = h;
       h = fmaf(e[i], h, add[i]);
     }
   }
 }
 
-// B_t and C_t as fp32 rows of 2 SP, zeros behind S.
+// B_t and C_t as fp32 rows of 2 SP, then A log2 e as [SP][C]; zeros behind S.
 template <class T>
-__global__ __launch_bounds__(kScanThreads) void prepare_kernel(const T* __restrict__ Bt, const T* __restrict__ Ct,
-                                                               float* __restrict__ bc, long long rows, int S, int SP) {
-  const long long i = (long long)blockIdx.x * kScanThreads + threadIdx.x;
-  if (i >= rows * 2 * SP) return;
-  const long long row = i / (2 * SP);
-  const int j = (int)(i - row * 2 * SP), s = j < SP ? j : j - SP;
-  bc[i] = s < S ? widen((j < SP ? Bt : Ct)[row * S + s]) : 0.f;
+__global__ __launch_bounds__(kScanThreads) void prepare_kernel(ScanArgs a, ScanSpace ws, int SP) {
+  const long long i = (long long)blockIdx.x * kScanThreads + threadIdx.x, n = (long long)a.B * a.N * 2 * SP;
+  if (i < n) {
+    const long long row = i / (2 * SP);
+    const int j = (int)(i - row * 2 * SP), s = j < SP ? j : j - SP;
+    ws.bc[i] = s < a.S ? load1<T>(j < SP ? a.Bt : a.Ct, row * a.S + s) : 0.f;
+  } else if (i < n + (long long)SP * a.C) {
+    const int j = (int)(i - n), s = j / a.C, c = j - s * a.C;
+    ws.A2[j] = s < a.S ? a.A[(long long)c * a.S + s] * kLog2e : 0.f;
+  }
 }
 
 // One token: thread of V neighbouring channels of one component, the states
@@ -234,6 +280,7 @@ ScanChunks forward_chunks(int64_t B, int64_t N, int K, int64_t C) {
 ScanSpace forward_space(void* base, const ScanChunks& ch, int64_t B, int64_t N, int K, int64_t C, int S) {
   ScanSpace w;
   w.place(base, &w.bc, (size_t)B * N * 2 * scan_padded(S));
+  w.place(base, &w.A2, (size_t)scan_padded(S) * C);
   if (ch.chunks > 1) {
     w.place(base, &w.hs, (size_t)B * ch.chunks * S * K * C);
     w.place(base, &w.ds, (size_t)B * ch.chunks * C);
@@ -275,11 +322,11 @@ template <class T>
 hipError_t scan_forward(const ScanArgs& a, hipStream_t s) {
   const ScanChunks ch = forward_chunks(a.B, a.N, a.K, a.C);
   const ScanSpace w = forward_space(a.ws, ch, a.B, a.N, a.K, a.C, a.S);
-  hipError_t e = launch_scan_prepare(a, w.bc, s);
+  hipError_t e = launch_scan_prepare(a, w, s);
   if (e != hipSuccess) return e;
   if (ch.chunks > 1) {
     if ((e = run_scan_components<T, true>(a, ch, w, s)) != hipSuccess) return e;
-    if ((e = launch_scan_carry(a, ch, a.state_in, w.hs, w.ds, false, s)) != hipSuccess) return e;
+    if ((e = launch_scan_carry(a, ch, w, a.state_in, false, s)) != hipSuccess) return e;
   }
   return run_scan_components<T, false>(a, ch, w, s);
 }
@@ -295,32 +342,23 @@ hipError_t scan_step(const ScanArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_scan_prepare(const ScanArgs& a, float* bc, hipStream_t s) {
+hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, hipStream_t s) {
   const int SP = scan_padded(a.S);
-  const long long rows = (long long)a.B * a.N, blocks = (rows * 2 * SP + kScanThreads - 1) / kScanThreads;
+  const long long n = (long long)a.B * a.N * 2 * SP + (long long)SP * a.C;
+  const long long blocks = (n + kScanThreads - 1) / kScanThreads;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
   if (a.type == SEQ_BF16)
-    hipLaunchKernelGGL(prepare_kernel<bf16>, dim3((unsigned)blocks), dim3(kScanThreads), 0, s,
-                       static_cast<const bf16*>(a.Bt), static_cast<const bf16*>(a.Ct), bc, rows, a.S, SP);
+    hipLaunchKernelGGL(prepare_kernel<bf16>, dim3((unsigned)blocks), dim3(kScanThreads), 0, s, a, w, SP);
   else
-    hipLaunchKernelGGL(prepare_kernel<float>, dim3((unsigned)blocks), dim3(kScanThreads), 0, s,
-                       static_cast<const float*>(a.Bt), static_cast<const float*>(a.Ct), bc, rows, a.S, SP);
+    hipLaunchKernelGGL(prepare_kernel<float>, dim3((unsigned)blocks), dim3(kScanThreads), 0, s, a, w, SP);
   return hipGetLastError();
 }
 
-hipError_t launch_scan_local(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, hipStream_t s) {
-  return a.type == SEQ_BF16 ? run_scan_components<bf16, true>(a, ch, w, s)
-                            : run_scan_components<float, true>(a, ch, w, s);
-}
-
-hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const float* first, float* hs, const float* ds,
-                             bool reverse, hipStream_t s) {
+hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, const float* first, bool reverse,
+                             hipStream_t s) {
   const long long n = (long long)a.S * a.K * a.C;
-  const dim3 grid((unsigned)((n + kScanThreads - 1) / kScanThreads), a.B);
-  if (reverse)
-    hipLaunchKernelGGL(carry_kernel<true>, grid, dim3(kScanThreads), 0, s, a, ch, first, hs, ds);
-  else
-    hipLaunchKernelGGL(carry_kernel<false>, grid, dim3(kScanThreads), 0, s, a, ch, first, hs, ds);
+  hipLaunchKernelGGL(carry_kernel, dim3((unsigned)((n + 63) / 64), reverse ? 2 : 1, a.B), dim3(64 * kCarrySlices), 0, s,
+                     a, ch, w, first);
   return hipGetLastError();
 }
 

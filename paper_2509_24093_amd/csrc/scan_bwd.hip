@@ -9,13 +9,15 @@
 //
 // The states are formed again rather than kept (S times the input) or run
 // backwards (a division by decays that may vanish): chunks of kChunk tokens from
-// their start states (the forward's passes 1 and 2), inside a chunk the states
-// before every kSub tokens in LDS, the kSub states of a piece in registers.
-// Like the states, r enters a chunk from a pass over the chunks in reverse.  gB
-// and gC add over the lanes: the 2 SP values of a token are halved from step to
-// step, each lane keeping the half of its bit, so 64 lanes x 32 values take 31
-// exchanges instead of 192; waves add through LDS, column blocks in a last
-// kernel.  No atomics: every sum has a fixed order.
+// their start states, inside a chunk the states before every kSub tokens in LDS,
+// the kSub states of a piece in registers.  What the chunks add to the states
+// behind them and to r before them comes from one pass over the tokens: with the
+// running product P_t of the decays, sum_t P_t C_t gy_t is the chunk's own r, so
+// both take one exponential per state.  gB and gC add over the lanes: the SP
+// values of a token are halved from step to step, each lane keeping the half of
+// its bit, so 16 values take 15 exchanges and 2 more instead of 96; waves add
+// through LDS, column blocks in a last kernel.  No atomics: every sum has a fixed
+// order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -42,43 +44,84 @@ struct BwdShape {
 int bwd_chunk(int S) { return scan_padded(S) == 32 ? BwdShape<32>::kChunk : BwdShape<16>::kChunk; }
 int bwd_threads(int S) { return scan_padded(S) == 32 ? BwdShape<32>::kThreads : BwdShape<16>::kThreads; }
 
-// Pass over the chunks behind the first: the gradient that a chunk's own
-// outputs send to the state before it, and its sum of delta.
+// The states that a chunk ends with from zero, the gradient that its own outputs
+// send to the state before it, and its sum of delta.
 template <class T, int SP>
-__global__ __launch_bounds__(256) void reverse_kernel(ScanBwdArgs g, ScanChunks sh, ScanSpace ws, int colblocks) {
+__global__ __launch_bounds__(BwdShape<SP>::kThreads) void ends_kernel(ScanBwdArgs g, ScanChunks sh, ScanSpace ws,
+                                                                      int colblocks) {
   const ScanArgs& a = g.a;
-  const int ch = blockIdx.x / colblocks + 1, b = blockIdx.y;
+  const int ch = blockIdx.x / colblocks, b = blockIdx.y;
   const int KC = a.K * a.C;
-  const int id = (blockIdx.x - (ch - 1) * colblocks) * blockDim.x + threadIdx.x;
+  const int id = (blockIdx.x - ch * colblocks) * blockDim.x + threadIdx.x;
   const bool here = id < KC;
   const int j = here ? id : 0, c = j % a.C;
   const int len = scan_length(a.lengths, b, a.N);
   const int t0 = ch * sh.chunk, t2 = min(min(a.N, t0 + sh.chunk), len);
-  float A2[SP], r[SP];
-#pragma unroll
-  for (int s = 0; s < SP; ++s) {
-    A2[s] = s < a.S ? a.A[(long long)c * a.S + s] * kLog2e : 0.f;
-    r[s] = 0.f;
-  }
-  const float bias = a.bias ? a.bias[c] : 0.f;
   const long long row0 = (long long)b * a.N;
+  const T* xp = static_cast<const T*>(a.x) + row0 * KC + j;
   const T* gyp = static_cast<const T*>(g.gy) + row0 * KC + j;
   const T* dp = static_cast<const T*>(a.delta) + row0 * a.C + c;
   const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
-  float total = 0.f;
-#pragma unroll 2
-  for (int t = t2 - 1; t >= t0; --t) {
-    const float d = softplus(widen(dp[(long long)t * a.C]) + bias), gy = widen(gyp[(long long)t * KC]);
-    total += d;
-    const ConstFloats p = bc + (long long)t * 2 * SP + SP;
+  constexpr int kAhead = 4;
+  float dn[kAhead], xn[kAhead], gn[kAhead];
+  auto fetch = [&](int tb) {
 #pragma unroll
-    for (int s = 0; s < SP; ++s) r[s] = exp2_fast(d * A2[s]) * fmaf(p[s], gy, r[s]);
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = min(tb + u, t2 - 1);
+      dn[u] = widen(dp[(long long)t * a.C]);
+      xn[u] = widen(xp[(long long)t * KC]);
+      gn[u] = widen(gyp[(long long)t * KC]);
+    }
+  };
+  TokenRow<SP> p;
+  if (t0 < t2) {
+    fetch(t0);
+    p.load(bc + (long long)t0 * 2 * SP);
+  }
+  float A2[SP], h[SP], r[SP], P[SP];
+#pragma unroll
+  for (int s = 0; s < SP; ++s) {
+    A2[s] = ws.A2[s * a.C + c];
+    h[s] = r[s] = 0.f;
+    P[s] = 1.f;
+  }
+  const float bias = a.bias ? a.bias[c] : 0.f;
+  float total = 0.f;
+  for (int tb = t0; tb < t2; tb += kAhead) {
+    float dc[kAhead], xc[kAhead], gc[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      dc[u] = dn[u];
+      xc[u] = xn[u];
+      gc[u] = gn[u];
+    }
+    if (tb + kAhead < t2) fetch(tb + kAhead);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = tb + u;
+      if (t >= t2) break;
+      TokenRow<SP> next;
+      next.load(bc + (long long)min(t + 1, t2 - 1) * 2 * SP);
+      const float d = softplus(dc[u] + bias), dx = d * xc[u];
+      total += d;
+#pragma unroll
+      for (int s = 0; s < SP; ++s) {
+        const float e = exp2_fast(d * A2[s]);
+        h[s] = fmaf(e, h[s], p.v[s] * dx);
+        P[s] *= e;
+        r[s] = fmaf(P[s], p.v[SP + s] * gc[u], r[s]);
+      }
+      p = next;
+    }
   }
   if (!here) return;
-  float* out = ws.rs + ((long long)b * sh.chunks + ch) * a.S * KC + j;
+  const long long at = ((long long)b * sh.chunks + ch) * a.S * KC + j;
 #pragma unroll
   for (int s = 0; s < SP; ++s)
-    if (s < a.S) out[(long long)s * KC] = r[s];
+    if (s < a.S) {
+      ws.hs[at + (long long)s * KC] = h[s];
+      ws.rs[at + (long long)s * KC] = r[s];
+    }
   if (j < a.C) ws.ds[((long long)b * sh.chunks + ch) * a.C + c] = total;
 }
 
@@ -132,10 +175,11 @@ __device__ __forceinline__ float wave_scatter_sum(float (&v)[N], int lane) {
 template <int N>
 __device__ __forceinline__ int scatter_index(int lane) { return lane / (64 / N); }
 
-// Block (chunk, column block) of a batch element; thread = column k C + c.
-template <class T, int SP>
-__global__ __launch_bounds__(BwdShape<SP>::kThreads) void scan_bwd_kernel(ScanBwdArgs g, ScanChunks sh, ScanSpace ws,
-                                                                          int colblocks) {
+// Block (chunk, column block) of a batch element; thread = column k C + c.  ONE:
+// K = 1, delta's gradient is finished here.
+template <class T, int SP, bool ONE>
+__global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(ScanBwdArgs g, ScanChunks sh,
+                                                                             ScanSpace ws, int colblocks) {
   constexpr int kSub = BwdShape<SP>::kSub, kThreads = BwdShape<SP>::kThreads;
   constexpr int kPieces = BwdShape<SP>::kChunk / kSub, kWaves = kThreads / 64;
   __shared__ float starts[kPieces - 1][SP][kThreads];
@@ -143,9 +187,9 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads) void scan_bwd_kernel(ScanBw
   const ScanArgs& a = g.a;
   const int ch = blockIdx.x / colblocks, cb = blockIdx.x - ch * colblocks, b = blockIdx.y;
   const int KC = a.K * a.C, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int id = cb * kThreads + tid;
+  const int id = cb * blockDim.x + tid;
   const bool here = id < KC;
-  const int j = here ? id : 0, c = j % a.C;
+  const int j = here ? id : 0, c = ONE ? j : j % a.C;
   const int len = scan_length(a.lengths, b, a.N);
   const int t0 = ch * sh.chunk, t1 = min(a.N, t0 + sh.chunk), t2 = min(t1, len);
   const long long row0 = (long long)b * a.N;
@@ -153,72 +197,95 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads) void scan_bwd_kernel(ScanBw
   const T* gyp = static_cast<const T*>(g.gy) + row0 * KC + j;
   const T* dp = static_cast<const T*>(a.delta) + row0 * a.C + c;
   T* gxp = static_cast<T*>(g.gx) + row0 * KC + j;
-  float* gdp = ws.gd + row0 * KC + j;
+  T* gdp = static_cast<T*>(g.gdelta) + row0 * KC + j;  // ONE
+  float* gdk = ws.gd + row0 * KC + j;                  // else
   const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
   const long long at = ((long long)b * sh.chunks + ch) * a.S * KC + j;
-  float A2[SP], h[SP], r[SP], gA[SP];
+  const bool carried = here && sh.chunks > 1;
+  float A2[SP], r[SP], gA[SP];
+  const float bias = a.bias ? a.bias[c] : 0.f, D = a.D ? a.D[c] : 0.f;
+  float gD = 0.f, gbias = 0.f;
+  const int last = t2 > t0 ? (t2 - t0 - 1) / kSub : -1;  // the last piece
+#pragma unroll
+  for (int s = 0; s < SP; ++s) A2[s] = ws.A2[s * a.C + c];
+  auto start = [&](float (&h)[SP]) {
+#pragma unroll
+    for (int s = 0; s < SP; ++s) h[s] = carried && s < a.S ? ws.hs[at + (long long)s * KC] : 0.f;
+  };
+  {  // the states before every piece but the first
+    float h[SP];
+    start(h);
+#pragma unroll 1
+    for (int piece = 0; piece < last; ++piece) {
+      const int ts = t0 + piece * kSub;
+      float d[kSub], x[kSub];
+#pragma unroll
+      for (int i = 0; i < kSub; ++i) {
+        d[i] = widen(dp[(long long)(ts + i) * a.C]);
+        x[i] = here ? widen(xp[(long long)(ts + i) * KC]) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kSub; ++i) {
+        const float di = softplus(d[i] + bias), dx = di * x[i];
+        const ConstFloats p = bc + (long long)(ts + i) * 2 * SP;
+#pragma unroll
+        for (int s = 0; s < SP; ++s) h[s] = fmaf(exp2_fast(di * A2[s]), h[s], p[s] * dx);
+      }
+#pragma unroll
+      for (int s = 0; s < SP; ++s) starts[piece][s][tid] = h[s];
+    }
+  }
 #pragma unroll
   for (int s = 0; s < SP; ++s) {
-    const bool there = s < a.S && here;
-    A2[s] = s < a.S ? a.A[(long long)c * a.S + s] * kLog2e : 0.f;
-    h[s] = there && sh.chunks > 1 ? ws.hs[at + (long long)s * KC] : 0.f;
-    r[s] = there && sh.chunks > 1 ? ws.rs[at + (long long)s * KC] : 0.f;
+    r[s] = carried && s < a.S ? ws.rs[at + (long long)s * KC] : 0.f;
     gA[s] = 0.f;
   }
-  const float bias = a.bias ? a.bias[c] : 0.f, D = a.D ? a.D[c] : 0.f;
-  float gD = 0.f;
-  // the states before every piece but the first
 #pragma unroll 1
-  for (int t = t0; t < t2; ++t) {
-    const int n = t - t0;
-    if (n > 0 && n % kSub == 0) {
-#pragma unroll
-      for (int s = 0; s < SP; ++s) starts[n / kSub - 1][s][tid] = h[s];
-    }
-    if (t - t0 >= (t2 - t0 - 1) / kSub * kSub) break;  // the last piece forms its own
-    const float d = softplus(widen(dp[(long long)t * a.C]) + bias);
-    const float dx = d * widen(xp[(long long)t * KC]);
-    const ConstFloats p = bc + (long long)t * 2 * SP;
-#pragma unroll
-    for (int s = 0; s < SP; ++s) h[s] = fmaf(exp2_fast(d * A2[s]), h[s], p[s] * dx);
-  }
-  for (int piece = t2 > t0 ? (t2 - t0 - 1) / kSub : -1; piece >= 0; --piece) {
+  for (int piece = last; piece >= 0; --piece) {
     const int ts = t0 + piece * kSub, n = min(kSub, t2 - ts);
-    float hist[kSub + 1][SP], d[kSub], x[kSub], gy[kSub];
+    float hist[kSub][SP], d[kSub], x[kSub], gy[kSub];  // hist[i]: before token i
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
       const int t = ts + min(i, n - 1);
       const bool on = here && i < n;
-      d[i] = widen(dp[(long long)t * a.C]);
+      d[i] = widen(dp[(long long)t * a.C]) + bias;
       x[i] = on ? widen(xp[(long long)t * KC]) : 0.f;
       gy[i] = on ? widen(gyp[(long long)t * KC]) : 0.f;
     }
+    if (piece) {
 #pragma unroll
-    for (int s = 0; s < SP; ++s)
-      hist[0][s] = piece ? starts[piece - 1][s][tid]
-                         : (s < a.S && here && sh.chunks > 1 ? ws.hs[at + (long long)s * KC] : 0.f);
+      for (int s = 0; s < SP; ++s) hist[0][s] = starts[piece - 1][s][tid];
+    } else {
+      start(hist[0]);
+    }
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
       if (i < n) {  // uniform
-        d[i] = softplus(d[i] + bias);
+        d[i] = softplus(d[i]);
         const float dx = d[i] * x[i];
         const ConstFloats p = bc + (long long)(ts + i) * 2 * SP;
+        float v[SP];
 #pragma unroll
-        for (int s = 0; s < SP; ++s) hist[i + 1][s] = fmaf(exp2_fast(d[i] * A2[s]), hist[i][s], p[s] * dx);
+        for (int s = 0; s < SP; ++s) {
+          const float h = fmaf(exp2_fast(d[i] * A2[s]), hist[i][s], p[s] * dx);
+          v[s] = h * gy[i];
+          if (i + 1 < kSub) hist[i + 1][s] = h;
+        }
+        red[wave][i][SP + scatter_index<SP>(lane)] = wave_scatter_sum(v, lane);
       }
     }
 #pragma unroll
     for (int i = kSub - 1; i >= 0; --i) {
       if (i < n) {
-        const int t = ts + i;
-        const ConstFloats p = bc + (long long)t * 2 * SP;
+        const long long t = ts + i;
+        const ConstFloats p = bc + t * 2 * SP;
         const float dx = d[i] * x[i];
-        float v[2 * SP], into = 0.f, gd = 0.f;
+        const float raw = ONE ? widen(dp[t * a.C]) + bias : 0.f;  // read again: fewer registers
+        float v[SP], into = 0.f, gd = 0.f;
 #pragma unroll
         for (int s = 0; s < SP; ++s) {
           const float gs = fmaf(p[SP + s], gy[i], r[s]);
           v[s] = gs * dx;
-          v[SP + s] = hist[i + 1][s] * gy[i];
           into = fmaf(p[s], gs, into);
           r[s] = exp2_fast(d[i] * A2[s]) * gs;
           const float q = r[s] * hist[i][s];
@@ -226,33 +293,43 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads) void scan_bwd_kernel(ScanBw
           gd = fmaf(A2[s], q, gd);
         }
         gD = fmaf(gy[i], x[i], gD);
-        if (here) {
-          if (g.gx) gxp[(long long)t * KC] = (T)fmaf(d[i], into, D * gy[i]);
-          gdp[(long long)t * KC] = fmaf(gd, kLn2, into * x[i]);
+        gd = fmaf(gd, kLn2, into * x[i]);
+        if (ONE) {
+          gd /= 1.f + exp2_fast(-kLog2e * raw);  // the derivative of softplus
+          gbias += gd;
         }
-        const float sum = wave_scatter_sum(v, lane);
-        const int o = scatter_index<2 * SP>(lane);
-        red[wave][i][o] = sum;
+        if (here) {
+          if (g.gx) gxp[t * KC] = (T)fmaf(d[i], into, D * gy[i]);
+          if (ONE) {
+            if (g.gdelta) gdp[t * KC] = (T)gd;
+          } else {
+            gdk[t * KC] = gd;
+          }
+        }
+        red[wave][i][scatter_index<SP>(lane)] = wave_scatter_sum(v, lane);
       }
     }
     __syncthreads();
+    const int waves = blockDim.x >> 6;
     float* out = ws.gbc + (((long long)cb * a.B + b) * a.N + ts) * 2 * SP;
-    for (int o = tid; o < n * 2 * SP; o += kThreads) {
+    for (int o = tid; o < n * 2 * SP; o += blockDim.x) {
       float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) s += (&red[w][0][0])[o];
+      for (int w = 0; w < waves; ++w) s += (&red[w][0][0])[o];
       out[o] = s;
     }
     __syncthreads();
   }
   if (!here) return;
-  if (g.gx)
-    for (int t = max(t0, t2); t < t1; ++t) gxp[(long long)t * KC] = (T)0.f;
-  float* ga = ws.ga + ((long long)b * sh.chunks + ch) * (a.S + 1) * KC + j;
+  for (int t = max(t0, t2); t < t1; ++t) {
+    if (g.gx) gxp[(long long)t * KC] = (T)0.f;
+    if (ONE && g.gdelta) gdp[(long long)t * KC] = (T)0.f;
+  }
+  float* ga = ws.ga + ((long long)b * sh.chunks + ch) * (a.S + 2) * KC + j;
 #pragma unroll
   for (int s = 0; s < SP; ++s)
     if (s < a.S) ga[(long long)s * KC] = gA[s];
   ga[(long long)a.S * KC] = gD;
+  if (ONE) ga[(long long)(a.S + 1) * KC] = gbias;
 }
 
 // gB_t, gC_t from the column blocks' sums.
@@ -275,66 +352,77 @@ __global__ __launch_bounds__(256) void sum_bc_kernel(ScanBwdArgs g, const float*
   out[row * a.S + s] = (T)v;
 }
 
-// graw from the components' parts of gdelta, and its sums over kBiasTokens
-// tokens: block of 64 channels x 4 token slots.
-constexpr int kBiasTokens = 64;
+// K > 1: graw from the components' parts of gdelta, and its sums over a block's
+// tokens.  A block takes `width` channels (a power of two) x 256 / width token
+// slots, kBiasRows tokens a slot.
+constexpr int kBiasRows = 4;
 template <class T>
-__global__ __launch_bounds__(256) void delta_kernel(ScanBwdArgs g, ScanSpace ws, int colblocks) {
-  __shared__ float lds[4][64];
+__global__ __launch_bounds__(256) void delta_kernel(ScanBwdArgs g, ScanSpace ws, int width, int colblocks) {
+  __shared__ float lds[256];
   const ScanArgs& a = g.a;
-  const int tb = blockIdx.x / colblocks, c = (blockIdx.x - tb * colblocks) * 64 + (threadIdx.x & 63);
-  const int slot = threadIdx.x >> 6;
-  const long long rows = (long long)a.B * a.N, r0 = (long long)tb * kBiasTokens;
-  const long long r1 = min(rows, r0 + kBiasTokens);
+  const int tb = blockIdx.x / colblocks, lane = threadIdx.x & (width - 1), slot = threadIdx.x / width;
+  const int slots = 256 / width, c = (blockIdx.x - tb * colblocks) * width + lane;
+  const long long rows = (long long)a.B * a.N, r0 = (long long)tb * slots * kBiasRows;
   float sum = 0.f;
   if (c < a.C) {
     const float bias = a.bias ? a.bias[c] : 0.f;
-    for (long long row = r0 + slot; row < r1; row += 4) {
+    for (int i = 0; i < kBiasRows; ++i) {
+      const long long row = r0 + i * slots + slot;
+      if (row >= rows) break;
       const int b = (int)(row / a.N), t = (int)(row - (long long)b * a.N);
       float v = 0.f;
       if (t < scan_length(a.lengths, b, a.N)) {
         const float* p = ws.gd + row * a.K * a.C + c;
+        const float raw = load1<T>(a.delta, row * a.C + c) + bias;
+#pragma unroll 9
         for (int k = 0; k < a.K; ++k) v += p[(long long)k * a.C];
-        v /= 1.f + exp2_fast(-kLog2e * (load1<T>(a.delta, row * a.C + c) + bias));
+        v /= 1.f + exp2_fast(-kLog2e * raw);
       }
       if (g.gdelta) static_cast<T*>(g.gdelta)[row * a.C + c] = (T)v;
       sum += v;
     }
   }
-  lds[slot][threadIdx.x & 63] = sum;
+  lds[threadIdx.x] = sum;
   __syncthreads();
-  if (slot == 0 && c < a.C)
-    ws.gbp[(long long)tb * a.C + c] = lds[0][threadIdx.x] + lds[1][threadIdx.x] + lds[2][threadIdx.x] + lds[3][threadIdx.x];
+  if (slot == 0 && c < a.C) {
+    for (int i = 1; i < slots; ++i) sum += lds[i * width + lane];
+    ws.gbp[(long long)tb * a.C + c] = sum;
+  }
 }
 
-// out[row, c] = sum over units and components of part[unit][row][k C + c]:
-// 16 slices x 64 outputs per block.  The first `rowsA` rows go to outA[c rowsA +
-// row], one behind them to outD[c].
-constexpr int kSumSlices = 16;
-__global__ __launch_bounds__(64 * kSumSlices) void sum_units_kernel(const float* __restrict__ part, long long units,
-                                                                    int rows, int rowsA, int K, int C, float* outA,
-                                                                    float* outD) {
-  __shared__ float lds[kSumSlices][64];
-  const int o = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
-  const int row = o / C, c = o - row * C;
+// Sums over units and components of part[unit][row][k C + c], rows: 64 slices x
+// 16 outputs per block.  Output row < rowsA: outA[c rowsA + row]; the two behind
+// them: out1[c], out2[c].
+constexpr int kSumSlices = 64, kSumLanes = 16;
+__global__ __launch_bounds__(kSumSlices * kSumLanes) void sum_units_kernel(const float* __restrict__ part,
+                                                                           long long units, int rows, int rowsA, int K,
+                                                                           int C, float* outA, float* out1,
+                                                                           float* out2) {
+  __shared__ float lds[kSumSlices][kSumLanes];
+  const int lane = threadIdx.x & (kSumLanes - 1), slice = threadIdx.x / kSumLanes;
+  const int o = blockIdx.x * kSumLanes + lane, row = o / C, c = o - row * C;
   float s = 0.f;
   if (row < rows) {
     for (int k = 0; k < K; ++k) {
       const float* p = part + ((long long)row * K + k) * C + c;
       const long long stride = (long long)rows * K * C;
-#pragma unroll 8
+#pragma unroll 4
       for (long long u = slice; u < units; u += kSumSlices) s += p[u * stride];
     }
   }
-  lds[slice][threadIdx.x & 63] = s;
+  lds[slice][lane] = s;
   __syncthreads();
+  for (int n = kSumSlices / 2; n > 0; n /= 2) {
+    if (slice < n) lds[slice][lane] += lds[slice + n][lane];
+    __syncthreads();
+  }
   if (slice == 0 && row < rows) {
-    float v = 0.f;
-    for (int i = 0; i < kSumSlices; ++i) v += lds[i][threadIdx.x];
+    const float v = lds[0][lane];
     if (row < rowsA) {
       if (outA) outA[(long long)c * rowsA + row] = v;
-    } else if (outD) {
-      outD[c] = v;
+    } else {
+      float* out = row == rowsA ? out1 : out2;
+      if (out) out[c] = v;
     }
   }
 }
@@ -346,44 +434,66 @@ ScanChunks backward_chunks(int64_t N, int S) {
   return s;
 }
 
-long long bias_blocks(int64_t B, int64_t N) { return (B * N + kBiasTokens - 1) / kBiasTokens; }
+// Lanes over the channels in delta_kernel, and its blocks over the tokens.
+int bias_width(int64_t C) {
+  int w = 16;
+  while (w < 64 && w < C) w *= 2;
+  return w;
+}
+long long bias_blocks(int64_t B, int64_t N, int64_t C) {
+  const int rows = 256 / bias_width(C) * kBiasRows;
+  return (B * N + rows - 1) / rows;
+}
+
+// Column blocks of the main kernel, of equal numbers of waves.
+int bwd_colblocks(int64_t KC, int S) { return (int)((KC + bwd_threads(S) - 1) / bwd_threads(S)); }
 
 ScanSpace backward_space(void* base, int64_t B, int64_t N, int K, int64_t C, int S) {
   ScanSpace w;
   const ScanChunks ch = backward_chunks(N, S);
   const size_t KC = (size_t)K * C, units = (size_t)B * ch.chunks;
-  const size_t colblocks = (KC + bwd_threads(S) - 1) / bwd_threads(S);
   w.place(base, &w.bc, (size_t)B * N * 2 * scan_padded(S));
+  w.place(base, &w.A2, (size_t)scan_padded(S) * C);
   if (ch.chunks > 1) {
     w.place(base, &w.hs, units * S * KC);
     w.place(base, &w.rs, units * S * KC);
     w.place(base, &w.ds, units * C);
   }
-  w.place(base, &w.gbc, colblocks * B * N * 2 * scan_padded(S));
-  w.place(base, &w.gd, (size_t)B * N * KC);
-  w.place(base, &w.ga, units * (S + 1) * KC);
-  w.place(base, &w.gbp, (size_t)bias_blocks(B, N) * C);
+  w.place(base, &w.gbc, (size_t)bwd_colblocks(KC, S) * B * N * 2 * scan_padded(S));
+  w.place(base, &w.ga, units * (S + 2) * KC);
+  if (K > 1) {
+    w.place(base, &w.gd, (size_t)B * N * KC);
+    w.place(base, &w.gbp, (size_t)bias_blocks(B, N, C) * C);
+  }
   return w;
+}
+
+hipError_t sum_units(const float* part, long long units, int rows, int rowsA, int K, int C, float* outA, float* out1,
+                     float* out2, hipStream_t s) {
+  hipLaunchKernelGGL(sum_units_kernel, dim3((rows * C + kSumLanes - 1) / kSumLanes), dim3(kSumSlices * kSumLanes), 0, s,
+                     part, units, rows, rowsA, K, C, outA, out1, out2);
+  return hipGetLastError();
 }
 
 template <class T, int SP>
 hipError_t run_backward(const ScanBwdArgs& g, const ScanChunks& ch, const ScanSpace& w, hipStream_t s) {
   const ScanArgs& a = g.a;
   const int KC = a.K * a.C;
-  constexpr int kThreads = BwdShape<SP>::kThreads;
-  const int colblocks = (KC + kThreads - 1) / kThreads;
+  const int colblocks = bwd_colblocks(KC, a.S);
+  const int threads = ((KC + colblocks - 1) / colblocks + 63) / 64 * 64;
   const long long blocks = (long long)colblocks * ch.chunks;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks, a.B);
   hipError_t e;
   if (ch.chunks > 1) {
-    if ((e = launch_scan_local(a, ch, w, s)) != hipSuccess) return e;
-    if ((e = launch_scan_carry(a, ch, nullptr, w.hs, w.ds, false, s)) != hipSuccess) return e;
-    hipLaunchKernelGGL((reverse_kernel<T, SP>), dim3((unsigned)(blocks - colblocks), a.B), dim3(kThreads), 0, s, g, ch,
-                       w, colblocks);
+    hipLaunchKernelGGL((ends_kernel<T, SP>), grid, dim3(threads), 0, s, g, ch, w, colblocks);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if ((e = launch_scan_carry(a, ch, nullptr, w.rs, w.ds, true, s)) != hipSuccess) return e;
+    if ((e = launch_scan_carry(a, ch, w, nullptr, true, s)) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((scan_bwd_kernel<T, SP>), dim3((unsigned)blocks, a.B), dim3(kThreads), 0, s, g, ch, w, colblocks);
+  if (a.K == 1)
+    hipLaunchKernelGGL((scan_bwd_kernel<T, SP, true>), grid, dim3(threads), 0, s, g, ch, w, colblocks);
+  else
+    hipLaunchKernelGGL((scan_bwd_kernel<T, SP, false>), grid, dim3(threads), 0, s, g, ch, w, colblocks);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (g.gB || g.gC) {
     const long long n = ((long long)a.B * a.N * 2 * SP + 255) / 256;
@@ -391,24 +501,17 @@ hipError_t run_backward(const ScanBwdArgs& g, const ScanChunks& ch, const ScanSp
     hipLaunchKernelGGL(sum_bc_kernel<T>, dim3((unsigned)n), dim3(256), 0, s, g, w.gbc, colblocks, SP);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (g.gdelta || g.gbias) {
-    const int cbs = (a.C + 63) / 64;
-    const long long tbs = bias_blocks(a.B, a.N);
+  if (a.K > 1 && (g.gdelta || g.gbias)) {
+    const int width = bias_width(a.C), cbs = (a.C + width - 1) / width;
+    const long long tbs = bias_blocks(a.B, a.N, a.C);
     if (tbs * cbs > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(delta_kernel<T>, dim3((unsigned)(tbs * cbs)), dim3(256), 0, s, g, w, cbs);
+    hipLaunchKernelGGL(delta_kernel<T>, dim3((unsigned)(tbs * cbs)), dim3(256), 0, s, g, w, width, cbs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (g.gbias) {
-      hipLaunchKernelGGL(sum_units_kernel, dim3(cbs), dim3(64 * kSumSlices), 0, s, w.gbp, tbs, 1, 0, 1, a.C, nullptr,
-                         g.gbias);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    if (g.gbias && (e = sum_units(w.gbp, tbs, 1, 0, 1, a.C, nullptr, g.gbias, nullptr, s)) != hipSuccess) return e;
   }
-  if (g.gA || g.gD) {
-    const int outputs = (a.S + 1) * a.C;
-    hipLaunchKernelGGL(sum_units_kernel, dim3((outputs + 63) / 64), dim3(64 * kSumSlices), 0, s, w.ga,
-                       (long long)a.B * ch.chunks, a.S + 1, a.S, a.K, a.C, g.gA, g.gD);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
+  if (g.gA || g.gD || (a.K == 1 && g.gbias))
+    return sum_units(w.ga, (long long)a.B * ch.chunks, a.S + 2, a.S, a.K, a.C, g.gA, g.gD,
+                     a.K == 1 ? g.gbias : nullptr, s);
   return hipSuccess;
 }
 
@@ -417,7 +520,7 @@ hipError_t by_states(const ScanBwdArgs& g, hipStream_t s) {
   const ScanArgs& a = g.a;
   const ScanChunks ch = backward_chunks(a.N, a.S);
   const ScanSpace w = backward_space(a.ws, a.B, a.N, a.K, a.C, a.S);
-  const hipError_t e = launch_scan_prepare(a, w.bc, s);
+  const hipError_t e = launch_scan_prepare(a, w, s);
   if (e != hipSuccess) return e;
   switch (scan_padded(a.S)) {
     case 8: return run_backward<T, 8>(g, ch, w, s);

@@ -8,7 +8,8 @@
 // Lanes are channels (of one or several components), so B_t and C_t are the
 // same for a whole wave: a preparing kernel writes them as fp32 rows of SP
 // states each (SP = S rounded up, zeros behind S), and the scans read them
-// through the scalar cache as scalar operands.  The states stay in registers.
+// through the scalar cache as scalar operands, a token ahead of their use.  The
+// states stay in registers.
 #pragma once
 
 #include "seq_common.h"
@@ -44,6 +45,16 @@ __device__ __forceinline__ int scan_length(const int* lengths, int b, int N) {
   return lengths ? min(max(lengths[b], 0), N) : N;
 }
 
+// B_t (v[0..SP)) and C_t (v[SP..2SP)) of one token, in scalar registers.
+template <int SP>
+struct TokenRow {
+  float v[2 * SP];
+  __device__ __forceinline__ void load(ConstFloats p) {
+#pragma unroll
+    for (int s = 0; s < 2 * SP; ++s) v[s] = p[s];
+  }
+};
+
 template <class T>
 __device__ __forceinline__ float load1(const void* p, long long i) {
   return widen(static_cast<const T*>(p)[i]);
@@ -62,14 +73,15 @@ inline int scan_padded(int S) { return S <= 8 ? 8 : S <= 16 ? 16 : 32; }
 // Workspace: parts of one allocation, 256-byte aligned.
 struct ScanSpace {
   float* bc = nullptr;   // [B][N][2 SP]: B_t, C_t
+  float* A2 = nullptr;   // [SP][C]: A log2 e
   float* hs = nullptr;   // [B][chunks][S][K C]: states at the chunks' ends, then starts
   float* ds = nullptr;   // [B][chunks][C]: sum of delta over a chunk
   // backward
   float* rs = nullptr;   // [B][chunks][S][K C]: gradients of the states behind a chunk
   float* gbc = nullptr;  // [column blocks][B][N][2 SP]: of B_t, C_t
-  float* gd = nullptr;   // [B][N][K][C]: the components' parts of delta's
-  float* ga = nullptr;   // [B][chunks][S + 1][K C]: of A and (last) D over a chunk
-  float* gbp = nullptr;  // [token blocks][C]: of the bias
+  float* gd = nullptr;   // [B][N][K][C]: the components' parts of delta's (K > 1)
+  float* ga = nullptr;   // [B][chunks][S + 2][K C]: of A, D and (K = 1) the bias over a chunk
+  float* gbp = nullptr;  // [token blocks][C]: of the bias (K > 1)
   size_t bytes = 0;
   void place(void* base, float** p, size_t floats) {
     *p = reinterpret_cast<float*>(static_cast<char*>(base) + bytes);
@@ -80,9 +92,9 @@ struct ScanSpace {
 size_t scan_forward_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
 size_t scan_backward_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
 
-hipError_t launch_scan_prepare(const ScanArgs& a, float* bc, hipStream_t s);
-hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const float* first, float* hs, const float* ds,
-                             bool reverse, hipStream_t s);
-hipError_t launch_scan_local(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, hipStream_t s);
+hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, hipStream_t s);
+// hs: what the chunks add to what they start with; rs (or nullptr) likewise, in reverse
+hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, const float* first, bool reverse,
+                             hipStream_t s);
 
 }  // namespace cgconv

@@ -138,27 +138,41 @@ def cgconv_unpack8(dtype, rows, C, codes, scales, x, stream) -> int:
 
 # ---- tensors -------------------------------------------------------------------
 
+_codes = {}  # torch dtype: CGCONV_* code
+
+
 def _dtype_code(name, dtype) -> int:
-    import torch
-    if dtype == torch.float32:
-        return CGCONV_F32
-    if dtype == torch.bfloat16:
-        return CGCONV_BF16
-    raise ValueError(f"{name} must be float32 or bfloat16")
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: CGCONV_F32, torch.bfloat16: CGCONV_BF16})
+    code = _codes.get(dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32 or bfloat16")
+    return code
 
 
 def _tensor(name, t, shape, dtype, device):
-    """t's address after its checks; None stays None."""
-    import torch
+    """t's address after its checks; None stays None.  A step's call spends most
+    of its time here: the accepted case is five cheap queries."""
     if t is None:
         return None
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.device.index != device:
         raise ValueError(f"{name} is on GPU {t.device.index}, expected GPU {device}")
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+
+
+def _features_dtype(name, t):
+    """dtype and code of a feature tensor."""
+    dtype = getattr(t, "dtype", None)
+    return dtype, _dtype_code(name, dtype)
 
 
 def _scale_shape(shape):
@@ -238,48 +252,61 @@ def kept(ctx):
 
 class SequencePlan:
     """Sizes and workspace of the sequence operators for features
-    [batch, N, (L_max+1)^2, C] (fp32 or bf16) on the current GPU."""
+    [batch, N, (L_max+1)^2, C] (fp32 or bf16) on the current GPU; states: S of
+    the selective scan (0: no scans, a smaller workspace)."""
 
     def __init__(self, batch: int, N: int, L_max: int, C: int, states: int = 0):
+        import torch
         self._h = None
         self._h = cgconv_seq_plan_create(int(batch), int(N), int(L_max), int(C), int(states))
-        import torch
+        self._lib = _main().library()
         self.device = torch.cuda.current_device()
         self.batch, self.N, self.L_max, self.C, self.states = int(batch), int(N), int(L_max), int(C), int(states)
         self.shape = (self.batch, self.N, (self.L_max + 1) ** 2, self.C)
+        self.token_shape = (self.batch,) + self.shape[2:]  # of a step
+        self.state_shape = (self.batch, self.states) + self.shape[2:]  # of a scan
+        self._on = torch.device("cuda", self.device)
+        self._f32, self._empty = torch.float32, torch.empty
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._raw_stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
     def info(self) -> int:
         """Workspace bytes."""
         return cgconv_seq_plan_info(self._h)
 
-    def _features(self, name, t, dtype):
-        return _tensor(name, t, self.shape, dtype, self.device)
+    def _done(self, status: int) -> None:
+        if status < 0:
+            P = _main()
+            raise P.CgconvError(status, P.cgconv_last_error())
 
-    def _empty(self, shape, dtype):
-        import torch
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", self.device))
+    def _out(self, out, like, shape):
+        """(out, its address); a new tensor if out is None."""
+        if out is None:
+            out = self._empty(shape, dtype=like.dtype, device=self._on)
+            return out, out.data_ptr()
+        return out, _tensor("out", out, shape, like.dtype, self.device)
+
+    def _new(self, shape, dtype, wanted=True):
+        return self._empty(shape, dtype=dtype, device=self._on) if wanted else None
 
     def norm(self, x, weight=None, bias=None, eps: float = 1e-5, checkpoint: bool = False, out=None):
         """Layer norm by degree (L_max = 0: the ordinary layer norm): weight
         [L_max+1, C] and bias [C], fp32 or None.  Returns (y, mean [batch, N],
         rstd [batch, N, L_max+1]), and the 8-bit checkpoint (codes, scales) of x
         behind them if asked for."""
-        import torch
-        P = _main()
-        code = _dtype_code("x", x.dtype)
-        f32 = torch.float32
-        px = self._features("x", x, x.dtype)
-        if out is None:
-            out = self._empty(self.shape, x.dtype)
-        mean, rstd = self._empty(self.shape[:2], f32), self._empty(self.shape[:2] + (self.L_max + 1,), f32)
+        dtype, code = _features_dtype("x", x)
+        f32, dev = self._f32, self.device
+        px = _tensor("x", x, self.shape, dtype, dev)
+        pw, pb = _tensor("weight", weight, (self.L_max + 1, self.C), f32, dev), _tensor("bias", bias, (self.C,), f32, dev)
+        out, po = self._out(out, x, self.shape)
+        mean, rstd = self._new(self.shape[:2], f32), self._new(self.shape[:2] + (self.L_max + 1,), f32)
         codes = scales = None
         if checkpoint:
-            codes = self._empty(self.shape, torch.int8)
-            scales = self._empty(_scale_shape(self.shape), torch.uint8)
-        cgconv_seq_norm(self._h, code, px, _tensor("weight", weight, (self.L_max + 1, self.C), f32, self.device),
-                        _tensor("bias", bias, (self.C,), f32, self.device), eps, self._features("out", out, x.dtype),
-                        mean.data_ptr(), rstd.data_ptr(), codes.data_ptr() if checkpoint else None,
-                        scales.data_ptr() if checkpoint else None, P._current_stream(torch))
+            import torch
+            codes, scales = self._new(self.shape, torch.int8), self._new(_scale_shape(self.shape), torch.uint8)
+        self._done(self._lib.cgconv_seq_norm(self._h, code, px, pw, pb, eps, po, mean.data_ptr(), rstd.data_ptr(),
+                                             codes.data_ptr() if checkpoint else None,
+                                             scales.data_ptr() if checkpoint else None, self._raw_stream(dev)))
         return (out, mean, rstd, codes, scales) if checkpoint else (out, mean, rstd)
 
     def norm_backward(self, x, weight, mean, rstd, grad_y, need_x: bool = True, need_weight: bool = True,
@@ -287,51 +314,50 @@ class SequencePlan:
         """(grad_x, grad_weight, grad_bias) given grad_y and the forward's
         statistics; x is the input or its checkpoint (codes, scales).  A
         gradient that is not needed is None."""
-        import torch
-        P = _main()
         if not (need_x or need_weight or need_bias):
             return None, None, None
-        f32, dtype = torch.float32, grad_y.dtype
-        code = _dtype_code("grad_y", dtype)
+        dtype, code = _features_dtype("grad_y", grad_y)
+        f32, dev = self._f32, self.device
         px = pc = ps = None
         if isinstance(x, (tuple, list)):
+            import torch
             codes, scales = x
-            pc = _tensor("codes", codes, self.shape, torch.int8, self.device)
-            ps = _tensor("scales", scales, _scale_shape(self.shape), torch.uint8, self.device)
+            pc = _tensor("codes", codes, self.shape, torch.int8, dev)
+            ps = _tensor("scales", scales, _scale_shape(self.shape), torch.uint8, dev)
         else:
-            px = self._features("x", x, dtype)
-        args = (self._h, code, px, pc, ps, _tensor("weight", weight, (self.L_max + 1, self.C), f32, self.device),
-                _tensor("mean", mean, self.shape[:2], f32, self.device),
-                _tensor("rstd", rstd, self.shape[:2] + (self.L_max + 1,), f32, self.device),
-                self._features("grad_y", grad_y, dtype))
-        gx = self._empty(self.shape, dtype) if need_x else None
-        gw = self._empty((self.L_max + 1, self.C), f32) if need_weight else None
-        gb = self._empty((self.C,), f32) if need_bias else None
-        cgconv_seq_norm_backward(*args, *(None if t is None else t.data_ptr() for t in (gx, gw, gb)),
-                                 P._current_stream(torch))
-        return gx, gw, gb
+            px = _tensor("x", x, self.shape, dtype, dev)
+        args = (self._h, code, px, pc, ps, _tensor("weight", weight, (self.L_max + 1, self.C), f32, dev),
+                _tensor("mean", mean, self.shape[:2], f32, dev),
+                _tensor("rstd", rstd, self.shape[:2] + (self.L_max + 1,), f32, dev),
+                _tensor("grad_y", grad_y, self.shape, dtype, dev))
+        grads = (self._new(self.shape, dtype, need_x), self._new((self.L_max + 1, self.C), f32, need_weight),
+                 self._new((self.C,), f32, need_bias))
+        self._done(self._lib.cgconv_seq_norm_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
+                                                      self._raw_stream(dev)))
+        return grads
 
     # ---- short causal convolution
 
     def _conv_args(self, x, weight, bias, shape):
-        import torch
-        f32 = torch.float32
-        code = _dtype_code("x", x.dtype)
-        if not isinstance(weight, torch.Tensor) or weight.ndim != 3:
-            raise ValueError(f"weight must be a GPU tensor of shape [width, {self.L_max + 1}, {self.C}]")
-        width = int(weight.shape[0])
-        return (self._h, code, width, _tensor("x", x, shape, x.dtype, self.device),
-                _tensor("weight", weight, (width, self.L_max + 1, self.C), f32, self.device),
-                _tensor("bias", bias, (self.C,), f32, self.device))
+        dtype, code = _features_dtype("x", x)
+        width = len(weight) if getattr(weight, "ndim", 0) == 3 else 0
+        dev, f32 = self.device, self._f32
+        return dtype, width, (self._h, code, width, _tensor("x", x, shape, dtype, dev),
+                              _tensor("weight", weight, (width, self.L_max + 1, self.C), f32, dev),
+                              _tensor("bias", bias, (self.C,), f32, dev))
 
     def _lengths(self, lengths):
+        if lengths is None:
+            return None
         import torch
         return _tensor("lengths", lengths, (self.batch,), torch.int32, self.device)
 
+    def _conv_state_shape(self, width):
+        return (self.batch, max(width - 1, 0)) + self.shape[2:]
+
     def conv_state(self, width: int, dtype=None):
         """The state before the first token: zeros [batch, width - 1, K, C]."""
-        import torch
-        return self._empty((self.batch, width - 1) + self.shape[2:], dtype or torch.float32).zero_()
+        return self._new(self._conv_state_shape(width), dtype or self._f32).zero_()
 
     def conv(self, x, weight, bias=None, lengths=None, state=None, activation: bool = True, out=None):
         """Short causal convolution over the tokens: weight [width, L_max+1, C]
@@ -340,115 +366,90 @@ class SequencePlan:
         their outputs are zero.  Returns (y, state): the width - 1 inputs before
         every sequence's end, [batch, width - 1, K, C], for conv_step or the
         next piece (state=)."""
-        import torch
-        P = _main()
-        args = self._conv_args(x, weight, bias, self.shape)
-        if out is None:
-            out = self._empty(self.shape, x.dtype)
-        state_shape = (self.batch, max(args[2] - 1, 0)) + self.shape[2:]
-        last = self._empty(state_shape, x.dtype)
-        cgconv_seq_conv(*args, int(bool(activation)), self._lengths(lengths),
-                        _tensor("state", state, state_shape, x.dtype, self.device),
-                        self._features("out", out, x.dtype), last.data_ptr(), P._current_stream(torch))
+        dtype, width, args = self._conv_args(x, weight, bias, self.shape)
+        shape, pl = self._conv_state_shape(width), self._lengths(lengths)
+        ps = _tensor("state", state, shape, dtype, self.device)
+        out, po = self._out(out, x, self.shape)
+        last = self._new(shape, dtype)
+        self._done(self._lib.cgconv_seq_conv(*args, 1 if activation else 0, pl, ps, po, last.data_ptr(),
+                                             self._raw_stream(self.device)))
         return out, last
 
     def conv_step(self, x, weight, bias, state, activation: bool = True, out=None):
         """One token of every sequence: x [batch, K, C]; state is moved on in
         place.  Returns y [batch, K, C]."""
-        import torch
-        P = _main()
-        shape = (self.batch,) + self.shape[2:]
-        args = self._conv_args(x, weight, bias, shape)
-        if out is None:
-            out = self._empty(shape, x.dtype)
-        cgconv_seq_conv_step(*args, int(bool(activation)),
-                             _tensor("state", state, (self.batch, max(args[2] - 1, 0)) + self.shape[2:], x.dtype,
-                                     self.device),
-                             _tensor("out", out, shape, x.dtype, self.device), P._current_stream(torch))
+        dtype, width, args = self._conv_args(x, weight, bias, self.token_shape)
+        ps = _tensor("state", state, self._conv_state_shape(width), dtype, self.device)
+        out, po = self._out(out, x, self.token_shape)
+        self._done(self._lib.cgconv_seq_conv_step(*args, 1 if activation else 0, ps, po,
+                                                  self._raw_stream(self.device)))
         return out
 
     def conv_backward(self, x, weight, bias, grad_y, lengths=None, activation: bool = True, need_x: bool = True,
                       need_weight: bool = True, need_bias: bool = True):
         """(grad_x, grad_weight, grad_bias) given grad_y, from the zero state; a
         gradient that is not needed is None."""
-        import torch
-        P = _main()
         if not (need_x or need_weight or need_bias):
             return None, None, None
-        args = self._conv_args(x, weight, bias, self.shape) + (
-            int(bool(activation)), self._lengths(lengths), self._features("grad_y", grad_y, x.dtype))
-        gx = self._empty(self.shape, x.dtype) if need_x else None
-        gw = self._empty(weight.shape, torch.float32) if need_weight else None
-        gb = self._empty((self.C,), torch.float32) if need_bias else None
-        cgconv_seq_conv_backward(*args, *(None if t is None else t.data_ptr() for t in (gx, gw, gb)),
-                                 P._current_stream(torch))
-        return gx, gw, gb
+        dtype, width, args = self._conv_args(x, weight, bias, self.shape)
+        args += (1 if activation else 0, self._lengths(lengths),
+                 _tensor("grad_y", grad_y, self.shape, dtype, self.device))
+        grads = (self._new(self.shape, dtype, need_x), self._new(weight.shape, self._f32, need_weight),
+                 self._new((self.C,), self._f32, need_bias))
+        self._done(self._lib.cgconv_seq_conv_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
+                                                      self._raw_stream(self.device)))
+        return grads
 
     # ---- selective scan
 
-    def _scan_args(self, x, delta, A, Bt, Ct, D, delta_bias, tokens):
-        import torch
-        f32 = torch.float32
-        code = _dtype_code("x", x.dtype)
-        lead = (self.batch,) + tokens
-        S, C, dev = self.states, self.C, self.device
-        return (self._h, code, _tensor("x", x, lead + self.shape[2:], x.dtype, dev),
-                _tensor("delta", delta, lead + (C,), x.dtype, dev), _tensor("A", A, (C, S), f32, dev),
-                _tensor("Bt", Bt, lead + (S,), x.dtype, dev), _tensor("Ct", Ct, lead + (S,), x.dtype, dev),
-                _tensor("D", D, (C,), f32, dev), _tensor("delta_bias", delta_bias, (C,), f32, dev))
+    def _scan_args(self, x, delta, A, Bt, Ct, D, delta_bias, lead, shape):
+        dtype, code = _features_dtype("x", x)
+        S, C, dev, f32 = self.states, self.C, self.device, self._f32
+        rows = lead + (S,)
+        return dtype, (self._h, code, _tensor("x", x, shape, dtype, dev),
+                       _tensor("delta", delta, lead + (C,), dtype, dev), _tensor("A", A, (C, S), f32, dev),
+                       _tensor("Bt", Bt, rows, dtype, dev), _tensor("Ct", Ct, rows, dtype, dev),
+                       _tensor("D", D, (C,), f32, dev), _tensor("delta_bias", delta_bias, (C,), f32, dev))
 
     def scan_state(self):
         """The state before the first token: fp32 zeros [batch, S, K, C]."""
-        import torch
-        return self._empty((self.batch, self.states) + self.shape[2:], torch.float32).zero_()
+        return self._new(self.state_shape, self._f32).zero_()
 
     def scan(self, x, delta, A, Bt, Ct, D=None, delta_bias=None, lengths=None, state=None, out=None):
         """Selective scan of whole sequences: delta [batch, N, C], Bt and Ct
         [batch, N, S] of x's type, A [C, S], D and delta_bias [C] in fp32.
         Returns (y, state): the state [batch, S, K, C] (fp32) after every
         sequence's last token, for scan_step or the next piece (state=)."""
-        import torch
-        P = _main()
-        args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, (self.N,))
-        if out is None:
-            out = self._empty(self.shape, x.dtype)
-        state_shape = (self.batch, self.states) + self.shape[2:]
-        last = self._empty(state_shape, torch.float32)
-        cgconv_seq_scan(*args, self._lengths(lengths),
-                        _tensor("state", state, state_shape, torch.float32, self.device),
-                        self._features("out", out, x.dtype), last.data_ptr(), P._current_stream(torch))
+        _, args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, self.shape[:2], self.shape)
+        pl, ps = self._lengths(lengths), _tensor("state", state, self.state_shape, self._f32, self.device)
+        out, po = self._out(out, x, self.shape)
+        last = self._new(self.state_shape, self._f32)
+        self._done(self._lib.cgconv_seq_scan(*args, pl, ps, po, last.data_ptr(), self._raw_stream(self.device)))
         return out, last
 
     def scan_step(self, x, delta, A, Bt, Ct, D, state, delta_bias=None, out=None):
         """One token of every sequence: x [batch, K, C], delta [batch, C], Bt
         and Ct [batch, S]; state is moved on in place.  Returns y [batch, K, C]."""
-        import torch
-        P = _main()
-        args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, ())
-        shape = (self.batch,) + self.shape[2:]
-        if out is None:
-            out = self._empty(shape, x.dtype)
-        cgconv_seq_scan_step(*args, _tensor("state", state, (self.batch, self.states) + self.shape[2:],
-                                            torch.float32, self.device),
-                             _tensor("out", out, shape, x.dtype, self.device), P._current_stream(torch))
+        _, args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, self.shape[:1], self.token_shape)
+        ps = _tensor("state", state, self.state_shape, self._f32, self.device)
+        out, po = self._out(out, x, self.token_shape)
+        self._done(self._lib.cgconv_seq_scan_step(*args, ps, po, self._raw_stream(self.device)))
         return out
 
     def scan_backward(self, x, delta, A, Bt, Ct, D, grad_y, delta_bias=None, lengths=None, need=(True,) * 7):
         """Gradients of (x, delta, A, Bt, Ct, D, delta_bias) given grad_y, from
         the zero state; None where ``need`` is False."""
-        import torch
-        P = _main()
         if not any(need):
             return (None,) * 7
-        f32 = torch.float32
-        args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, (self.N,)) + (
-            self._lengths(lengths), self._features("grad_y", grad_y, x.dtype))
-        lead = (self.batch, self.N)
-        shapes = ((self.shape, x.dtype), (lead + (self.C,), x.dtype), ((self.C, self.states), f32),
-                  (lead + (self.states,), x.dtype), (lead + (self.states,), x.dtype), ((self.C,), f32), ((self.C,), f32))
-        grads = tuple(self._empty(*s) if n else None for s, n in zip(shapes, need))
-        cgconv_seq_scan_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
-                                 P._current_stream(torch))
+        lead, f32 = self.shape[:2], self._f32
+        dtype, args = self._scan_args(x, delta, A, Bt, Ct, D, delta_bias, lead, self.shape)
+        args += (self._lengths(lengths), _tensor("grad_y", grad_y, self.shape, dtype, self.device))
+        rows = (lead + (self.states,), dtype)
+        shapes = ((self.shape, dtype), (lead + (self.C,), dtype), ((self.C, self.states), f32), rows, rows,
+                  ((self.C,), f32), ((self.C,), f32))
+        grads = tuple(self._new(*s, n) for s, n in zip(shapes, need))
+        self._done(self._lib.cgconv_seq_scan_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
+                                                      self._raw_stream(self.device)))
         return grads
 
     def close(self):
