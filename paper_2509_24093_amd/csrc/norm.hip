@@ -41,6 +41,24 @@ struct RowShape {
 
 __device__ __forceinline__ int degree_of(int comp) { return (int)__builtin_sqrtf((float)comp + 0.5f); }
 
+// out[i] = f(sum of the rows of degree i % (L+1) of token i / (L+1)), 16 lanes per
+// sum: a lane reads one row's sum (the first also the 17th row's of degree 8), so
+// the block waits for one LDS access and four lane steps rather than for a loop
+// over the rows.
+template <class F>
+__device__ __forceinline__ void degree_sums(const float* rowsum, float* out, int toks, int degs, int K, int threads,
+                                            F f) {
+  const int lane = threadIdx.x & 15;
+  for (int i = threadIdx.x >> 4; i < toks * degs; i += threads >> 4) {
+    const int tok = i / degs, l = i - tok * degs;
+    const float* p = rowsum + tok * K + l * l;
+    float s = lane < 2 * l + 1 ? p[lane] : 0.f;
+    if (lane == 0 && l == 8) s += p[16];
+    s = group_sum(s, 16);
+    if (lane == 0) out[i] = f(s, i, l);
+  }
+}
+
 // Dynamic LDS: a row's sums, then a degree's.
 template <class T, int V, int R, bool CODES>
 __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
@@ -94,15 +112,11 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
   }
   __syncthreads();
   const int degs = a.L + 1;
-  for (int i = tid; i < toks * degs; i += sh.threads) {
-    const int tok = i / degs, l = i - tok * degs;
-    const float* p = rowsum + tok * a.K + l * l;
-    float s = 0.f;
-    for (int m = 0; m < 2 * l + 1; ++m) s += p[m];
+  degree_sums(rowsum, rs, toks, degs, a.K, sh.threads, [&](float s, int i, int l) {
     const float r = 1.f / __builtin_sqrtf(s / (float)((2 * l + 1) * a.C) + a.eps);
-    rs[i] = r;
     if (a.rstd) a.rstd[t0 * degs + i] = r;
-  }
+    return r;
+  });
   __syncthreads();
   T* y = static_cast<T*>(a.y) + t0 * a.K * a.C;
 #pragma unroll
@@ -143,10 +157,28 @@ __device__ __forceinline__ float block_sum(float v, float* lds, int threads) {
   return s;
 }
 
+// Sums of two values over the block in one exchange.
+__device__ __forceinline__ void block_sum2(float& u, float& v, float* lds, int threads) {
+  u = group_sum(u, 64);
+  v = group_sum(v, 64);
+  if (threads == 64) return;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    lds[threadIdx.x >> 6] = u;
+    lds[16 + (threadIdx.x >> 6)] = v;
+  }
+  __syncthreads();
+  u = v = 0.f;
+  for (int w = 0; w < threads / 64; ++w) {
+    u += lds[w];
+    v += lds[16 + w];
+  }
+}
+
 // Wide rows: block (token, degree), the degree's (2l+1) C values in registers.
 // CODES only where C is a multiple of 32 (a scale's lanes are then neighbours).
-template <class T, int V, int R, bool CODES>
-__global__ void norm_wide_kernel(NormArgs a) {
+template <class T, int V, int R, bool CODES, int MAXT>
+__global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a) {
   __shared__ float lds[16];
   const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
   const int n = (2 * l + 1) * a.C;
@@ -288,13 +320,8 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
       if (j == 0 && tok[i] < toks) rowsum[i * per + rg] = q;
     }
     __syncthreads();
-    for (int i = tid; i < toks * degs; i += sh.threads) {
-      const int t = i / degs, l = i - t * degs;
-      const float* p = rowsum + t * a.K + l * l;
-      float s = 0.f;
-      for (int m = 0; m < 2 * l + 1; ++m) s += p[m];
-      ds[i] = s / (float)((2 * l + 1) * a.C);
-    }
+    degree_sums(rowsum, ds, toks, degs, a.K, sh.threads,
+                [&](float s, int, int l) { return s / (float)((2 * l + 1) * a.C); });
     __syncthreads();
     if (a.gx) {
       T* gx = static_cast<T*>(a.gx) + t0 * a.K * a.C;
@@ -342,11 +369,18 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
   }
 }
 
-// Wide rows: block (slot, degree) takes tokens slot, slot + gridDim.x, ...
+// Wide rows: block (slot, degree) takes tokens slot, slot + gridDim.x, ..., each
+// loaded as it is stored while the one before is computed for bf16 rows of whole
+// vectors, where that takes 16 registers and four waves per SIMD still fit (8 x
+// 2048 tokens of 4096 channels, forward and backward: 185 -> 164 us, at three waves
+// 190; with 8-bit inputs three waves, 32768 of 1024 139 -> 107; fp32, 4 x 4096
+// tokens of L=2 C=512 with 32 registers ahead: 320 -> 392).
 // Partial sums: part[slot][K components, then gb][C].
-template <class T, int V, int R, bool CODES>
-__global__ void norm_wide_bwd_kernel(NormBwdArgs a) {
-  __shared__ float lds[16];
+template <class T, int V, int R, bool CODES, int MAXT>
+__global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 3 : 4) : 2) void norm_wide_bwd_kernel(
+    NormBwdArgs a) {
+  constexpr bool kAhead = MAXT <= 256 && V == 8;
+  __shared__ float lds[32];
   const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
   const int n = (2 * l + 1) * a.C, nb = (a.C + kPackBlock - 1) / kPackBlock;
   float gw[R][V], gb[R][V];
@@ -354,9 +388,34 @@ __global__ void norm_wide_bwd_kernel(NormBwdArgs a) {
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) gw[i][e] = gb[i][e] = 0.f;
-  for (long long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+  constexpr int kHeld = kAhead ? R : 1;
+  Raw<T, V> xr[kHeld], gr[kHeld];
+  Raw<int8_t, V> cr[kHeld];
+  uint32_t sc[kHeld];
+  float r0n = 0.f, m0n = 0.f;
+  auto fetch = [&](long long t) {
     const long long row0 = t * a.K + l * l;
-    const float r0 = a.rstd[t * (a.L + 1) + l], m0 = l == 0 ? a.mean[t] : 0.f;
+    r0n = a.rstd[t * (a.L + 1) + l];
+    m0n = l == 0 ? a.mean[t] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int e0 = (i * threads + tid) * V;
+      if (e0 < n) {
+        if (CODES) {
+          const int m = e0 / a.C;
+          cr[i].load(a.codes + row0 * a.C + e0);
+          sc[i] = a.scales[(row0 + m) * nb + (e0 - m * a.C) / kPackBlock];
+        } else {
+          xr[i].load(static_cast<const T*>(a.x) + row0 * a.C + e0);
+        }
+        gr[i].load(static_cast<const T*>(a.gy) + row0 * a.C + e0);
+      }
+    }
+  };
+  if (kAhead && blockIdx.x < a.tokens) fetch(blockIdx.x);
+  for (long long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+    const float r0 = kAhead ? r0n : a.rstd[t * (a.L + 1) + l];
+    const float m0 = kAhead ? m0n : l == 0 ? a.mean[t] : 0.f;
     float h[R][V], g[R][V];
     float q = 0.f, s = 0.f;
 #pragma unroll
@@ -364,12 +423,21 @@ __global__ void norm_wide_bwd_kernel(NormBwdArgs a) {
       const int e0 = (i * threads + tid) * V;
 #pragma unroll
       for (int e = 0; e < V; ++e) h[i][e] = m0, g[i][e] = 0.f;
-      if (e0 < n) {
+      if (e0 >= n) continue;
+      if constexpr (kAhead) {
+        if (CODES)
+          unpack_codes(cr[i], sc[i], h[i]);
+        else
+          xr[i].widen_to(h[i]);
+        gr[i].widen_to(g[i]);
+      } else {
+        const long long row0 = t * a.K + l * l;
         const int m = e0 / a.C;
         load_input<T, V, CODES>(a, row0 + m, e0 - m * a.C, nb, h[i]);
         load_vec(static_cast<const T*>(a.gy) + row0 * a.C + e0, g[i]);
       }
     }
+    if (kAhead && t + gridDim.x < a.tokens) fetch(t + gridDim.x);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int e0 = (i * threads + tid) * V;
@@ -388,9 +456,9 @@ __global__ void norm_wide_bwd_kernel(NormBwdArgs a) {
       }
     }
     if (!a.gx) continue;
-    const float d = block_sum(q, lds, threads) / (float)n;
-    const float m1 = l == 0 ? block_sum(s, lds, threads) / (float)n : 0.f;
-    T* gx = static_cast<T*>(a.gx) + row0 * a.C;
+    block_sum2(q, s, lds, threads);
+    const float d = q / (float)n, m1 = l == 0 ? s / (float)n : 0.f;
+    T* gx = static_cast<T*>(a.gx) + (t * a.K + l * l) * a.C;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int e0 = (i * threads + tid) * V;
@@ -407,11 +475,8 @@ __global__ void norm_wide_bwd_kernel(NormBwdArgs a) {
   for (int i = 0; i < R; ++i) {
     const int e0 = (i * threads + tid) * V;
     if (e0 >= n) continue;
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      part[(long long)l * l * a.C + e0 + e] = gw[i][e];
-      if (l == 0) part[(long long)a.K * a.C + e0 + e] = gb[i][e];
-    }
+    store_vec(part + (long long)l * l * a.C + e0, gw[i]);
+    if (l == 0) store_vec(part + (long long)a.K * a.C + e0, gb[i]);
   }
 }
 
@@ -453,9 +518,14 @@ __global__ __launch_bounds__(64 * kSumSlices) void norm_sum_kernel(const float* 
 constexpr int kPassStep = 2;
 
 // Row form: the block and pass count that leave the fewest lanes without a row,
-// at most max_passes rows per thread and max_values values per block; 0 tokens
-// if a token does not fit.
-RowShape row_shape(int C, int K, int V, int max_passes, int max_threads, int max_values) {
+// at most max_passes rows per thread, max_threads threads and max_values values
+// per block; a block larger than 256 threads has to gain `gain` of its lanes for
+// it; 0 tokens if a token does not fit.  At B=8 N=16384 L=6 C=32 (49 rows of 8
+// lanes): forward, 512 threads x 4 rows (96% of the lanes) against 256 x 8 and 256
+// x 4 (77%), whole step 753, 773, 772 us; backward, whose blocks wait for each
+// other at two barriers a tile, 256 x 4 against 512 x 4: 773, 784, with the 8-bit
+// input 778, 899.
+RowShape row_shape(int C, int K, int V, int max_passes, int max_threads, int max_values, double gain) {
   RowShape best{1, 0, 0, 0};
   const int vecs = (C + V - 1) / V;
   if (vecs > 64) return best;
@@ -466,8 +536,8 @@ RowShape row_shape(int C, int K, int V, int max_passes, int max_threads, int max
     for (int passes = kPassStep; passes <= max_passes; passes += kPassStep) {
       const int tokens = per * passes / K;
       if (tokens < 1 || threads * passes * V > max_values) continue;
-      const double use = (double)(tokens * K) / (per * passes) - (threads > 512 ? 0.1 : 0.0);
-      if (use > score + 0.02) {
+      const double use = (double)(tokens * K) / (per * passes);
+      if (use > score + (threads > best.threads && best.threads ? gain : 0.02)) {
         score = use;
         best.threads = threads;
         best.passes = passes;
@@ -497,8 +567,12 @@ int row_bwd_blocks(long long tokens, const RowShape& sh) {
   const long long tiles = (tokens + sh.tokens - 1) / sh.tokens;
   return (int)std::min<long long>(tiles, kBwdBlocks * 256 / sh.threads);
 }
-int wide_bwd_blocks(long long tokens, int L) {
-  return (int)std::min<long long>(tokens, std::max(64, 1024 / (L + 1)));
+// A thread's share of the chip per degree, at most 2048 blocks in all: each writes
+// sums that are read again (16384 tokens of 4096 bf16 channels in blocks of 256: 512
+// blocks 178 us, 1024 164, 2048 179; 32768 of 1024 in blocks of 64: 1024 173, 2048
+// 139).
+int wide_bwd_blocks(long long tokens, int L, int threads) {
+  return (int)std::min<long long>(tokens, std::max(64, std::min(2048, (1 << 18) / threads) / (L + 1)));
 }
 
 size_t row_lds_floats(const RowShape& sh, int K, int L) { return (size_t)sh.tokens * (K + L + 1); }
@@ -520,16 +594,17 @@ template <class T, int V, int R>
 hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
   if (a.tokens > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)a.tokens, a.L + 1);
-  if (a.codes && a.C % kPackBlock == 0) {
-    hipLaunchKernelGGL((norm_wide_kernel<T, V, R, true>), grid, dim3(threads), 0, s, a);
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
     return hipGetLastError();
-  }
+  };
+  if (a.codes && a.C % kPackBlock == 0)
+    return threads <= 256 ? run(norm_wide_kernel<T, V, R, true, 256>) : run(norm_wide_kernel<T, V, R, true, 1024>);
   if (a.codes) {  // a scale's channels would straddle the lanes: a pass of its own
     const hipError_t e = launch_pack(a.type, a.x, a.codes, a.scales, a.tokens * a.K, a.C, s);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((norm_wide_kernel<T, V, R, false>), grid, dim3(threads), 0, s, a);
-  return hipGetLastError();
+  return threads <= 256 ? run(norm_wide_kernel<T, V, R, false, 256>) : run(norm_wide_kernel<T, V, R, false, 1024>);
 }
 
 template <class T, int V, int R>
@@ -552,13 +627,17 @@ hipError_t norm_rows_bwd(const NormBwdArgs& a, const RowShape& sh, hipStream_t s
 
 template <class T, int V, int R>
 hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
-  const int blocks = wide_bwd_blocks(a.tokens, a.L);
+  const int blocks = wide_bwd_blocks(a.tokens, a.L, threads);
   const dim3 grid(blocks, a.L + 1);
-  if (a.codes)
-    hipLaunchKernelGGL((norm_wide_bwd_kernel<T, V, R, true>), grid, dim3(threads), 0, s, a);
-  else
-    hipLaunchKernelGGL((norm_wide_bwd_kernel<T, V, R, false>), grid, dim3(threads), 0, s, a);
-  const hipError_t e = hipGetLastError();
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+    return hipGetLastError();
+  };
+  const hipError_t e =
+      a.codes ? (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, true, 256>)
+                                : run(norm_wide_bwd_kernel<T, V, R, true, 1024>))
+              : (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, false, 256>)
+                                : run(norm_wide_bwd_kernel<T, V, R, false, 1024>));
   if (e != hipSuccess || !a.part) return e;
   hipLaunchKernelGGL(norm_sum_kernel, dim3(((a.L + 2) * a.C + 63) / 64), dim3(64 * kSumSlices), 0, s, a.part, blocks,
                      a.L, a.K, a.C, 0, a.gw, a.gb);
@@ -567,22 +646,20 @@ hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
 
 // Values a thread holds of one array: 32 in the forward, 16 in the backward
 // (which holds four arrays).
-constexpr int kFwdPasses = 8;
+constexpr int kFwdPasses = 4;
 constexpr int fwd_values(int V) { return V >= 4 ? 32 : 16; }
 constexpr int kBwdValues = 16;
 constexpr int bwd_passes(int V) { return V >= 4 ? kBwdValues / V : 4; }
 // a block's gw is staged in at most 64 KiB of LDS
-RowShape bwd_row_shape(int C, int K, int V) { return row_shape(C, K, V, bwd_passes(V), kBwdRowThreads, 16384); }
+RowShape bwd_row_shape(int C, int K, int V) { return row_shape(C, K, V, bwd_passes(V), kBwdRowThreads, 16384, 1.0); }
 
 template <class T, int V>
 hipError_t norm_any(const NormArgs& a, hipStream_t s) {
-  const RowShape sh = row_shape(a.C, a.K, V, kFwdPasses, 1024, 1024 * 32);
+  const RowShape sh = row_shape(a.C, a.K, V, kFwdPasses, 1024, 1024 * 32, 0.1);
   if (sh.tokens) {
     switch (sh.passes) {
       case 2: return norm_rows<T, V, 2>(a, sh, s);
       case 4: return norm_rows<T, V, 4>(a, sh, s);
-      case 6: return norm_rows<T, V, 6>(a, sh, s);
-      case 8: return norm_rows<T, V, 8>(a, sh, s);
       default: return hipErrorInvalidValue;
     }
   }
@@ -623,8 +700,9 @@ size_t norm_bwd_part_bytes(long long tokens, int L, int C) {
   size_t rows = 0;
   for (int type : {SEQ_F32, SEQ_BF16}) {
     const RowShape sh = bwd_row_shape(C, K, seq_vec(type, C));
+    const int v = seq_vec(type, C), threads = wide_shape((2 * L + 1) * C, v, kBwdValues / v).threads;
     rows = std::max(rows, sh.tokens ? (size_t)row_bwd_blocks(tokens, sh) * (L + 2)
-                                    : (size_t)wide_bwd_blocks(tokens, L) * (K + 1));
+                                    : (size_t)wide_bwd_blocks(tokens, L, threads) * (K + 1));
   }
   return rows * C * sizeof(float);
 }

@@ -1,6 +1,9 @@
 // Activation checkpoints in 8 bits (format: seq_common.h): rows of C channels
 // of any tensor to int8 codes and one power-of-two scale byte per 32 channels,
-// and back.  Both directions are streams, bound by HBM.
+// and back.  Both directions are streams, bound by HBM.  A tensor larger than the
+// chip's caches (kPackNtBytes) is read and written with nontemporal accesses: it
+// leaves the caches before anybody reads it again (410 MB of bf16 there and back
+// 216 -> 192 us; 57 MB, which stay cached between the two, would go 28.5 -> 30).
 #include <hip/hip_runtime.h>
 
 #include "seq_common.h"
@@ -12,10 +15,11 @@ namespace {
 using namespace seqdev;
 
 constexpr int kThreads = 256;
+constexpr long long kPackNtBytes = 256LL << 20;
 
 // One group of V lanes-worth of elements per thread: the 32 / V lanes of a
 // scale's channels are neighbours, and a row's last group leaves lanes idle.
-template <class T, int V, bool PACK>
+template <class T, int V, bool PACK, bool NT>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const T* __restrict__ x, const int8_t* __restrict__ codes_in,
                                                         const uint8_t* __restrict__ scales_in, T* __restrict__ out,
                                                         int8_t* __restrict__ codes, uint8_t* __restrict__ scales,
@@ -33,13 +37,13 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const T* __restrict__ x,
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = 0.f;
   if (PACK) {
-    if (here) load_vec(x + at, v);
+    if (here) load_vec<NT>(x + at, v);
     const uint32_t scale = pack_scale(group_max_bits(max_bits(v), kLanes));
     if (here) store_codes(codes + at, v, scale);
     if (j == 0) scales[g] = (uint8_t)scale;
   } else if (here) {
     load_codes(codes_in + at, scales_in[g], v);
-    store_vec(out + at, v);
+    store_vec<NT>(out + at, v);
   }
 }
 
@@ -49,9 +53,13 @@ hipError_t launch(const void* x, int8_t* codes, uint8_t* scales, void* out, long
   const long long groups = rows * nb;
   const long long blocks = (groups * (kPackBlock / V) + kThreads - 1) / kThreads;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((pack_kernel<T, V, PACK>), dim3((unsigned)blocks), dim3(kThreads), 0, s,
-                     static_cast<const T*>(x), codes, scales, static_cast<T*>(out), codes, scales, groups, C, nb);
-  return hipGetLastError();
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, static_cast<const T*>(x), codes, scales,
+                       static_cast<T*>(out), codes, scales, groups, C, nb);
+    return hipGetLastError();
+  };
+  return rows * C * (long long)sizeof(T) > kPackNtBytes ? run(pack_kernel<T, V, PACK, true>)
+                                                        : run(pack_kernel<T, V, PACK, false>);
 }
 
 template <bool PACK>

@@ -36,9 +36,6 @@ struct Column {
   }
 };
 
-// Tokens whose x and delta are loaded while the ones before are computed.
-constexpr int kAhead = 4;
-
 // LOCAL: pass (1), else pass (3) from pass (2)'s states (or the caller's, or zero).
 template <class T, int KG, int SP, bool LOCAL>
 __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChunks sh, ScanSpace ws, int colblocks) {
@@ -53,20 +50,24 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
   T* yp = static_cast<T*>(a.y) + row0 * KC + col;
   const T* dp = static_cast<const T*>(a.delta) + row0 * a.C + q.c;
   const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
-  float dn[kAhead], xn[kAhead][KG];
+  // tokens whose x and delta are loaded while the ones before are computed
+  constexpr int kAhead = 4;
+  const float rows_seen = colblocks <= 2 ? touch_rows<SP>(ws.bc + row0 * 2 * SP, t0, t2) : 0.f;
+  T dn[kAhead], xn[kAhead][KG];  // as stored: widening them here would wait for them
   auto fetch = [&](int tb) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int t = min(tb + u, t2 - 1);
-      dn[u] = widen(dp[(long long)t * a.C]);
+      dn[u] = dp[(long long)t * a.C];
+      // (a component that is not there repeats the last one; it is never stored)
 #pragma unroll
-      for (int i = 0; i < KG; ++i) xn[u][i] = i < q.nk ? widen(xp[t * KC + (long long)i * a.C]) : 0.f;
+      for (int i = 0; i < KG; ++i) xn[u][i] = xp[t * KC + (long long)min(i, q.nk - 1) * a.C];
     }
   };
-  TokenRow<SP> p;
+  TokenRows<SP> rows;
   if (t0 < t2) {
     fetch(t0);
-    p.load(bc + (long long)t0 * 2 * SP);
+    rows.begin(bc, t0);
   }
   float A2[SP], h[SP][KG];
 #pragma unroll
@@ -87,46 +88,50 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
   }
   const float bias = a.bias ? a.bias[q.c] : 0.f, D = !LOCAL && a.D ? a.D[q.c] : 0.f;
   float total = 0.f;
-  for (int tb = t0; tb < t2; tb += kAhead) {
-    float dc[kAhead], xc[kAhead][KG];
+  settle_rows(rows_seen);
+  auto token = [&](int t, T draw, const T (&xraw)[KG]) {
+    const float* p = rows.at(t, min(t + 1, t2 - 1));
+    const float d = softplus(widen(draw) + bias);
+    if (LOCAL) total += d;
+    float dx[KG], y[KG];
+#pragma unroll
+    for (int i = 0; i < KG; ++i) {
+      const float x = widen(xraw[i]);
+      dx[i] = d * x;
+      y[i] = D * x;
+    }
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+      const float e = exp2_fast(d * A2[s]);
+#pragma unroll
+      for (int i = 0; i < KG; ++i) {
+        h[s][i] = fmaf(e, h[s][i], p[s] * dx[i]);
+        if (!LOCAL) y[i] = fmaf(p[SP + s], h[s][i], y[i]);
+      }
+    }
+    if (!LOCAL && q.here) {
+#pragma unroll
+      for (int i = 0; i < KG; ++i)
+        if (i < q.nk) yp[t * KC + (long long)i * a.C] = (T)y[i];
+    }
+  };
+  int tb = t0;
+  for (; tb + kAhead <= t2; tb += kAhead) {  // no conditions inside: the rows change registers without copies
+    T dc[kAhead], xc[kAhead][KG];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       dc[u] = dn[u];
 #pragma unroll
       for (int i = 0; i < KG; ++i) xc[u][i] = xn[u][i];
     }
-    if (tb + kAhead < t2) fetch(tb + kAhead);
+    fetch(tb + kAhead);  // (the last token again at the end: under a condition it would move behind the loop)
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int t = tb + u;
-      if (t >= t2) break;
-      TokenRow<SP> next;
-      next.load(bc + (long long)min(t + 1, t2 - 1) * 2 * SP);
-      const float d = softplus(dc[u] + bias);
-      if (LOCAL) total += d;
-      float dx[KG], y[KG];
-#pragma unroll
-      for (int i = 0; i < KG; ++i) {
-        dx[i] = d * xc[u][i];
-        y[i] = D * xc[u][i];
-      }
-#pragma unroll
-      for (int s = 0; s < SP; ++s) {
-        const float e = exp2_fast(d * A2[s]);
-#pragma unroll
-        for (int i = 0; i < KG; ++i) {
-          h[s][i] = fmaf(e, h[s][i], p.v[s] * dx[i]);
-          if (!LOCAL) y[i] = fmaf(p.v[SP + s], h[s][i], y[i]);
-        }
-      }
-      if (!LOCAL && q.here) {
-#pragma unroll
-        for (int i = 0; i < KG; ++i)
-          if (i < q.nk) yp[t * KC + (long long)i * a.C] = (T)y[i];
-      }
-      p = next;
-    }
+    for (int u = 0; u < kAhead; ++u) token(tb + u, dc[u], xc[u]);
   }
+#pragma unroll
+  for (int u = 0; u < kAhead - 1; ++u)
+    if (tb + u < t2) token(tb + u, dn[u], xn[u]);
   if (!q.here) return;
   if (!LOCAL) {
     for (int t = max(t0, t2); t < t1; ++t)
@@ -148,10 +153,12 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
 
 // Pass (2): h <- exp(A ds) h + add from chunk to chunk, for 64 states per block;
 // each of its kCarrySlices waves first composes its own run of chunks, then
-// starts from the runs before it.  The arrays hold, in, what a chunk adds and,
-// out, what it starts with; y = 1 of the grid goes through rs backwards.  The
-// chunk at the far end adds to nobody and need not be formed.
-constexpr int kCarrySlices = 8;
+// starts from the runs before it.  A run of at most RUN chunks stays in registers
+// between the two, a longer one (not HELD) is read twice.  The arrays hold, in,
+// what a chunk adds and, out, what it starts with; y = 1 of the grid goes through
+// rs backwards.  The chunk at the far end adds to nobody and need not be formed.
+constexpr int kCarrySlices = 16;
+template <int RUN, bool HELD>
 __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, ScanChunks sh, ScanSpace ws,
                                                                   const float* first) {
   __shared__ float scale[kCarrySlices][64], shift[kCarrySlices][64];
@@ -166,11 +173,11 @@ __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, Sc
   float* p = (reverse ? ws.rs : ws.hs) + (long long)b * sh.chunks * a.S * KC + id;
   const float* d = ws.ds + (long long)b * sh.chunks * a.C + c;
   const int run = (sh.chunks + kCarrySlices - 1) / kCarrySlices;
-  const int n0 = slice * run, n1 = min(n0 + run, sh.chunks);
-  constexpr int kBatch = 8;
-  auto load = [&](int n, float (&add)[kBatch], float (&e)[kBatch]) {
+  const int n0 = min(slice * run, sh.chunks), n1 = min(n0 + run, sh.chunks);
+  float add[RUN], e[RUN];
+  auto load = [&](int n) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
+    for (int i = 0; i < RUN; ++i) {
       const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
       const bool in = n + i < n1 && n + i < sh.chunks - 1;
       add[i] = in ? p[ch * a.S * KC] : 0.f;
@@ -178,14 +185,14 @@ __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, Sc
     }
   };
   float E = 1.f, H = 0.f;
-  for (int n = n0; n < n1; n += kBatch) {
-    float add[kBatch], e[kBatch];
-    load(n, add, e);
+  for (int n = n0; n < n1; n += RUN) {
+    load(n);
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
+    for (int i = 0; i < RUN; ++i) {
       H = fmaf(e[i], H, add[i]);
       E *= e[i];
     }
+    if (HELD) break;
   }
   scale[slice][lane] = E;
   shift[slice][lane] = H;
@@ -193,16 +200,17 @@ __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, Sc
   float h = first && !reverse ? first[(long long)b * a.S * KC + id] : 0.f;
   for (int i = 0; i < slice; ++i) h = fmaf(scale[i][lane], h, shift[i][lane]);
   if (!here) return;
-  for (int n = n0; n < n1; n += kBatch) {
-    float add[kBatch], e[kBatch];
-    load(n, add, e);
+  for (int n = n0; n < n1; n += RUN) {
+    if (!HELD) load(n);
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      if (n + i >= n1) break;
-      const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
-      p[ch * a.S * KC] = h;
-      h = fmaf(e[i], h, add[i]);
+    for (int i = 0; i < RUN; ++i) {
+      if (n + i < n1) {
+        const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
+        p[ch * a.S * KC] = h;
+        h = fmaf(e[i], h, add[i]);
+      }
     }
+    if (HELD) break;
   }
 }
 
@@ -220,16 +228,42 @@ __global__ __launch_bounds__(kScanThreads) void prepare_kernel(ScanArgs a, ScanS
   }
 }
 
-// One token: thread of V neighbouring channels of one component, the states
-// streamed through.
+// One token: a thread takes V neighbouring channels of one component and four
+// states; the 1 .. 8 groups of states of the same channels are lanes of one wave,
+// 64 / groups apart, so the loads of a group are neighbours and y is a sum over
+// lanes.  Bound by reading and writing the state: 16 states as one loop per thread
+// with A read value by value took 12.8 us at 64 x 2048 channels, XXX this way.
+constexpr int kStepStates = 4;
 template <class T, int V>
-__global__ __launch_bounds__(kScanThreads) void scan_step_kernel(ScanArgs a, int cols, long long threads) {
-  const long long id = (long long)blockIdx.x * kScanThreads + threadIdx.x;
-  if (id >= threads) return;
-  const long long b = id / cols;
-  const int e0 = (int)(id - b * cols) * V, c = e0 % a.C;
+__global__ __launch_bounds__(kScanThreads) void scan_step_kernel(ScanArgs a, int cols, long long vecs, int groups) {
+  const int lanes = 64 / groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long id = ((long long)blockIdx.x * (kScanThreads / 64) + wave) * lanes + lane % lanes;
+  const bool here = id < vecs;
+  const int s0 = lane / lanes * kStepStates;
+  const long long at = here ? id : 0, b = at / cols;
+  const int e0 = (int)(at - b * cols) * V, c = e0 % a.C;
   const long long KC = (long long)a.K * a.C;
-  float x[V], d[V], y[V], dx[V];
+  float x[V], d[V], y[V], h[kStepStates][V], A[V][kStepStates], Bs[kStepStates], Cs[kStepStates];
+  float* state = a.state_out + (b * a.S + s0) * KC + e0;
+#pragma unroll
+  for (int s = 0; s < kStepStates; ++s) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[s][e] = 0.f;
+    const bool there = s0 + s < a.S;
+    if (there) load_vec(state + s * KC, h[s]);
+    Bs[s] = there ? load1<T>(a.Bt, b * a.S + s0 + s) : 0.f;
+    Cs[s] = there ? load1<T>(a.Ct, b * a.S + s0 + s) : 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float* p = a.A + (long long)(c + e) * a.S + s0;
+    if (a.S % 4 == 0 && s0 < a.S) {  // whole rows of four, 16-byte aligned
+      load_vec(p, A[e]);
+    } else {
+#pragma unroll
+      for (int s = 0; s < kStepStates; ++s) A[e][s] = s0 + s < a.S ? p[s] : 0.f;
+    }
+  }
   load_vec(static_cast<const T*>(a.x) + b * KC + e0, x);
   load_vec(static_cast<const T*>(a.delta) + b * a.C + c, d);
   float D[V], bias[V];
@@ -239,38 +273,36 @@ __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(ScanArgs a, int
   if (a.bias) load_vec(a.bias + c, bias);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    d[e] = softplus(d[e] + bias[e]);
-    dx[e] = d[e] * x[e];
-    y[e] = D[e] * x[e];
-    d[e] *= kLog2e;
-  }
-  float* h = a.state_out + b * a.S * KC + e0;
-#pragma unroll 4
-  for (int s = 0; s < a.S; ++s) {
-    const float Bs = load1<T>(a.Bt, b * a.S + s), Cs = load1<T>(a.Ct, b * a.S + s);
-    float v[V];
-    load_vec(h + s * KC, v);
+    const float step = softplus(d[e] + bias[e]), dx = step * x[e], d2 = step * kLog2e;
+    y[e] = 0.f;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      v[e] = fmaf(exp2_fast(d[e] * a.A[(long long)(c + e) * a.S + s]), v[e], Bs * dx[e]);
-      y[e] = fmaf(Cs, v[e], y[e]);
+    for (int s = 0; s < kStepStates; ++s) {
+      h[s][e] = fmaf(exp2_fast(d2 * A[e][s]), h[s][e], Bs[s] * dx);
+      y[e] = fmaf(Cs[s], h[s][e], y[e]);
     }
-    store_vec(h + s * KC, v);
+    for (int n = lanes; n < 64; n *= 2) y[e] += __shfl_xor(y[e], n);
+    y[e] = fmaf(D[e], x[e], y[e]);
   }
-  store_vec(static_cast<T*>(a.y) + b * KC + e0, y);
+  if (!here) return;
+#pragma unroll
+  for (int s = 0; s < kStepStates; ++s)
+    if (s0 + s < a.S) store_vec(state + s * KC, h[s]);
+  if (s0 == 0) store_vec(static_cast<T*>(a.y) + b * KC + e0, y);
 }
 
-// Waves that keep the vector units busy, and the shortest chunk worth its
-// state (S values written and read per chunk and column).
-constexpr long long kWantedWaves = 4096;
-constexpr int kMinChunk = 32;
+// Waves that keep the vector units busy (4 x 8192 tokens of 2048 channels: 1024
+// 778 us, 2048 523, 4096 460, 8192 345, 16384 350), and the shortest chunk worth its
+// states (S values written and read per chunk and column), shorter in short
+// sequences, whose time is that of one chunk (300 tokens of 9 x 16: XXX).
+constexpr long long kWantedWaves = 8192;
+int64_t min_chunk(int64_t N) { return std::max<int64_t>(8, std::min<int64_t>(32, N / 16)); }
 
 int components_per_thread(int K) { return K == 1 ? 1 : K == 9 ? 3 : 4; }
 
 ScanChunks forward_chunks(int64_t B, int64_t N, int K, int64_t C) {
   const int kg = components_per_thread(K);
   const int64_t waves = B * (((K + kg - 1) / kg * C + 63) / 64);
-  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(kWantedWaves / waves, N / kMinChunk));
+  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(kWantedWaves / waves, N / min_chunk(N)));
   ScanChunks s;
   s.chunk = (int)((N + chunks - 1) / chunks);
   s.chunks = (int)((N + s.chunk - 1) / s.chunk);
@@ -334,9 +366,12 @@ hipError_t scan_forward(const ScanArgs& a, hipStream_t s) {
 template <class T, int V>
 hipError_t scan_step(const ScanArgs& a, hipStream_t s) {
   const int cols = a.K * a.C / V;
-  const long long threads = (long long)a.B * cols;
-  hipLaunchKernelGGL((scan_step_kernel<T, V>), dim3((unsigned)((threads + kScanThreads - 1) / kScanThreads)),
-                     dim3(kScanThreads), 0, s, a, cols, threads);
+  const long long vecs = (long long)a.B * cols;
+  int groups = 1;
+  while (groups * kStepStates < a.S) groups *= 2;
+  const int per = kScanThreads / groups;  // vectors per block
+  hipLaunchKernelGGL((scan_step_kernel<T, V>), dim3((unsigned)((vecs + per - 1) / per)), dim3(kScanThreads), 0, s, a,
+                     cols, vecs, groups);
   return hipGetLastError();
 }
 
@@ -357,8 +392,17 @@ hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, hipStream_
 hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, const float* first, bool reverse,
                              hipStream_t s) {
   const long long n = (long long)a.S * a.K * a.C;
-  hipLaunchKernelGGL(carry_kernel, dim3((unsigned)((n + 63) / 64), reverse ? 2 : 1, a.B), dim3(64 * kCarrySlices), 0, s,
-                     a, ch, w, first);
+  const dim3 grid((unsigned)((n + 63) / 64), reverse ? 2 : 1, a.B), block(64 * kCarrySlices);
+  const int run = (ch.chunks + kCarrySlices - 1) / kCarrySlices;
+  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, ch, w, first); };
+  if (run <= 1)
+    go(carry_kernel<1, true>);
+  else if (run <= 4)
+    go(carry_kernel<4, true>);
+  else if (run <= 16)
+    go(carry_kernel<16, true>);
+  else
+    go(carry_kernel<16, false>);
   return hipGetLastError();
 }
 

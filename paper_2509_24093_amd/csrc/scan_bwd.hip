@@ -32,22 +32,31 @@ using namespace seqdev;
 
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// Tokens per chunk and per piece, threads per block, by states: the piece's
-// states take kSub SP registers, the pieces' starts (chunk / sub - 1) SP threads
-// 4 bytes of LDS (48 KiB).
+// A thread of the main kernel holds kGroup states of a column; the SP / kGroup
+// groups of a column are waves of one block, so B_t and C_t stay scalar and the
+// sums over all states go through LDS.  Tokens per chunk and per piece, columns per
+// block: the states of a piece take kSub kGroup registers, the pieces' starts
+// (chunk / sub - 1) kGroup columns groups 4 bytes of LDS (48 KiB), the sums kSub
+// columns groups 8 bytes.  With all 16 states in a thread the registers allowed two
+// waves per SIMD, which left the vector units idle 40% of the time (2 x 4096 x 1024
+// bf16: 195 us, XXX now).
+constexpr int kGroup = 8;
 template <int SP>
 struct BwdShape {
-  static constexpr int kSub = SP == 32 ? 4 : 8;
-  static constexpr int kChunk = SP == 32 ? 16 : 32;
-  static constexpr int kThreads = SP == 32 ? 128 : 256;
+  static constexpr int kGroups = SP / kGroup;
+  static constexpr int kSub = SP == 8 ? 8 : 4;
+  static constexpr int kChunk = 4 * kSub;
+  static constexpr int kColumns = SP == 32 ? 128 : 256;
+  static constexpr int kThreads = kColumns * kGroups;
 };
-int bwd_chunk(int S) { return scan_padded(S) == 32 ? BwdShape<32>::kChunk : BwdShape<16>::kChunk; }
-int bwd_threads(int S) { return scan_padded(S) == 32 ? BwdShape<32>::kThreads : BwdShape<16>::kThreads; }
+int bwd_chunk(int S) { return scan_padded(S) == 8 ? BwdShape<8>::kChunk : BwdShape<16>::kChunk; }
+static_assert(BwdShape<16>::kChunk == BwdShape<32>::kChunk, "");
+int bwd_columns(int S) { return scan_padded(S) == 32 ? BwdShape<32>::kColumns : BwdShape<16>::kColumns; }
 
 // The states that a chunk ends with from zero, the gradient that its own outputs
 // send to the state before it, and its sum of delta.
 template <class T, int SP>
-__global__ __launch_bounds__(BwdShape<SP>::kThreads) void ends_kernel(ScanBwdArgs g, ScanChunks sh, ScanSpace ws,
+__global__ __launch_bounds__(256) void ends_kernel(ScanBwdArgs g, ScanChunks sh, ScanSpace ws,
                                                                       int colblocks) {
   const ScanArgs& a = g.a;
   const int ch = blockIdx.x / colblocks, b = blockIdx.y;
@@ -63,20 +72,21 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads) void ends_kernel(ScanBwdArg
   const T* dp = static_cast<const T*>(a.delta) + row0 * a.C + c;
   const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
   constexpr int kAhead = 4;
-  float dn[kAhead], xn[kAhead], gn[kAhead];
+  const float rows_seen = colblocks <= 2 ? touch_rows<SP>(ws.bc + row0 * 2 * SP, t0, t2) : 0.f;
+  T dn[kAhead], xn[kAhead], gn[kAhead];  // as stored: widening them here would wait for them
   auto fetch = [&](int tb) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int t = min(tb + u, t2 - 1);
-      dn[u] = widen(dp[(long long)t * a.C]);
-      xn[u] = widen(xp[(long long)t * KC]);
-      gn[u] = widen(gyp[(long long)t * KC]);
+      dn[u] = dp[(long long)t * a.C];
+      xn[u] = xp[(long long)t * KC];
+      gn[u] = gyp[(long long)t * KC];
     }
   };
-  TokenRow<SP> p;
+  TokenRows<SP> rows;
   if (t0 < t2) {
     fetch(t0);
-    p.load(bc + (long long)t0 * 2 * SP);
+    rows.begin(bc, t0);
   }
   float A2[SP], h[SP], r[SP], P[SP];
 #pragma unroll
@@ -87,33 +97,36 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads) void ends_kernel(ScanBwdArg
   }
   const float bias = a.bias ? a.bias[c] : 0.f;
   float total = 0.f;
-  for (int tb = t0; tb < t2; tb += kAhead) {
-    float dc[kAhead], xc[kAhead], gc[kAhead];
+  settle_rows(rows_seen);
+  auto token = [&](int t, T draw, T xraw, T graw) {
+    const float* p = rows.at(t, min(t + 1, t2 - 1));
+    const float d = softplus(widen(draw) + bias), dx = d * widen(xraw), gy = widen(graw);
+    total += d;
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+      const float e = exp2_fast(d * A2[s]);
+      h[s] = fmaf(e, h[s], p[s] * dx);
+      P[s] *= e;
+      r[s] = fmaf(P[s], p[SP + s] * gy, r[s]);
+    }
+  };
+  int tb = t0;
+  for (; tb + kAhead <= t2; tb += kAhead) {  // no conditions inside: the rows change registers without copies
+    T dc[kAhead], xc[kAhead], gc[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       dc[u] = dn[u];
       xc[u] = xn[u];
       gc[u] = gn[u];
     }
-    if (tb + kAhead < t2) fetch(tb + kAhead);
+    fetch(tb + kAhead);  // (the last token again at the end: under a condition it would move behind the loop)
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int t = tb + u;
-      if (t >= t2) break;
-      TokenRow<SP> next;
-      next.load(bc + (long long)min(t + 1, t2 - 1) * 2 * SP);
-      const float d = softplus(dc[u] + bias), dx = d * xc[u];
-      total += d;
-#pragma unroll
-      for (int s = 0; s < SP; ++s) {
-        const float e = exp2_fast(d * A2[s]);
-        h[s] = fmaf(e, h[s], p.v[s] * dx);
-        P[s] *= e;
-        r[s] = fmaf(P[s], p.v[SP + s] * gc[u], r[s]);
-      }
-      p = next;
-    }
+    for (int u = 0; u < kAhead; ++u) token(tb + u, dc[u], xc[u], gc[u]);
   }
+#pragma unroll
+  for (int u = 0; u < kAhead - 1; ++u)
+    if (tb + u < t2) token(tb + u, dn[u], xn[u], gn[u]);
   if (!here) return;
   const long long at = ((long long)b * sh.chunks + ch) * a.S * KC + j;
 #pragma unroll
@@ -166,7 +179,7 @@ __device__ __forceinline__ float wave_scatter_sum(float (&v)[N], int lane) {
   }
   halve<0x140, N / 4>(v, lane & 8);                      // row mirror
   halve<0x141, N / 8>(v, lane & 4);                      // half-row mirror
-  halve<0x4E, N / 16>(v, lane & 2);                      // quad_perm 2, 3, 0, 1
+  halve<0x4E, (N / 16 > 0 ? N / 16 : 1)>(v, lane & 2);   // quad_perm 2, 3, 0, 1
   halve<0xB1, (N / 32 > 0 ? N / 32 : 1)>(v, lane & 1);   // quad_perm 1, 0, 3, 2
   return v[0];
 }
@@ -175,21 +188,28 @@ __device__ __forceinline__ float wave_scatter_sum(float (&v)[N], int lane) {
 template <int N>
 __device__ __forceinline__ int scatter_index(int lane) { return lane / (64 / N); }
 
-// Block (chunk, column block) of a batch element; thread = column k C + c.  ONE:
-// K = 1, delta's gradient is finished here.
+// Block (chunk, column block) of a batch element: `columns` columns k C + c (whole
+// waves) x the groups of states, group slowest.  ONE: K = 1, delta's gradient is
+// finished here.
 template <class T, int SP, bool ONE>
-__global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(ScanBwdArgs g, ScanChunks sh,
-                                                                             ScanSpace ws, int colblocks) {
-  constexpr int kSub = BwdShape<SP>::kSub, kThreads = BwdShape<SP>::kThreads;
-  constexpr int kPieces = BwdShape<SP>::kChunk / kSub, kWaves = kThreads / 64;
-  __shared__ float starts[kPieces - 1][SP][kThreads];
-  __shared__ float red[kWaves][kSub][2 * SP];
+__global__ __launch_bounds__(BwdShape<SP>::kThreads, SP == 8 ? 3 : 4) void scan_bwd_kernel(ScanBwdArgs g,
+                                                                                           ScanChunks sh, ScanSpace ws,
+                                                                                           int colblocks, int columns) {
+  typedef BwdShape<SP> Shape;
+  constexpr int kSub = Shape::kSub, kGroups = Shape::kGroups, kWaves = Shape::kColumns / 64;
+  constexpr int kPieces = Shape::kChunk / kSub;
+  __shared__ float starts[kPieces - 1][kGroup][Shape::kThreads];
+  __shared__ float sums[kGroups > 1 ? kSub : 1][2][kGroups > 1 ? Shape::kThreads : 1];
+  __shared__ float red[kGroups][kWaves][kSub][2 * kGroup];
   const ScanArgs& a = g.a;
   const int ch = blockIdx.x / colblocks, cb = blockIdx.x - ch * colblocks, b = blockIdx.y;
-  const int KC = a.K * a.C, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int id = cb * blockDim.x + tid;
+  const int KC = a.K * a.C, tid = threadIdx.x, lane = tid & 63;
+  const int group = __builtin_amdgcn_readfirstlane(kGroups > 1 ? tid / columns : 0);
+  const int column = tid - group * columns, wave = column >> 6;
+  const int id = cb * columns + column;
   const bool here = id < KC;
   const int j = here ? id : 0, c = ONE ? j : j % a.C;
+  const int s0 = group * kGroup;
   const int len = scan_length(a.lengths, b, a.N);
   const int t0 = ch * sh.chunk, t1 = min(a.N, t0 + sh.chunk), t2 = min(t1, len);
   const long long row0 = (long long)b * a.N;
@@ -199,22 +219,24 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(Sca
   T* gxp = static_cast<T*>(g.gx) + row0 * KC + j;
   T* gdp = static_cast<T*>(g.gdelta) + row0 * KC + j;  // ONE
   float* gdk = ws.gd + row0 * KC + j;                  // else
-  const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP);
-  const long long at = ((long long)b * sh.chunks + ch) * a.S * KC + j;
+  const ConstFloats bc = (ConstFloats)(ws.bc + row0 * 2 * SP + s0);
+  const long long at = (((long long)b * sh.chunks + ch) * a.S + s0) * KC + j;
   const bool carried = here && sh.chunks > 1;
-  float A2[SP], r[SP], gA[SP];
+  float A2[kGroup], r[kGroup], gA[kGroup];
   const float bias = a.bias ? a.bias[c] : 0.f, D = a.D ? a.D[c] : 0.f;
   float gD = 0.f, gbias = 0.f;
   const int last = t2 > t0 ? (t2 - t0 - 1) / kSub : -1;  // the last piece
+  const float rows_seen = colblocks <= 2 ? touch_rows<SP>(ws.bc + row0 * 2 * SP, t0, t2) : 0.f;
 #pragma unroll
-  for (int s = 0; s < SP; ++s) A2[s] = ws.A2[s * a.C + c];
-  auto start = [&](float (&h)[SP]) {
+  for (int s = 0; s < kGroup; ++s) A2[s] = ws.A2[(s0 + s) * a.C + c];
+  auto start = [&](float (&h)[kGroup]) {
 #pragma unroll
-    for (int s = 0; s < SP; ++s) h[s] = carried && s < a.S ? ws.hs[at + (long long)s * KC] : 0.f;
+    for (int s = 0; s < kGroup; ++s) h[s] = carried && s0 + s < a.S ? ws.hs[at + (long long)s * KC] : 0.f;
   };
   {  // the states before every piece but the first
-    float h[SP];
+    float h[kGroup];
     start(h);
+    settle_rows(rows_seen);
 #pragma unroll 1
     for (int piece = 0; piece < last; ++piece) {
       const int ts = t0 + piece * kSub;
@@ -229,21 +251,21 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(Sca
         const float di = softplus(d[i] + bias), dx = di * x[i];
         const ConstFloats p = bc + (long long)(ts + i) * 2 * SP;
 #pragma unroll
-        for (int s = 0; s < SP; ++s) h[s] = fmaf(exp2_fast(di * A2[s]), h[s], p[s] * dx);
+        for (int s = 0; s < kGroup; ++s) h[s] = fmaf(exp2_fast(di * A2[s]), h[s], p[s] * dx);
       }
 #pragma unroll
-      for (int s = 0; s < SP; ++s) starts[piece][s][tid] = h[s];
+      for (int s = 0; s < kGroup; ++s) starts[piece][s][tid] = h[s];
     }
   }
 #pragma unroll
-  for (int s = 0; s < SP; ++s) {
-    r[s] = carried && s < a.S ? ws.rs[at + (long long)s * KC] : 0.f;
+  for (int s = 0; s < kGroup; ++s) {
+    r[s] = carried && s0 + s < a.S ? ws.rs[at + (long long)s * KC] : 0.f;
     gA[s] = 0.f;
   }
 #pragma unroll 1
   for (int piece = last; piece >= 0; --piece) {
     const int ts = t0 + piece * kSub, n = min(kSub, t2 - ts);
-    float hist[kSub][SP], d[kSub], x[kSub], gy[kSub];  // hist[i]: before token i
+    float hist[kSub][kGroup], d[kSub], x[kSub], gy[kSub];  // hist[i]: before token i
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
       const int t = ts + min(i, n - 1);
@@ -254,7 +276,7 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(Sca
     }
     if (piece) {
 #pragma unroll
-      for (int s = 0; s < SP; ++s) hist[0][s] = starts[piece - 1][s][tid];
+      for (int s = 0; s < kGroup; ++s) hist[0][s] = starts[piece - 1][s][tid];
     } else {
       start(hist[0]);
     }
@@ -264,26 +286,40 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(Sca
         d[i] = softplus(d[i]);
         const float dx = d[i] * x[i];
         const ConstFloats p = bc + (long long)(ts + i) * 2 * SP;
-        float v[SP];
+        float v[kGroup];
 #pragma unroll
-        for (int s = 0; s < SP; ++s) {
+        for (int s = 0; s < kGroup; ++s) {
           const float h = fmaf(exp2_fast(d[i] * A2[s]), hist[i][s], p[s] * dx);
           v[s] = h * gy[i];
           if (i + 1 < kSub) hist[i + 1][s] = h;
         }
-        red[wave][i][SP + scatter_index<SP>(lane)] = wave_scatter_sum(v, lane);
+        red[group][wave][i][kGroup + scatter_index<kGroup>(lane)] = wave_scatter_sum(v, lane);
       }
     }
+    // gradients that add over the states: of x (from `into`) and of delta
+    auto finish = [&](int i, float into, float gd) {
+      const long long t = ts + i;
+      gd = fmaf(gd, kLn2, into * x[i]);
+      if (ONE) {
+        gd /= 1.f + exp2_fast(-kLog2e * (widen(dp[t * a.C]) + bias));  // the derivative of softplus; delta read again
+        gbias += gd;
+      }
+      if (!here) return;
+      if (g.gx) gxp[t * KC] = (T)fmaf(d[i], into, D * gy[i]);
+      if (ONE) {
+        if (g.gdelta) gdp[t * KC] = (T)gd;
+      } else {
+        gdk[t * KC] = gd;
+      }
+    };
 #pragma unroll
     for (int i = kSub - 1; i >= 0; --i) {
       if (i < n) {
-        const long long t = ts + i;
-        const ConstFloats p = bc + t * 2 * SP;
+        const ConstFloats p = bc + (long long)(ts + i) * 2 * SP;
         const float dx = d[i] * x[i];
-        const float raw = ONE ? widen(dp[t * a.C]) + bias : 0.f;  // read again: fewer registers
-        float v[SP], into = 0.f, gd = 0.f;
+        float v[kGroup], into = 0.f, gd = 0.f;
 #pragma unroll
-        for (int s = 0; s < SP; ++s) {
+        for (int s = 0; s < kGroup; ++s) {
           const float gs = fmaf(p[SP + s], gy[i], r[s]);
           v[s] = gs * dx;
           into = fmaf(p[s], gs, into);
@@ -293,43 +329,63 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, 2) void scan_bwd_kernel(Sca
           gd = fmaf(A2[s], q, gd);
         }
         gD = fmaf(gy[i], x[i], gD);
-        gd = fmaf(gd, kLn2, into * x[i]);
-        if (ONE) {
-          gd /= 1.f + exp2_fast(-kLog2e * raw);  // the derivative of softplus
-          gbias += gd;
+        red[group][wave][i][scatter_index<kGroup>(lane)] = wave_scatter_sum(v, lane);
+        if (kGroups > 1) {
+          sums[i][0][tid] = into;
+          sums[i][1][tid] = gd;
+        } else {
+          finish(i, into, gd);
         }
-        if (here) {
-          if (g.gx) gxp[t * KC] = (T)fmaf(d[i], into, D * gy[i]);
-          if (ONE) {
-            if (g.gdelta) gdp[t * KC] = (T)gd;
-          } else {
-            gdk[t * KC] = gd;
-          }
-        }
-        red[wave][i][scatter_index<SP>(lane)] = wave_scatter_sum(v, lane);
       }
     }
     __syncthreads();
-    const int waves = blockDim.x >> 6;
+    if (kGroups > 1) {  // group g finishes tokens g, g + kGroups, ...
+#pragma unroll
+      for (int i = 0; i < kSub; ++i) {
+        if (i < n && i % kGroups == group) {
+          float into = 0.f, gd = 0.f;
+#pragma unroll
+          for (int q = 0; q < kGroups; ++q) {
+            into += sums[i][0][q * columns + column];
+            gd += sums[i][1][q * columns + column];
+          }
+          finish(i, into, gd);
+        }
+      }
+    }
+    const int waves = columns >> 6;
     float* out = ws.gbc + (((long long)cb * a.B + b) * a.N + ts) * 2 * SP;
     for (int o = tid; o < n * 2 * SP; o += blockDim.x) {
-      float s = 0.f;
-      for (int w = 0; w < waves; ++w) s += (&red[w][0][0])[o];
-      out[o] = s;
+      const int i = o / (2 * SP), s = o % SP;
+      const bool isC = o % (2 * SP) >= SP;
+      float v = 0.f;
+      for (int w = 0; w < waves; ++w) v += red[s / kGroup][w][i][(isC ? kGroup : 0) + s % kGroup];
+      out[o] = v;
     }
     __syncthreads();
   }
+  if (ONE && kGroups > 1) {  // (the last barrier of the pieces was the last reader's)
+    sums[0][0][tid] = gbias;
+    __syncthreads();
+    gbias = 0.f;
+#pragma unroll
+    for (int q = 0; q < kGroups; ++q) gbias += sums[0][0][q * columns + column];
+  }
   if (!here) return;
-  for (int t = max(t0, t2); t < t1; ++t) {
-    if (g.gx) gxp[(long long)t * KC] = (T)0.f;
-    if (ONE && g.gdelta) gdp[(long long)t * KC] = (T)0.f;
+  if (group == 0) {
+    for (int t = max(t0, t2); t < t1; ++t) {
+      if (g.gx) gxp[(long long)t * KC] = (T)0.f;
+      if (ONE && g.gdelta) gdp[(long long)t * KC] = (T)0.f;
+    }
   }
   float* ga = ws.ga + ((long long)b * sh.chunks + ch) * (a.S + 2) * KC + j;
 #pragma unroll
-  for (int s = 0; s < SP; ++s)
-    if (s < a.S) ga[(long long)s * KC] = gA[s];
-  ga[(long long)a.S * KC] = gD;
-  if (ONE) ga[(long long)(a.S + 1) * KC] = gbias;
+  for (int s = 0; s < kGroup; ++s)
+    if (s0 + s < a.S) ga[(long long)(s0 + s) * KC] = gA[s];
+  if (group == 0) {
+    ga[(long long)a.S * KC] = gD;
+    if (ONE) ga[(long long)(a.S + 1) * KC] = gbias;
+  }
 }
 
 // gB_t, gC_t from the column blocks' sums.
@@ -445,8 +501,8 @@ long long bias_blocks(int64_t B, int64_t N, int64_t C) {
   return (B * N + rows - 1) / rows;
 }
 
-// Column blocks of the main kernel, of equal numbers of waves.
-int bwd_colblocks(int64_t KC, int S) { return (int)((KC + bwd_threads(S) - 1) / bwd_threads(S)); }
+// Column blocks, of equal numbers of waves.
+int bwd_colblocks(int64_t KC, int S) { return (int)((KC + bwd_columns(S) - 1) / bwd_columns(S)); }
 
 ScanSpace backward_space(void* base, int64_t B, int64_t N, int K, int64_t C, int S) {
   ScanSpace w;
@@ -480,20 +536,21 @@ hipError_t run_backward(const ScanBwdArgs& g, const ScanChunks& ch, const ScanSp
   const ScanArgs& a = g.a;
   const int KC = a.K * a.C;
   const int colblocks = bwd_colblocks(KC, a.S);
-  const int threads = ((KC + colblocks - 1) / colblocks + 63) / 64 * 64;
+  const int columns = ((KC + colblocks - 1) / colblocks + 63) / 64 * 64;
   const long long blocks = (long long)colblocks * ch.chunks;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks, a.B);
   hipError_t e;
   if (ch.chunks > 1) {
-    hipLaunchKernelGGL((ends_kernel<T, SP>), grid, dim3(threads), 0, s, g, ch, w, colblocks);
+    hipLaunchKernelGGL((ends_kernel<T, SP>), grid, dim3(columns), 0, s, g, ch, w, colblocks);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if ((e = launch_scan_carry(a, ch, w, nullptr, true, s)) != hipSuccess) return e;
   }
+  const dim3 block(columns * BwdShape<SP>::kGroups);
   if (a.K == 1)
-    hipLaunchKernelGGL((scan_bwd_kernel<T, SP, true>), grid, dim3(threads), 0, s, g, ch, w, colblocks);
+    hipLaunchKernelGGL((scan_bwd_kernel<T, SP, true>), grid, block, 0, s, g, ch, w, colblocks, columns);
   else
-    hipLaunchKernelGGL((scan_bwd_kernel<T, SP, false>), grid, dim3(threads), 0, s, g, ch, w, colblocks);
+    hipLaunchKernelGGL((scan_bwd_kernel<T, SP, false>), grid, block, 0, s, g, ch, w, colblocks, columns);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (g.gB || g.gC) {
     const long long n = ((long long)a.B * a.N * 2 * SP + 255) / 256;

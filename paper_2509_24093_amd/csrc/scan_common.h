@@ -55,6 +55,50 @@ struct TokenRow {
   }
 };
 
+// The rows of consecutive tokens: at(t) gives token t's, asked for a token ahead
+// where two rows fit the scalar registers.  Scalar loads return in any order, so
+// a wait is for all of them: the next row is asked for behind the wait for this
+// one, or this one's first use would wait for both; and the scheduler would move
+// the request to the row's use.
+template <int SP>
+struct TokenRows {
+  static constexpr bool kAhead = SP <= 16;
+  TokenRow<SP> row, next;
+  ConstFloats base;
+  __device__ __forceinline__ void begin(ConstFloats p, int t) {
+    base = p;
+    if (kAhead) next.load(base + (long long)t * 2 * SP);
+  }
+  __device__ __forceinline__ const float* at(int t, int following) {
+    if (kAhead) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+      __builtin_amdgcn_sched_barrier(0);
+      row = next;
+      next.load(base + (long long)following * 2 * SP);
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
+      row.load(base + (long long)t * 2 * SP);
+    }
+    return row.v;
+  }
+};
+
+// Brings the rows of tokens t0 .. t2 - 1 into the caches near this block: where only
+// one or two blocks share them, a scalar load of every token would otherwise wait
+// for memory on its own (2 x 8192 tokens of 49 x 32, forward: 218 -> 209 us; 4 x 8192
+// of 2048, 8 blocks a chunk, 346 -> 353).  Returns a value for settle_rows, behind
+// the block's other first loads.
+template <int SP>
+__device__ __forceinline__ float touch_rows(const float* rows, int t0, int t2) {
+  constexpr int kLine = 32;  // floats of a cache line
+  const int n = (t2 - t0) * 2 * SP;
+  const float* p = rows + (long long)t0 * 2 * SP;
+  float v = 0.f;
+  for (int i = threadIdx.x * kLine; i < n; i += blockDim.x * kLine) v += p[i];
+  return v;
+}
+__device__ __forceinline__ void settle_rows(float v) { asm volatile("" ::"v"(v)); }
+
 template <class T>
 __device__ __forceinline__ float load1(const void* p, long long i) {
   return widen(static_cast<const T*>(p)[i]);

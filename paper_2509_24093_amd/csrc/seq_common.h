@@ -28,25 +28,47 @@ typedef __bf16 bf16;
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(bf16 v) { return (float)v; }
+__device__ __forceinline__ float widen(int8_t v) { return (float)v; }
 
 // V consecutive elements (a power of two; the address a multiple of their size,
-// or of 16 where they take 32 bytes), in accesses of at most 16 bytes.
-template <class T, int V>
+// or of 16 where they take 32 bytes), in accesses of at most 16 bytes.  NT:
+// nontemporal, for what nobody reads again soon.
+template <bool NT = false, class T, int V>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[V]) {
   constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16;
   typedef typename Word<kWord>::type W;
   T t[V];
 #pragma unroll
   for (int i = 0; i < kBytes / kWord; ++i) {
-    const W w = reinterpret_cast<const W*>(p)[i];
+    const W* q = reinterpret_cast<const W*>(p) + i;
+    const W w = NT ? __builtin_nontemporal_load(q) : *q;
     __builtin_memcpy(t + i * kWord / (int)sizeof(T), &w, sizeof w);
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = widen(t[i]);
 }
 
-// Rounds to T to nearest, ties to even (nothing to round for float).
+// V elements as they are stored, to be widened later: loads kept in flight take
+// the registers of the storage type only.
 template <class T, int V>
+struct Raw {
+  static constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16, kWords = kBytes / kWord;
+  typedef typename Word<kWord>::type W;
+  W w[kWords];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const W*>(p)[i];
+  }
+  __device__ __forceinline__ void widen_to(float (&v)[V]) const {
+    T t[V];
+    __builtin_memcpy(t, w, kBytes);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = widen(t[i]);
+  }
+};
+
+// Rounds to T to nearest, ties to even (nothing to round for float).
+template <bool NT = false, class T, int V>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[V]) {
   constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16;
   typedef typename Word<kWord>::type W;
@@ -57,7 +79,11 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[V]) {
   for (int i = 0; i < kBytes / kWord; ++i) {
     W w;
     __builtin_memcpy(&w, t + i * kWord / (int)sizeof(T), sizeof w);
-    reinterpret_cast<W*>(p)[i] = w;
+    W* q = reinterpret_cast<W*>(p) + i;
+    if (NT)
+      __builtin_nontemporal_store(w, q);
+    else
+      *q = w;
   }
 }
 
@@ -143,14 +169,18 @@ __device__ __forceinline__ void store_codes(int8_t* p, const float (&v)[V], uint
 }
 
 template <int V>
-__device__ __forceinline__ void load_codes(const int8_t* p, uint32_t scale, float (&v)[V]) {
-  typedef typename Word<V>::type W;
-  const W w = *reinterpret_cast<const W*>(p);
-  int8_t t[V];
-  __builtin_memcpy(t, &w, sizeof w);
+__device__ __forceinline__ void unpack_codes(const Raw<int8_t, V>& codes, uint32_t scale, float (&v)[V]) {
+  codes.widen_to(v);
   const float s = unpack_scale(scale);
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = (float)t[i] * s;
+  for (int i = 0; i < V; ++i) v[i] *= s;
+}
+
+template <int V>
+__device__ __forceinline__ void load_codes(const int8_t* p, uint32_t scale, float (&v)[V]) {
+  Raw<int8_t, V> codes;
+  codes.load(p);
+  unpack_codes(codes, scale, v);
 }
 
 }  // namespace seqdev
