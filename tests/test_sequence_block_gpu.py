@@ -1,0 +1,271 @@
+"""The sequence operators together with the convolution, as a causal block uses
+them: training steps against the composed float64 oracle, a prompt and the tokens
+behind it, HIP graphs, streams."""
+
+import numpy as np
+import pytest
+
+from oracle import sequence as S
+from oracle.backward import backward_direct
+from oracle.conv import cgconv_direct_linear
+from tests.conftest import rel_l2
+from tests.seq_util import get, put, torch_gpu
+
+pytestmark = pytest.mark.gpu
+
+B, N, L, C, ST, W = 2, 48, 2, 8, 16, 4
+K = (L + 1) ** 2
+EPS = 1e-5
+
+
+def _parameters(seed):
+    r = np.random.default_rng(seed)
+    f = lambda *s: r.normal(size=s)  # noqa: E731
+    p = {"x": f(B, N, K, C), "k": f(B, N, K, C) / 8, "w1": 1 + 0.1 * f(L + 1, C), "b1": 0.1 * f(C),
+         "cw": f(W, L + 1, C) / 2, "cb": 0.1 * f(C), "delta": f(B, N, C), "A": -np.exp(f(C, ST)),
+         "Bt": f(B, N, ST), "Ct": f(B, N, ST), "D": f(C), "db": f(C) - 2}
+    return {k: np.asarray(v, dtype=np.float32) for k, v in p.items()}, np.asarray(f(B, N, K, C), dtype=np.float32)
+
+
+NAMES = ("x", "k", "w1", "b1", "cw", "cb", "delta", "A", "Bt", "Ct", "D", "db")
+
+
+def _oracle(p, g):
+    """Output and gradients of h = norm(x); s = scan(conv(h)); out = x + s + causal cgconv(h, k)."""
+    p = {k: v.astype(np.float64) for k, v in p.items()}
+    h = S.norm(p["x"], p["w1"], p["b1"], L, EPS)
+    c, _ = S.conv(h, p["cw"], p["cb"], L)
+    s, _ = S.scan(c, p["delta"], p["A"], p["Bt"], p["Ct"], p["D"], p["db"])
+    u = cgconv_direct_linear(h, p["k"], L)
+    gc, gdelta, gA, gB, gC, gD, gdb = S.scan_backward(c, p["delta"], p["A"], p["Bt"], p["Ct"], p["D"], g, p["db"])
+    gh, gcw, gcb = S.conv_backward(h, p["cw"], p["cb"], gc, L)
+    gq, gk = backward_direct(h, p["k"], g, L, boundary="linear")
+    gx, gw, gb = S.norm_backward(p["x"], p["w1"], gh + gq, L, EPS)
+    return p["x"] + s + u, (gx + g, gk, gw, gb, gcw, gcb, gdelta, gA, gB, gC, gD, gdb)
+
+
+def _block(P, t, seq, plan, checkpoint=None):
+    h = P.cgconv_norm(t["x"], t["w1"], t["b1"], seq, EPS, checkpoint=checkpoint)
+    c = P.cgconv_short_conv(h, t["cw"], t["cb"], seq, checkpoint=checkpoint)
+    s = P.cgconv_scan(c, t["delta"], t["A"], t["Bt"], t["Ct"], t["D"], seq, delta_bias=t["db"], checkpoint=checkpoint)
+    return t["x"] + s + P.cgconv(h, t["k"], plan, checkpoint=checkpoint)
+
+
+def test_training_step_of_a_block():
+    """Bar: the library's 1e-4 relative L2 in fp32 for every gradient (a chain of
+    four operators, each within a few 1e-6).  With 8-bit checkpoints a kept value
+    moves by at most 1/127 of its group's largest, uniformly: about 0.3 / 127 x 3
+    deviations = 0.7% of the norm; the gradients are made of four such inputs."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    p, g = _parameters(1)
+    out, grads = _oracle(p, g.astype(np.float64))
+    seq, plan = P.SequencePlan(B, N, L, C, states=ST), P.Plan(B, N, L, C, boundary="linear")
+    gt = put(g)[0]
+    for checkpoint, bar in ((None, 1e-4), ("int8", 0.05)):
+        t = {k: put(v)[0].requires_grad_(True) for k, v in p.items()}
+        y = _block(P, t, seq, plan, checkpoint)
+        got = torch.autograd.grad(y, [t[n] for n in NAMES], gt)
+        assert rel_l2(get(y), out) <= 1e-4
+        for n, a, r in zip(NAMES, got, grads):
+            assert rel_l2(get(a), r) <= bar, (checkpoint, n)
+    seq.close()
+    plan.close()
+
+
+def test_gradient_against_differences():
+    """A central difference of the fp32 loss along a random direction of all inputs:
+    with steps of 1e-2 the two losses' rounding (1e-6 of |loss| terms) and the cubic
+    term stay below 1%."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    p, g = _parameters(2)
+    seq, plan = P.SequencePlan(B, N, L, C, states=ST), P.Plan(B, N, L, C, boundary="linear")
+    gt = put(g)[0].double()
+    t = {k: put(v)[0].requires_grad_(True) for k, v in p.items()}
+    r = np.random.default_rng(3)
+    d = {k: put(r.normal(size=v.shape) * np.abs(v).mean())[0] for k, v in p.items()}
+    grads = torch.autograd.grad((_block(P, t, seq, plan).double() * gt).sum(), [t[n] for n in NAMES])
+    along = sum(float((a.double() * d[n].double()).sum()) for n, a in zip(NAMES, grads))
+    with torch.no_grad():
+        e = 1e-2 / 4
+        hi, lo = ({k: v + s * e * d[k] for k, v in t.items()} for s in (1, -1))
+        num = float(((_block(P, hi, seq, plan).double() - _block(P, lo, seq, plan).double()) * gt).sum()) / (2 * e)
+    assert abs(num - along) <= 0.01 * abs(along) + 0.05
+    seq.close()
+    plan.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_prompt_then_tokens(dtype):
+    """A padded batch of prompts, then the remaining tokens one by one: the outputs of
+    the whole sequences.  fp32: the same sums in another split (1e-5 of the largest
+    output); bf16: the same up to one rounding of each layer's values."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    p, _ = _parameters(4)
+    t = {k: put(v, dtype if k in ("x", "delta", "Bt", "Ct") else "fp32")[0] for k, v in p.items()}
+    seq = P.SequencePlan(B, N, L, C, states=ST)
+    one = P.SequencePlan(B, 1, L, C, states=ST)
+    h = seq.norm(t["x"], t["w1"], t["b1"])[0]
+    c = seq.conv(h, t["cw"], t["cb"])[0]
+    whole = seq.scan(c, t["delta"], t["A"], t["Bt"], t["Ct"], t["D"], t["db"])[0]
+    lengths = [N - 5, 17]
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    c, cs = seq.conv(h, t["cw"], t["cb"], lengths=n)
+    y, ss = seq.scan(c, t["delta"], t["A"], t["Bt"], t["Ct"], t["D"], t["db"], lengths=n)
+    for b in range(B):
+        assert torch.equal(y[b, :lengths[b]], whole[b, :lengths[b]]) and (y[b, lengths[b]:] == 0).all()
+    tol = (2e-2 if dtype == "bf16" else 1e-5) * float(whole.abs().max())
+    rows = torch.arange(B, device="cuda")
+    for i in range(5):  # sequence b's token lengths[b] + i
+        at = n.long() + i
+        pick = lambda v: v[rows, at].clone()  # noqa: E731
+        xt = pick(t["x"])
+        ht = one.norm(xt[:, None], t["w1"], t["b1"])[0][:, 0].clone()
+        ct = one.conv_step(ht, t["cw"], t["cb"], cs)
+        yt = one.scan_step(ct, pick(t["delta"]), t["A"], pick(t["Bt"]), pick(t["Ct"]), t["D"], ss, t["db"])
+        assert float((yt.float() - pick(whole).float()).abs().max()) <= tol
+    seq.close()
+    one.close()
+
+
+def _plan_calls(seq, t, g):
+    """Forward and backward of the block by the plan's methods."""
+    h, mean, rstd, codes, scales = seq.norm(t["x"], t["w1"], t["b1"], checkpoint=True)
+    c, cs = seq.conv(h, t["cw"], t["cb"])
+    s, ss = seq.scan(c, t["delta"], t["A"], t["Bt"], t["Ct"], t["D"], t["db"])
+    gs = seq.scan_backward(c, t["delta"], t["A"], t["Bt"], t["Ct"], t["D"], g, t["db"])
+    gc = seq.conv_backward(h, t["cw"], t["cb"], gs[0])
+    gn = seq.norm_backward((codes, scales), t["w1"], mean, rstd, gc[0])
+    return (h, c, cs, s, ss) + gs + gc + gn
+
+
+def test_captured_and_replayed():
+    """Two graphs of one plan, replayed in turn with eager calls of the plan between:
+    every replay gives the eager result."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    seq = P.SequencePlan(B, N, L, C, states=ST)
+    sets = []
+    for seed in (5, 6):
+        p, g = _parameters(seed)
+        sets.append(({k: put(v)[0] for k, v in p.items()}, put(g)[0]))
+    eager = [_plan_calls(seq, *s) for s in sets]
+    static = [({k: v.clone() for k, v in t.items()}, g.clone()) for t, g in sets]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _plan_calls(seq, *static[0])
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, outs = [], []
+    for t, g in static:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(_plan_calls(seq, t, g))
+        graphs.append(graph)
+    for rep in range(3):
+        for i in (0, 1, 1, 0):
+            src = (i + rep) % 2  # other inputs than the captured ones, every second round
+            for k, v in sets[src][0].items():
+                static[i][0][k].copy_(v)
+            static[i][1].copy_(sets[src][1])
+            graphs[i].replay()
+            got = [o.clone() for o in outs[i]]
+            again = _plan_calls(seq, *sets[1 - src])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, eager[src]))
+            assert all(torch.equal(a, b) for a, b in zip(again, eager[1 - src]))
+    seq.close()
+
+
+def test_captured_steps():
+    """A token's step in a graph: the states move on with every replay."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    p, _ = _parameters(7)
+    t = {k: put(v)[0] for k, v in p.items()}
+    one = P.SequencePlan(B, 1, L, C, states=ST)
+    x, delta, Bt, Ct = (t[k][:, 0].clone() for k in ("x", "delta", "Bt", "Ct"))
+
+    def step(cs, ss):
+        c = one.conv_step(x, t["cw"], t["cb"], cs)
+        return one.scan_step(c, delta, t["A"], Bt, Ct, t["D"], ss, t["db"])
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(one.conv_state(W), one.scan_state())
+    torch.cuda.synchronize()
+    cs, ss = one.conv_state(W), one.scan_state()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = step(cs, ss)
+    cs.zero_()
+    ss.zero_()
+    ec, es = one.conv_state(W), one.scan_state()
+    for i in range(6):
+        for dst, k in ((x, "x"), (delta, "delta"), (Bt, "Bt"), (Ct, "Ct")):
+            dst.copy_(t[k][:, i])
+        graph.replay()
+        want = step(ec, es)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(cs, ec) and torch.equal(ss, es)
+    one.close()
+
+
+def test_on_another_stream():
+    """Calls follow torch's current stream: inputs made on a side stream behind other
+    work, the calls there, the results read there."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    p, g = _parameters(8)
+    t, gt = {k: put(v)[0] for k, v in p.items()}, put(g)[0]
+    seq = P.SequencePlan(B, N, L, C, states=ST)
+    want = _plan_calls(seq, t, gt)
+    packed = P.checkpoint_unpack(*P.checkpoint_pack(t["x"]))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        a = torch.randn(4096, 4096, device="cuda")
+        for _ in range(4):
+            a = a @ a * 1e-4
+        late = {k: v + 0 * a[0, 0].nan_to_num() for k, v in t.items()}
+        got = _plan_calls(seq, late, gt)
+        held = P.checkpoint_unpack(*P.checkpoint_pack(late["x"]))
+        copies = [o.clone() for o in got] + [held.clone()]
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(copies, list(want) + [packed]))
+    seq.close()
+
+
+def test_gradients_reach_views_and_expanded_inputs():
+    """Leaves behind views: a weight shared by all degrees (expanded), features cut
+    out of a larger tensor; their gradients add up as autograd has it."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    p, g = _parameters(9)
+    gt = put(g)[0]
+    seq = P.SequencePlan(B, N, L, C, states=ST)
+    w = put(p["w1"][0])[0].requires_grad_(True)
+    big = torch.cat([put(p["x"])[0]] * 2, 1).requires_grad_(True)
+    y = P.cgconv_norm(big[:, :N].contiguous(), w.expand(L + 1, C).contiguous(), None, seq)
+    gw, gbig = torch.autograd.grad(y, (w, big), gt)
+    x = put(p["x"])[0]
+    _, mean, rstd = seq.norm(x, w.detach().expand(L + 1, C).contiguous())
+    gx, gws, _ = seq.norm_backward(x, w.detach().expand(L + 1, C).contiguous(), mean, rstd, gt, need_bias=False)
+    assert torch.equal(gbig[:, :N], gx) and (gbig[:, N:] == 0).all()
+    assert torch.allclose(gw, gws.sum(0), rtol=1e-6, atol=1e-6)
+    with pytest.raises(ValueError, match="contiguous"):
+        P.cgconv_norm(big[:, :N], w.expand(L + 1, C).contiguous(), None, seq)
+    # the same tensor as several inputs of a scan
+    b = put(p["Bt"])[0].requires_grad_(True)
+    y = P.cgconv_scan(x, put(p["delta"])[0], put(p["A"])[0], b, b, None, seq)
+    both, = torch.autograd.grad(y, (b,), gt)
+    parts = seq.scan_backward(x, put(p["delta"])[0], put(p["A"])[0], b.detach(), b.detach(), None, gt)
+    assert torch.equal(both, parts[3] + parts[4])
+    # no second derivatives: an error, not a silent zero
+    y = P.cgconv_norm(x.requires_grad_(True), None, None, seq)
+    gx, = torch.autograd.grad(y, (x,), gt, create_graph=True)
+    with pytest.raises(RuntimeError):
+        gx.sum().backward()
+    seq.close()
