@@ -258,6 +258,41 @@ def test_nothing_behind_a_length_is_read():
     plan.close()
 
 
+def test_masked_steps_and_vanishing_decays():
+    """A step input of minus infinity, or of the lowest number, is a step of zero: the
+    state passes by, y reads it, the step's gradient is zero.  Decays that vanish
+    leave the token's own term; a step that is large keeps finite."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    shape = (2, 45, 1, 12, 16)
+    t, (g, gv), (h0, h0v), _ = _inputs(shape, "fp32", 31, False)
+    raw = t["delta"][1].copy()
+    raw[0, 3] = raw[1, 20:40] = -np.inf
+    raw[0, 7] = np.finfo(np.float32).min
+    raw[0, :, 5] = -np.inf  # a channel without any step
+    raw[1, 2] = 60.0
+    A = t["A"][1].copy()
+    A[2, 4] = -1e30
+    A[3, 1] = -0.0
+    t["delta"], t["A"] = put(raw), put(A)
+    dev, val = {k: v[0] for k, v in t.items()}, {k: v[1] for k, v in t.items()}
+    seen = dict(val, delta=np.maximum(val["delta"], -200.0), A=np.maximum(val["A"], -1e4))  # for the bounds only
+    plan = P.SequencePlan(*shape[:4], states=16)
+    with np.errstate(over="ignore"):
+        y, last = plan.scan(*(dev[k] for k in ORDER), state=h0)
+        ry, rh = S.scan(*(val[k] for k in ORDER), None, h0v)
+        b = _Bounds(*(seen[k] for k in ORDER), None, h0v)
+        close("y", y, ry, b.ye)
+        close("state", last, rh, b.he[-1])
+        grads = plan.scan_backward(*(dev[k] for k in ORDER[:-1]), g, dev["bias"])
+        refs = S.scan_backward(*(val[k] for k in ORDER[:-1]), gv, val["bias"])
+        bounds = _Bounds(*(seen[k] for k in ORDER)).backward(gv)
+    for k, a, r in zip(ORDER, grads, refs):
+        close("grad " + k, a, r, bounds[k])
+    assert (grads[1][1, 20:40] == 0).all() and (grads[1][0, :, 5] == 0).all()
+    plan.close()
+
+
 @pytest.mark.parametrize("checkpoint", [None, "int8"])
 def test_autograd(checkpoint):
     torch = torch_gpu()

@@ -227,6 +227,6 @@ for L in (0, 1, 2, 3, 6, 8):
                                   lib.cgconv_seq_conv_backward(plan, dtype, W, big(0), big(1), big(2), 1, *(big(i) for i in range(3, 9)), None)]
                     assert not any(calls), (calls, P.cgconv_last_error())
                     for grid, block, lds, allowed in launches():
-                        assert 64 <= block[0] <= 1024 and block[0] % 64 == 0 and lds <= allowed and grid[1] <= 65535 and grid[2] == 1, (L, C, grid, block, lds)
+                        assert 64 <= block[0] <= 1024 and block[0] % 64 == 0 and lds <= allowed and grid[1] <= 65535 and grid[2] <= 65535, (L, C, grid, block, lds)
                 P.cgconv_seq_plan_destroy(plan)
 """)
