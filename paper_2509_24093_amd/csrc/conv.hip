@@ -314,9 +314,14 @@ __global__ __launch_bounds__(kSumSlices * kSumLanes) void conv_sum_kernel(const 
     const int n = j < W ? 2 * l + 1 : 1;
     const float* p = part + ((long long)j * K + l * l) * C + c;
     const long long stride = (long long)(W + 1) * K * C;
-    for (int m = 0; m < n; ++m) {
-#pragma unroll 4
-      for (int b = slice; b < blocks; b += kSumSlices) s += p[b * stride + (long long)m * C];
+    if (n == 1) {
+#pragma unroll 8
+      for (int b = slice; b < blocks; b += kSumSlices) s += p[b * stride];
+    } else {
+      for (int b = slice; b < blocks; b += kSumSlices) {
+#pragma unroll 8
+        for (int m = 0; m < n; ++m) s += p[b * stride + (long long)m * C];
+      }
     }
   }
   lds[slice][lane] = s;

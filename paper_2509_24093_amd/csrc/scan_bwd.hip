@@ -37,20 +37,22 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // sums over all states go through LDS.  Tokens per chunk and per piece, columns per
 // block: the states of a piece take kSub kGroup registers, the pieces' starts
 // (chunk / sub - 1) kGroup columns groups 4 bytes of LDS (48 KiB), the sums kSub
-// columns groups 8 bytes.  With all 16 states in a thread the registers allowed two
-// waves per SIMD, which left the vector units idle 40% of the time (2 x 4096 x 1024
-// bf16: 195 us, XXX now).
+// columns groups 8 bytes (16 KiB): two blocks per CU, four waves per SIMD.  2 x 4096
+// x 1024 bf16, 16 states, forward and backward: all 16 states in a thread, pieces of
+// 8, two waves per SIMD 366 us; groups of 8, pieces of 8 413, of 6 360, of 5 357, of 4
+// 351, of 3 374; the next piece's inputs asked for a piece ahead, with the other
+// loads ahead of their use: 302.
 constexpr int kGroup = 8;
 template <int SP>
 struct BwdShape {
   static constexpr int kGroups = SP / kGroup;
-  static constexpr int kSub = SP == 8 ? 8 : 4;
+  static constexpr int kSub = 4;
   static constexpr int kChunk = 4 * kSub;
   static constexpr int kColumns = SP == 32 ? 128 : 256;
   static constexpr int kThreads = kColumns * kGroups;
 };
-int bwd_chunk(int S) { return scan_padded(S) == 8 ? BwdShape<8>::kChunk : BwdShape<16>::kChunk; }
-static_assert(BwdShape<16>::kChunk == BwdShape<32>::kChunk, "");
+constexpr int kBwdChunk = BwdShape<16>::kChunk;  // of all
+static_assert(BwdShape<8>::kChunk == kBwdChunk && BwdShape<32>::kChunk == kBwdChunk, "");
 int bwd_columns(int S) { return scan_padded(S) == 32 ? BwdShape<32>::kColumns : BwdShape<16>::kColumns; }
 
 // The states that a chunk ends with from zero, the gradient that its own outputs
@@ -192,7 +194,7 @@ __device__ __forceinline__ int scatter_index(int lane) { return lane / (64 / N);
 // waves) x the groups of states, group slowest.  ONE: K = 1, delta's gradient is
 // finished here.
 template <class T, int SP, bool ONE>
-__global__ __launch_bounds__(BwdShape<SP>::kThreads, SP == 8 ? 3 : 4) void scan_bwd_kernel(ScanBwdArgs g,
+__global__ __launch_bounds__(BwdShape<SP>::kThreads, 4) void scan_bwd_kernel(ScanBwdArgs g,
                                                                                            ScanChunks sh, ScanSpace ws,
                                                                                            int colblocks, int columns) {
   typedef BwdShape<SP> Shape;
@@ -235,6 +237,15 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, SP == 8 ? 3 : 4) void scan_
   };
   {  // the states before every piece but the first
     float h[kGroup];
+    T dn[kSub], xn[kSub];
+    auto fetch = [&](int ts) {
+#pragma unroll
+      for (int i = 0; i < kSub; ++i) {
+        dn[i] = dp[(long long)min(ts + i, t2 - 1) * a.C];
+        xn[i] = xp[(long long)min(ts + i, t2 - 1) * KC];
+      }
+    };
+    if (last > 0) fetch(t0);
     start(h);
     settle_rows(rows_seen);
 #pragma unroll 1
@@ -243,9 +254,11 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, SP == 8 ? 3 : 4) void scan_
       float d[kSub], x[kSub];
 #pragma unroll
       for (int i = 0; i < kSub; ++i) {
-        d[i] = widen(dp[(long long)(ts + i) * a.C]);
-        x[i] = here ? widen(xp[(long long)(ts + i) * KC]) : 0.f;
+        d[i] = widen(dn[i]);
+        x[i] = here ? widen(xn[i]) : 0.f;
       }
+      fetch(ts + kSub);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < kSub; ++i) {
         const float di = softplus(d[i] + bias), dx = di * x[i];
@@ -262,18 +275,30 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, SP == 8 ? 3 : 4) void scan_
     r[s] = carried && s0 + s < a.S ? ws.rs[at + (long long)s * KC] : 0.f;
     gA[s] = 0.f;
   }
+  T dn[kSub], xn[kSub], gn[kSub];  // the next piece's, as stored
+  auto fetch = [&](int ts) {
+#pragma unroll
+    for (int i = 0; i < kSub; ++i) {
+      const int t = max(min(ts + i, t2 - 1), t0);
+      dn[i] = dp[(long long)t * a.C];
+      xn[i] = xp[(long long)t * KC];
+      gn[i] = gyp[(long long)t * KC];
+    }
+  };
+  if (last >= 0) fetch(t0 + last * kSub);
 #pragma unroll 1
   for (int piece = last; piece >= 0; --piece) {
     const int ts = t0 + piece * kSub, n = min(kSub, t2 - ts);
     float hist[kSub][kGroup], d[kSub], x[kSub], gy[kSub];  // hist[i]: before token i
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
-      const int t = ts + min(i, n - 1);
       const bool on = here && i < n;
-      d[i] = widen(dp[(long long)t * a.C]) + bias;
-      x[i] = on ? widen(xp[(long long)t * KC]) : 0.f;
-      gy[i] = on ? widen(gyp[(long long)t * KC]) : 0.f;
+      d[i] = widen(dn[i]) + bias;
+      x[i] = on ? widen(xn[i]) : 0.f;
+      gy[i] = on ? widen(gn[i]) : 0.f;
     }
+    fetch(ts - kSub);
+    __builtin_amdgcn_sched_barrier(0);
     if (piece) {
 #pragma unroll
       for (int s = 0; s < kGroup; ++s) hist[0][s] = starts[piece - 1][s][tid];
@@ -301,7 +326,7 @@ __global__ __launch_bounds__(BwdShape<SP>::kThreads, SP == 8 ? 3 : 4) void scan_
       const long long t = ts + i;
       gd = fmaf(gd, kLn2, into * x[i]);
       if (ONE) {
-        gd /= 1.f + exp2_fast(-kLog2e * (widen(dp[t * a.C]) + bias));  // the derivative of softplus; delta read again
+        gd *= __builtin_amdgcn_rcpf(1.f + exp2_fast(-kLog2e * (widen(dp[t * a.C]) + bias)));  // softplus' derivative, delta read again
         gbias += gd;
       }
       if (!here) return;
@@ -430,7 +455,7 @@ __global__ __launch_bounds__(256) void delta_kernel(ScanBwdArgs g, ScanSpace ws,
       if (t < scan_length(a.lengths, b, a.N)) {
         const float* p = ws.gd + row * a.K * a.C + c;
         const float raw = load1<T>(a.delta, row * a.C + c) + bias;
-#pragma unroll 9
+#pragma unroll 8
         for (int k = 0; k < a.K; ++k) v += p[(long long)k * a.C];
         v /= 1.f + exp2_fast(-kLog2e * raw);
       }
@@ -459,11 +484,16 @@ __global__ __launch_bounds__(kSumSlices * kSumLanes) void sum_units_kernel(const
   const int o = blockIdx.x * kSumLanes + lane, row = o / C, c = o - row * C;
   float s = 0.f;
   if (row < rows) {
-    for (int k = 0; k < K; ++k) {
-      const float* p = part + ((long long)row * K + k) * C + c;
-      const long long stride = (long long)rows * K * C;
-#pragma unroll 4
+    const float* p = part + (long long)row * K * C + c;
+    const long long stride = (long long)rows * K * C;
+    if (K == 1) {
+#pragma unroll 8
       for (long long u = slice; u < units; u += kSumSlices) s += p[u * stride];
+    } else {
+      for (long long u = slice; u < units; u += kSumSlices) {
+#pragma unroll 8
+        for (int k = 0; k < K; ++k) s += p[u * stride + (long long)k * C];
+      }
     }
   }
   lds[slice][lane] = s;
@@ -483,9 +513,9 @@ __global__ __launch_bounds__(kSumSlices * kSumLanes) void sum_units_kernel(const
   }
 }
 
-ScanChunks backward_chunks(int64_t N, int S) {
+ScanChunks backward_chunks(int64_t N) {
   ScanChunks s;
-  s.chunk = bwd_chunk(S);
+  s.chunk = kBwdChunk;
   s.chunks = (int)((N + s.chunk - 1) / s.chunk);
   return s;
 }
@@ -506,7 +536,7 @@ int bwd_colblocks(int64_t KC, int S) { return (int)((KC + bwd_columns(S) - 1) / 
 
 ScanSpace backward_space(void* base, int64_t B, int64_t N, int K, int64_t C, int S) {
   ScanSpace w;
-  const ScanChunks ch = backward_chunks(N, S);
+  const ScanChunks ch = backward_chunks(N);
   const size_t KC = (size_t)K * C, units = (size_t)B * ch.chunks;
   w.place(base, &w.bc, (size_t)B * N * 2 * scan_padded(S));
   w.place(base, &w.A2, (size_t)scan_padded(S) * C);
@@ -575,7 +605,7 @@ hipError_t run_backward(const ScanBwdArgs& g, const ScanChunks& ch, const ScanSp
 template <class T>
 hipError_t by_states(const ScanBwdArgs& g, hipStream_t s) {
   const ScanArgs& a = g.a;
-  const ScanChunks ch = backward_chunks(a.N, a.S);
+  const ScanChunks ch = backward_chunks(a.N);
   const ScanSpace w = backward_space(a.ws, a.B, a.N, a.K, a.C, a.S);
   const hipError_t e = launch_scan_prepare(a, w, s);
   if (e != hipSuccess) return e;
