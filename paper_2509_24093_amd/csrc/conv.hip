@@ -6,10 +6,14 @@
 //
 // A thread takes V neighbouring columns over a chunk of tokens and keeps the
 // last inputs in registers, so x is read once but for the W - 1 tokens before
-// a chunk.  The backward walks a chunk in the same direction: it forms z again,
+// a chunk; the next four tokens are asked for, as stored, while four are computed
+// (bf16, 4 x 8192 tokens of 2048 channels: forward 55 -> 48 us, backward 151 ->
+// 100).  The backward walks a chunk in the same direction: it forms z again,
 // gz = gy y'(z), adds gz[t] x[t-j] to gw in registers and emits
 // gx[t] = sum_j w[j] gz[t+j] W - 1 tokens later; the tokens behind a chunk are
-// formed twice.  Both are streams, bound by HBM.  A block's chunks add their
+// formed twice.  Both are streams, in fp32 bound by HBM (8 x 16384 tokens of 49 x 32:
+// 4.9 and 4.5 TB/s of what must move), in bf16 the backward by its vector
+// operations (4.0 TB/s).  A block's chunks add their
 // gw through LDS, the blocks' sums are added by a second kernel in a fixed
 // order.
 #include <hip/hip_runtime.h>
@@ -40,7 +44,8 @@ __device__ __forceinline__ int length_of(const ConvArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + __expf(-z)); }
+// (the reciprocal to one unit in the last place; a division would be ten instructions)
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
 // Weights of the thread's columns (j < a.W only) and the bias (component 0).
 template <int V, int WM>
@@ -98,10 +103,17 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a, ConvShape sh
       }
     }
   }
+  Raw<T, V> ahead[kAhead];  // the next tokens as stored, asked for while these are computed
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ahead[i].load(x + (long long)min(t + i, t2 - 1) * KC);
+  };
+  if (t0 < t2) fetch(t0);
   for (int t = t0; t < t2; t += kAhead) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (t + i < t2) load_vec(x + (t + i) * KC, row[WM - 1 + i]);
+    for (int i = 0; i < kAhead; ++i) ahead[i].widen_to(row[WM - 1 + i]);
+    fetch(t + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (t + i >= t2) break;
@@ -206,18 +218,31 @@ __global__ __launch_bounds__(kThreads) void conv_bwd_kernel(ConvBwdArgs g, ConvS
       // row[j] becomes row[j + 1] at the first token
       if (j + 1 < a.W && t0 < len) load_token<T, V>(x, nullptr, t0 - 1 - j, a.W, KC, row[j]);
     }
-    const int end = t1 + WM - 1;
+    const int end = t1 + WM - 1, there = min(end, len);
+    Raw<T, V> xr[kAhead], gr[kAhead];  // the next tokens as stored, asked for while these are computed
+    auto fetch = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const long long at = (long long)max(min(t + i, there - 1), 0) * KC;
+        xr[i].load(x + at);
+        gr[i].load(gy + at);
+      }
+    };
+    fetch(t0);
     for (int tb = t0; tb < end; tb += kAhead) {
       float xn[kAhead][V], gn[kAhead][V];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
+        xr[i].widen_to(xn[i]);
+        gr[i].widen_to(gn[i]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) xn[i][e] = gn[i][e] = 0.f;
-        if (tb + i < min(end, len)) {
-          load_vec(x + (tb + i) * KC, xn[i]);
-          load_vec(gy + (tb + i) * KC, gn[i]);
+        for (int e = 0; e < V; ++e) {
+          xn[i][e] = tb + i < there ? xn[i][e] : 0.f;
+          gn[i][e] = tb + i < there ? gn[i][e] : 0.f;
         }
       }
+      fetch(tb + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int t = tb + i;
@@ -339,8 +364,12 @@ __global__ __launch_bounds__(kSumSlices * kSumLanes) void conv_sum_kernel(const 
   }
 }
 
-// Chunks as long as leaves this many threads.
-constexpr long long kWantedThreads = 1 << 17;
+// Chunks as long as leaves this many columns in flight over all threads: short
+// ones read the tokens between them twice and write more partial sums, long ones
+// leave the chip idle (4 x 5000 tokens of 36 x 20 in vectors of four: 2^18 columns
+// forward 21 us, backward 44, 2^19 22 and 54; 4 x 2048 of 16 x 33 one by one: 2^18 10
+// and 22, 2^16 13 and 28).
+constexpr long long kWantedColumns = 1 << 18;
 
 ConvShape conv_shape(int64_t B, int64_t N, int K, int64_t C, int V) {
   ConvShape s;
@@ -349,7 +378,7 @@ ConvShape conv_shape(int64_t B, int64_t N, int K, int64_t C, int V) {
   while (s.width < 64 && s.width < s.cols) s.width *= 2;
   s.colblocks = (s.cols + s.width - 1) / s.width;
   s.chunk = 64;
-  while (s.chunk > 8 && B * ((N + s.chunk - 1) / s.chunk) * s.cols < kWantedThreads) s.chunk /= 2;
+  while (s.chunk > 8 && B * ((N + s.chunk - 1) / s.chunk) * s.cols * V < kWantedColumns) s.chunk /= 2;
   s.chunks = (int)((N + s.chunk - 1) / s.chunk);
   s.units = B * s.chunks;
   return s;
