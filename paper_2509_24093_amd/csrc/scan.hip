@@ -180,7 +180,7 @@ __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, Sc
     for (int i = 0; i < RUN; ++i) {
       const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
       const bool in = n + i < n1 && n + i < sh.chunks - 1;
-      add[i] = in ? p[ch * a.S * KC] : 0.f;
+      add[i] = in ? p[(long long)ch * a.S * KC] : 0.f;
       e[i] = in ? exp2_fast(A2 * d[(long long)ch * a.C]) : 1.f;
     }
   };
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, Sc
     for (int i = 0; i < RUN; ++i) {
       if (n + i < n1) {
         const int ch = reverse ? sh.chunks - 1 - (n + i) : n + i;
-        p[ch * a.S * KC] = h;
+        p[(long long)ch * a.S * KC] = h;
         h = fmaf(e[i], h, add[i]);
       }
     }

@@ -83,15 +83,15 @@ struct TokenRows {
   }
 };
 
-// Brings the rows of tokens t0 .. t2 - 1 into the caches near this block: where only
-// one or two blocks share them, a scalar load of every token would otherwise wait
-// for memory on its own (2 x 8192 tokens of 49 x 32, forward: 218 -> 209 us; 4 x 8192
-// of 2048, 8 blocks a chunk, 346 -> 353).  Returns a value for settle_rows, behind
-// the block's other first loads.
+// Brings the rows of tokens t0 .. t2 - 1, at most 64, into the caches near this
+// block: where only one or two blocks share them, a scalar load of every token
+// would otherwise wait for memory on its own (2 x 8192 tokens of 49 x 32, forward:
+// 218 -> 209 us; 4 x 8192 of 2048, 8 blocks a chunk, 346 -> 353).  Returns a value
+// for settle_rows, behind the block's other first loads.
 template <int SP>
 __device__ __forceinline__ float touch_rows(const float* rows, int t0, int t2) {
   constexpr int kLine = 32;  // floats of a cache line
-  const int n = (t2 - t0) * 2 * SP;
+  const int n = min(t2 - t0, 64) * 2 * SP;
   const float* p = rows + (long long)t0 * 2 * SP;
   float v = 0.f;
   for (int i = threadIdx.x * kLine; i < n; i += blockDim.x * kLine) v += p[i];
