@@ -22,6 +22,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "seq_common.h"
 
@@ -31,12 +32,20 @@ namespace {
 
 using namespace seqdev;
 
+// n / d of n d < 2^32 by one multiply-high (magic = floor((2^32 - 1) / d) + 1; d >= 2;
+// d = 1 has no such magic and is n itself).
+__device__ __forceinline__ int divide(int n, uint32_t magic) {
+  return magic ? (int)__umulhi((uint32_t)n, magic) : n;
+}
+uint32_t magic_of(int d) { return d > 1 ? 0xFFFFFFFFu / (uint32_t)d + 1 : 0; }
+
 // Launch shape of the row form.
 struct RowShape {
   int lanes;    // per row (a power of two)
   int threads;  // per block
   int passes;   // rows per thread: a multiple of kPassStep
   int tokens;   // per block
+  uint32_t magic = 0;  // of K
 };
 
 __device__ __forceinline__ int degree_of(int comp) { return (int)__builtin_sqrtf((float)comp + 0.5f); }
@@ -94,7 +103,7 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
         if (j % kLanes == 0) a.scales[row * nb + c / kPackBlock] = (uint8_t)scale;
       }
     }
-    const int tok = r / a.K;
+    const int tok = divide(r, sh.magic);
     if (r - tok * a.K == 0) {  // the invariants' row
       float s = 0.f;
 #pragma unroll
@@ -123,7 +132,7 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
   for (int i = 0; i < R; ++i) {
     const int r = i * per + rg;
     if (!col || r >= rows) continue;
-    const int tok = r / a.K, comp = r - tok * a.K, l = degree_of(comp);
+    const int tok = divide(r, sh.magic), comp = r - tok * a.K, l = degree_of(comp);
     const float m = rs[tok * degs + l];
     float w[V];
 #pragma unroll
@@ -178,7 +187,7 @@ __device__ __forceinline__ void block_sum2(float& u, float& v, float* lds, int t
 // Wide rows: block (token, degree), the degree's (2l+1) C values in registers.
 // CODES only where C is a multiple of 32 (a scale's lanes are then neighbours).
 template <class T, int V, int R, bool CODES, int MAXT>
-__global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a) {
+__global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a, uint32_t magic) {
   __shared__ float lds[16];
   const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
   const int n = (2 * l + 1) * a.C;
@@ -226,7 +235,7 @@ __global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a) {
   for (int i = 0; i < R; ++i) {
     const int e0 = (i * threads + tid) * V;
     if (e0 >= n) continue;
-    const int c = e0 % a.C;
+    const int c = l == 0 ? e0 : e0 - divide(e0, magic) * a.C;
     float w[V], b[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) w[e] = 1.f, b[e] = 0.f;
@@ -269,7 +278,7 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = i * per + rg;
-    tok[i] = r / a.K;
+    tok[i] = divide(r, sh.magic);
     comp[i] = r - tok[i] * a.K;
     deg[i] = degree_of(comp[i]);
 #pragma unroll
@@ -378,7 +387,7 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
 // Partial sums: part[slot][K components, then gb][C].
 template <class T, int V, int R, bool CODES, int MAXT>
 __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 3 : 4) : 2) void norm_wide_bwd_kernel(
-    NormBwdArgs a) {
+    NormBwdArgs a, uint32_t magic) {
   constexpr bool kAhead = MAXT <= 256 && V == 8;
   __shared__ float lds[32];
   const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
@@ -402,7 +411,7 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
       const int e0 = (i * threads + tid) * V;
       if (e0 < n) {
         if (CODES) {
-          const int m = e0 / a.C;
+          const int m = l == 0 ? 0 : divide(e0, magic);
           cr[i].load(a.codes + row0 * a.C + e0);
           sc[i] = a.scales[(row0 + m) * nb + (e0 - m * a.C) / kPackBlock];
         } else {
@@ -432,7 +441,7 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
         gr[i].widen_to(g[i]);
       } else {
         const long long row0 = t * a.K + l * l;
-        const int m = e0 / a.C;
+        const int m = l == 0 ? 0 : divide(e0, magic);
         load_input<T, V, CODES>(a, row0 + m, e0 - m * a.C, nb, h[i]);
         load_vec(static_cast<const T*>(a.gy) + row0 * a.C + e0, g[i]);
       }
@@ -444,7 +453,8 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
       float w[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) w[e] = 1.f;
-      if (a.weight && e0 < n) load_vec(a.weight + (long long)l * a.C + e0 % a.C, w);
+      const int c = l == 0 ? e0 : e0 - divide(e0, magic) * a.C;
+      if (a.weight && e0 < n) load_vec(a.weight + (long long)l * a.C + c, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         h[i][e] = (h[i][e] - m0) * r0;
@@ -526,7 +536,7 @@ constexpr int kPassStep = 2;
 // other at two barriers a tile, 256 x 4 against 512 x 4: 773, 784, with the 8-bit
 // input 778, 899.
 RowShape row_shape(int C, int K, int V, int max_passes, int max_threads, int max_values, double gain) {
-  RowShape best{1, 0, 0, 0};
+  RowShape best{1, 0, 0, 0, magic_of(K)};
   const int vecs = (C + V - 1) / V;
   if (vecs > 64) return best;
   while (best.lanes < vecs) best.lanes *= 2;
@@ -595,7 +605,7 @@ hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
   if (a.tokens > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)a.tokens, a.L + 1);
   const auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, magic_of(a.C));
     return hipGetLastError();
   };
   if (a.codes && a.C % kPackBlock == 0)
@@ -630,7 +640,7 @@ hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
   const int blocks = wide_bwd_blocks(a.tokens, a.L, threads);
   const dim3 grid(blocks, a.L + 1);
   const auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, magic_of(a.C));
     return hipGetLastError();
   };
   const hipError_t e =
@@ -653,6 +663,14 @@ constexpr int bwd_passes(int V) { return V >= 4 ? kBwdValues / V : 4; }
 // a block's gw is staged in at most 64 KiB of LDS
 RowShape bwd_row_shape(int C, int K, int V) { return row_shape(C, K, V, bwd_passes(V), kBwdRowThreads, 16384, 1.0); }
 
+// f of the number of vectors per thread, a power of two up to MAX
+template <int R, int MAX, class F>
+hipError_t by_vecs(int vecs, F f) {
+  if (vecs == R) return f(std::integral_constant<int, R>());
+  if constexpr (R < MAX) return by_vecs<2 * R, MAX>(vecs, f);
+  return hipErrorInvalidValue;
+}
+
 template <class T, int V>
 hipError_t norm_any(const NormArgs& a, hipStream_t s) {
   const RowShape sh = row_shape(a.C, a.K, V, kFwdPasses, 1024, 1024 * 32, 0.1);
@@ -665,12 +683,7 @@ hipError_t norm_any(const NormArgs& a, hipStream_t s) {
   }
   constexpr int kMax = fwd_values(V) / V;
   const WideShape w = wide_shape((2 * a.L + 1) * a.C, V, kMax);
-  if (w.vecs <= kMax) {
-    if (w.vecs <= 1) return norm_wide<T, V, 1>(a, w.threads, s);
-    if (w.vecs <= 4) return norm_wide<T, V, 4>(a, w.threads, s);
-    return norm_wide<T, V, kMax>(a, w.threads, s);
-  }
-  return hipErrorInvalidValue;
+  return by_vecs<1, kMax>(w.vecs, [&](auto r) { return norm_wide<T, V, decltype(r)::value>(a, w.threads, s); });
 }
 
 template <class T, int V>
@@ -685,12 +698,7 @@ hipError_t norm_bwd_any(const NormBwdArgs& a, hipStream_t s) {
   }
   constexpr int kMax = kBwdValues / V;
   const WideShape w = wide_shape((2 * a.L + 1) * a.C, V, kMax);
-  if (w.vecs <= kMax) {
-    if (w.vecs <= 1) return norm_wide_bwd<T, V, 1>(a, w.threads, s);
-    if (w.vecs <= 2) return norm_wide_bwd<T, V, 2>(a, w.threads, s);
-    return norm_wide_bwd<T, V, kMax>(a, w.threads, s);
-  }
-  return hipErrorInvalidValue;
+  return by_vecs<1, kMax>(w.vecs, [&](auto r) { return norm_wide_bwd<T, V, decltype(r)::value>(a, w.threads, s); });
 }
 
 }  // namespace
