@@ -69,13 +69,14 @@ __device__ __forceinline__ void degree_sums(const float* rowsum, float* out, int
 }
 
 // Dynamic LDS: a row's sums, then a degree's.
-template <class T, int V, int R, bool CODES>
+template <class T, int V, int R, bool CODES, bool TAIL>
 __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
   extern __shared__ float lds[];
   const int tid = threadIdx.x, per = sh.threads / sh.lanes;  // rows per pass
   const int j = tid & (sh.lanes - 1), rg = tid / sh.lanes;
   const int c = j * V;
-  const bool col = c < a.C;
+  const int left = a.C - c;  // channels from c on
+  const bool col = left > 0;
   const long long t0 = (long long)blockIdx.x * sh.tokens;
   const int toks = (int)min((long long)sh.tokens, a.tokens - t0);
   const int rows = toks * a.K;
@@ -88,7 +89,7 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
     const int r = i * per + rg;
 #pragma unroll
     for (int e = 0; e < V; ++e) v[i][e] = 0.f;
-    if (col && r < rows) load_vec(x + (long long)r * a.C + c, v[i]);
+    if (col && r < rows) load_part<TAIL>(x + (long long)r * a.C + c, left, v[i]);
   }
   const int nb = (a.C + kPackBlock - 1) / kPackBlock;
 #pragma unroll
@@ -99,7 +100,7 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
       const uint32_t scale = pack_scale(group_max_bits(max_bits(v[i]), min(kLanes, sh.lanes)));
       if (col && r < rows) {
         const long long row = t0 * a.K + r;
-        store_codes(a.codes + row * a.C + c, v[i], scale);
+        store_codes<TAIL>(a.codes + row * a.C + c, left, v[i], scale);
         if (j % kLanes == 0) a.scales[row * nb + c / kPackBlock] = (uint8_t)scale;
       }
     }
@@ -110,7 +111,7 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
       for (int e = 0; e < V; ++e) s += v[i][e];
       const float mean = group_sum(s, sh.lanes) / (float)a.C;
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[i][e] = col ? v[i][e] - mean : 0.f;
+      for (int e = 0; e < V; ++e) v[i][e] = e < left ? v[i][e] - mean : 0.f;
       if (a.mean && j == 0 && r < rows) a.mean[t0 + tok] = mean;
     }
     float q = 0.f;
@@ -138,7 +139,7 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
 #pragma unroll
     for (int e = 0; e < V; ++e) w[e] = m;
     if (a.weight) {
-      load_vec(a.weight + l * a.C + c, w);
+      load_part<TAIL>(a.weight + l * a.C + c, left, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) w[e] *= m;
     }
@@ -146,11 +147,11 @@ __global__ void norm_rows_kernel(NormArgs a, RowShape sh) {
     for (int e = 0; e < V; ++e) v[i][e] *= w[e];
     if (comp == 0 && a.bias) {
       float b[V];
-      load_vec(a.bias + c, b);
+      load_part<TAIL>(a.bias + c, left, b);
 #pragma unroll
       for (int e = 0; e < V; ++e) v[i][e] += b[e];
     }
-    store_vec(y + (long long)r * a.C + c, v[i]);
+    store_part<TAIL>(y + (long long)r * a.C + c, left, v[i]);
   }
 }
 
@@ -185,8 +186,9 @@ __device__ __forceinline__ void block_sum2(float& u, float& v, float* lds, int t
 }
 
 // Wide rows: block (token, degree), the degree's (2l+1) C values in registers.
-// CODES only where C is a multiple of 32 (a scale's lanes are then neighbours).
-template <class T, int V, int R, bool CODES, int MAXT>
+// CODES only where a scale's lanes are neighbours: C a multiple of 32, or L = 0.
+// TAIL: L = 0 and C no multiple of V.
+template <class T, int V, int R, bool CODES, int MAXT, bool TAIL>
 __global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a, uint32_t magic) {
   __shared__ float lds[16];
   const int tid = threadIdx.x, threads = blockDim.x, l = blockIdx.y;
@@ -195,19 +197,21 @@ __global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a, uint32_t ma
   const long long base = (t * a.K + l * l) * a.C;
   const T* x = static_cast<const T*>(a.x) + base;
   float v[R][V];
+  const int nb = (a.C + kPackBlock - 1) / kPackBlock;
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int e0 = (i * threads + tid) * V;
 #pragma unroll
     for (int e = 0; e < V; ++e) v[i][e] = 0.f;
-    if (e0 < n) load_vec(x + e0, v[i]);
+    if (e0 < n) load_part<TAIL>(x + e0, n - e0, v[i]);
     if (CODES) {
       constexpr int kLanes = kPackBlock / V;
       const uint32_t scale = pack_scale(group_max_bits(max_bits(v[i]), kLanes));
       if (e0 < n) {
-        store_codes(a.codes + base + e0, v[i], scale);
-        if (tid % kLanes == 0) a.scales[(base + e0) / kPackBlock] = (uint8_t)scale;
+        store_codes<TAIL>(a.codes + base + e0, n - e0, v[i], scale);
+        const int m = l == 0 ? 0 : divide(e0, magic);
+        if (tid % kLanes == 0) a.scales[(t * a.K + l * l + m) * nb + (e0 - m * a.C) / kPackBlock] = (uint8_t)scale;
       }
     }
 #pragma unroll
@@ -217,9 +221,9 @@ __global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a, uint32_t ma
     const float mean = block_sum(s, lds, threads) / (float)a.C;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const bool here = (i * threads + tid) * V < n;
+      const int left = n - (i * threads + tid) * V;
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[i][e] = here ? v[i][e] - mean : 0.f;
+      for (int e = 0; e < V; ++e) v[i][e] = (TAIL ? e < left : left > 0) ? v[i][e] - mean : 0.f;
     }
     if (a.mean && tid == 0) a.mean[t] = mean;
   }
@@ -239,23 +243,23 @@ __global__ __launch_bounds__(MAXT) void norm_wide_kernel(NormArgs a, uint32_t ma
     float w[V], b[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) w[e] = 1.f, b[e] = 0.f;
-    if (a.weight) load_vec(a.weight + (long long)l * a.C + c, w);
-    if (l == 0 && a.bias) load_vec(a.bias + c, b);
+    if (a.weight) load_part<TAIL>(a.weight + (long long)l * a.C + c, n - e0, w);
+    if (l == 0 && a.bias) load_part<TAIL>(a.bias + c, n - e0, b);
 #pragma unroll
     for (int e = 0; e < V; ++e) v[i][e] = fmaf(v[i][e] * r, w[e], b[e]);
-    store_vec(y + e0, v[i]);
+    store_part<TAIL>(y + e0, n - e0, v[i]);
   }
 }
 
 // ---- backward --------------------------------------------------------------------
 
 // Input values of a row vector: x itself, or its 8-bit checkpoint.
-template <class T, int V, bool CODES>
+template <class T, int V, bool CODES, bool TAIL>
 __device__ __forceinline__ void load_input(const NormBwdArgs& a, long long row, int c, int nb, float (&v)[V]) {
   if (CODES)
-    load_codes(a.codes + row * a.C + c, a.scales[row * nb + c / kPackBlock], v);
+    load_codes<TAIL>(a.codes + row * a.C + c, a.C - c, a.scales[row * nb + c / kPackBlock], v);
   else
-    load_vec(static_cast<const T*>(a.x) + row * a.C + c, v);
+    load_part<TAIL>(static_cast<const T*>(a.x) + row * a.C + c, a.C - c, v);
 }
 
 // Block b takes tiles b, b + gridDim.x, ... of sh.tokens tokens.  Dynamic LDS:
@@ -263,13 +267,14 @@ __device__ __forceinline__ void load_input(const NormBwdArgs& a, long long row, 
 // Partial sums of block b: part[b][L+1 degrees, then gb][C].
 constexpr int kBwdRowThreads = 512;
 
-template <class T, int V, int R, bool CODES>
+template <class T, int V, int R, bool CODES, bool TAIL>
 __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdArgs a, RowShape sh, long long tiles) {
   extern __shared__ float lds[];
   const int tid = threadIdx.x, per = sh.threads / sh.lanes;
   const int j = tid & (sh.lanes - 1), rg = tid / sh.lanes;
   const int c = j * V;
-  const bool col = c < a.C;
+  const int left = a.C - c;  // channels from c on
+  const bool col = left > 0;
   const int nb = (a.C + kPackBlock - 1) / kPackBlock, degs = a.L + 1;
   float* rowsum = lds;
   float* ds = lds + sh.tokens * a.K;  // mean(g h) of every degree
@@ -298,8 +303,8 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
       m0[i] = r0[i] = 0.f;
       if (col && tok[i] < toks) {
         const int r = i * per + rg;
-        load_input<T, V, CODES>(a, t0 * a.K + r, c, nb, h[i]);
-        load_vec(gy + (long long)r * a.C + c, g[i]);
+        load_input<T, V, CODES, TAIL>(a, t0 * a.K + r, c, nb, h[i]);
+        load_part<TAIL>(gy + (long long)r * a.C + c, left, g[i]);
         r0[i] = a.rstd[(t0 + tok[i]) * degs + deg[i]];
         if (comp[i] == 0) m0[i] = a.mean[t0 + tok[i]];
       }
@@ -309,7 +314,7 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
       float w[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) w[e] = 1.f;
-      if (a.weight && col) load_vec(a.weight + deg[i] * a.C + c, w);
+      if (a.weight && col) load_part<TAIL>(a.weight + deg[i] * a.C + c, left, w);
       float q = 0.f, s = 0.f;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
@@ -341,7 +346,7 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
         float o[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] = r0[i] * fmaf(-h[i][e], d, g[i][e]);
-        store_vec(gx + (long long)(i * per + rg) * a.C + c, o);
+        store_part<TAIL>(gx + (long long)(i * per + rg) * a.C + c, left, o);
       }
     }
     // the next tile writes rowsum only, which every thread has read before the
@@ -355,7 +360,8 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
   for (int i = 0; i < R; ++i)
     if (col) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) lds[(i * per + rg) * a.C + c + e] = gw[i][e];
+      for (int e = 0; e < V; ++e)
+        if (!TAIL || e < left) lds[(i * per + rg) * a.C + c + e] = gw[i][e];
     }
   __syncthreads();
   for (int o = tid; o < degs * a.C; o += sh.threads) {
@@ -368,7 +374,8 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
   __syncthreads();
   if (col) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) lds[rg * a.C + c + e] = gb[e];
+    for (int e = 0; e < V; ++e)
+      if (!TAIL || e < left) lds[rg * a.C + c + e] = gb[e];
   }
   __syncthreads();
   for (int ch = tid; ch < a.C; ch += sh.threads) {
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
 // 190; with 8-bit inputs three waves, 32768 of 1024 139 -> 107; fp32, 4 x 4096
 // tokens of L=2 C=512 with 32 registers ahead: 320 -> 392).
 // Partial sums: part[slot][K components, then gb][C].
-template <class T, int V, int R, bool CODES, int MAXT>
+template <class T, int V, int R, bool CODES, int MAXT, bool TAIL>
 __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 3 : 4) : 2) void norm_wide_bwd_kernel(
     NormBwdArgs a, uint32_t magic) {
   constexpr bool kAhead = MAXT <= 256 && V == 8;
@@ -412,12 +419,12 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
       if (e0 < n) {
         if (CODES) {
           const int m = l == 0 ? 0 : divide(e0, magic);
-          cr[i].load(a.codes + row0 * a.C + e0);
+          cr[i].template load_part<TAIL>(a.codes + row0 * a.C + e0, n - e0);
           sc[i] = a.scales[(row0 + m) * nb + (e0 - m * a.C) / kPackBlock];
         } else {
-          xr[i].load(static_cast<const T*>(a.x) + row0 * a.C + e0);
+          xr[i].template load_part<TAIL>(static_cast<const T*>(a.x) + row0 * a.C + e0, n - e0);
         }
-        gr[i].load(static_cast<const T*>(a.gy) + row0 * a.C + e0);
+        gr[i].template load_part<TAIL>(static_cast<const T*>(a.gy) + row0 * a.C + e0, n - e0);
       }
     }
   };
@@ -442,8 +449,8 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
       } else {
         const long long row0 = t * a.K + l * l;
         const int m = l == 0 ? 0 : divide(e0, magic);
-        load_input<T, V, CODES>(a, row0 + m, e0 - m * a.C, nb, h[i]);
-        load_vec(static_cast<const T*>(a.gy) + row0 * a.C + e0, g[i]);
+        load_input<T, V, CODES, TAIL>(a, row0 + m, e0 - m * a.C, nb, h[i]);
+        load_part<TAIL>(static_cast<const T*>(a.gy) + row0 * a.C + e0, n - e0, g[i]);
       }
     }
     if (kAhead && t + gridDim.x < a.tokens) fetch(t + gridDim.x);
@@ -454,7 +461,7 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
 #pragma unroll
       for (int e = 0; e < V; ++e) w[e] = 1.f;
       const int c = l == 0 ? e0 : e0 - divide(e0, magic) * a.C;
-      if (a.weight && e0 < n) load_vec(a.weight + (long long)l * a.C + c, w);
+      if (a.weight && e0 < n) load_part<TAIL>(a.weight + (long long)l * a.C + c, n - e0, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         h[i][e] = (h[i][e] - m0) * r0;
@@ -476,7 +483,7 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = r0 * fmaf(-h[i][e], d, g[i][e] - m1);
-      store_vec(gx + e0, o);
+      store_part<TAIL>(gx + e0, n - e0, o);
     }
   }
   if (!a.part) return;
@@ -485,8 +492,8 @@ __global__ __launch_bounds__(MAXT, MAXT > 256 || V == 4 ? 4 : V == 8 ? (CODES ? 
   for (int i = 0; i < R; ++i) {
     const int e0 = (i * threads + tid) * V;
     if (e0 >= n) continue;
-    store_vec(part + (long long)l * l * a.C + e0, gw[i]);
-    if (l == 0) store_vec(part + (long long)a.K * a.C + e0, gb[i]);
+    store_part<TAIL>(part + (long long)l * l * a.C + e0, n - e0, gw[i]);
+    if (l == 0) store_part<TAIL>(part + (long long)a.K * a.C + e0, n - e0, gb[i]);
   }
 }
 
@@ -587,20 +594,20 @@ int wide_bwd_blocks(long long tokens, int L, int threads) {
 
 size_t row_lds_floats(const RowShape& sh, int K, int L) { return (size_t)sh.tokens * (K + L + 1); }
 
-template <class T, int V, int R>
+template <class T, int V, bool TAIL, int R>
 hipError_t norm_rows(const NormArgs& a, const RowShape& sh, hipStream_t s) {
   const long long blocks = (a.tokens + sh.tokens - 1) / sh.tokens;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
   const size_t lds = row_lds_floats(sh, a.K, a.L) * sizeof(float);
   if (lds > 64 * 1024) return hipErrorInvalidValue;
   if (a.codes)
-    hipLaunchKernelGGL((norm_rows_kernel<T, V, R, true>), dim3((unsigned)blocks), dim3(sh.threads), lds, s, a, sh);
+    hipLaunchKernelGGL((norm_rows_kernel<T, V, R, true, TAIL>), dim3((unsigned)blocks), dim3(sh.threads), lds, s, a, sh);
   else
-    hipLaunchKernelGGL((norm_rows_kernel<T, V, R, false>), dim3((unsigned)blocks), dim3(sh.threads), lds, s, a, sh);
+    hipLaunchKernelGGL((norm_rows_kernel<T, V, R, false, TAIL>), dim3((unsigned)blocks), dim3(sh.threads), lds, s, a, sh);
   return hipGetLastError();
 }
 
-template <class T, int V, int R>
+template <class T, int V, bool TAIL, int R>
 hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
   if (a.tokens > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)a.tokens, a.L + 1);
@@ -608,16 +615,18 @@ hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, magic_of(a.C));
     return hipGetLastError();
   };
-  if (a.codes && a.C % kPackBlock == 0)
-    return threads <= 256 ? run(norm_wide_kernel<T, V, R, true, 256>) : run(norm_wide_kernel<T, V, R, true, 1024>);
+  if (a.codes && (a.C % kPackBlock == 0 || a.L == 0))
+    return threads <= 256 ? run(norm_wide_kernel<T, V, R, true, 256, TAIL>)
+                          : run(norm_wide_kernel<T, V, R, true, 1024, TAIL>);
   if (a.codes) {  // a scale's channels would straddle the lanes: a pass of its own
     const hipError_t e = launch_pack(a.type, a.x, a.codes, a.scales, a.tokens * a.K, a.C, s);
     if (e != hipSuccess) return e;
   }
-  return threads <= 256 ? run(norm_wide_kernel<T, V, R, false, 256>) : run(norm_wide_kernel<T, V, R, false, 1024>);
+  return threads <= 256 ? run(norm_wide_kernel<T, V, R, false, 256, TAIL>)
+                        : run(norm_wide_kernel<T, V, R, false, 1024, TAIL>);
 }
 
-template <class T, int V, int R>
+template <class T, int V, bool TAIL, int R>
 hipError_t norm_rows_bwd(const NormBwdArgs& a, const RowShape& sh, hipStream_t s) {
   const long long tiles = (a.tokens + sh.tokens - 1) / sh.tokens;
   const int blocks = row_bwd_blocks(a.tokens, sh);
@@ -625,9 +634,9 @@ hipError_t norm_rows_bwd(const NormBwdArgs& a, const RowShape& sh, hipStream_t s
   const size_t lds = std::max(row_lds_floats(sh, a.K, a.L), a.part ? (size_t)per * R * a.C : 0) * sizeof(float);
   if (lds > 64 * 1024) return hipErrorInvalidValue;
   if (a.codes)
-    hipLaunchKernelGGL((norm_rows_bwd_kernel<T, V, R, true>), dim3(blocks), dim3(sh.threads), lds, s, a, sh, tiles);
+    hipLaunchKernelGGL((norm_rows_bwd_kernel<T, V, R, true, TAIL>), dim3(blocks), dim3(sh.threads), lds, s, a, sh, tiles);
   else
-    hipLaunchKernelGGL((norm_rows_bwd_kernel<T, V, R, false>), dim3(blocks), dim3(sh.threads), lds, s, a, sh, tiles);
+    hipLaunchKernelGGL((norm_rows_bwd_kernel<T, V, R, false, TAIL>), dim3(blocks), dim3(sh.threads), lds, s, a, sh, tiles);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
   hipLaunchKernelGGL(norm_sum_kernel, dim3(((a.L + 2) * a.C + 63) / 64), dim3(64 * kSumSlices), 0, s, a.part, blocks,
@@ -635,7 +644,7 @@ hipError_t norm_rows_bwd(const NormBwdArgs& a, const RowShape& sh, hipStream_t s
   return hipGetLastError();
 }
 
-template <class T, int V, int R>
+template <class T, int V, bool TAIL, int R>
 hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
   const int blocks = wide_bwd_blocks(a.tokens, a.L, threads);
   const dim3 grid(blocks, a.L + 1);
@@ -644,10 +653,10 @@ hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
     return hipGetLastError();
   };
   const hipError_t e =
-      a.codes ? (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, true, 256>)
-                                : run(norm_wide_bwd_kernel<T, V, R, true, 1024>))
-              : (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, false, 256>)
-                                : run(norm_wide_bwd_kernel<T, V, R, false, 1024>));
+      a.codes ? (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, true, 256, TAIL>)
+                                : run(norm_wide_bwd_kernel<T, V, R, true, 1024, TAIL>))
+              : (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, false, 256, TAIL>)
+                                : run(norm_wide_bwd_kernel<T, V, R, false, 1024, TAIL>));
   if (e != hipSuccess || !a.part) return e;
   hipLaunchKernelGGL(norm_sum_kernel, dim3(((a.L + 2) * a.C + 63) / 64), dim3(64 * kSumSlices), 0, s, a.part, blocks,
                      a.L, a.K, a.C, 0, a.gw, a.gb);
@@ -660,8 +669,6 @@ constexpr int kFwdPasses = 4;
 constexpr int fwd_values(int V) { return V >= 4 ? 32 : 16; }
 constexpr int kBwdValues = 16;
 constexpr int bwd_passes(int V) { return V >= 4 ? kBwdValues / V : 4; }
-// a block's gw is staged in at most 64 KiB of LDS
-RowShape bwd_row_shape(int C, int K, int V) { return row_shape(C, K, V, bwd_passes(V), kBwdRowThreads, 16384, 1.0); }
 
 // f of the number of vectors per thread, a power of two up to MAX
 template <int R, int MAX, class F>
@@ -671,34 +678,65 @@ hipError_t by_vecs(int vecs, F f) {
   return hipErrorInvalidValue;
 }
 
-template <class T, int V>
-hipError_t norm_any(const NormArgs& a, hipStream_t s) {
-  const RowShape sh = row_shape(a.C, a.K, V, kFwdPasses, 1024, 1024 * 32, 0.1);
-  if (sh.tokens) {
-    switch (sh.passes) {
-      case 2: return norm_rows<T, V, 2>(a, sh, s);
-      case 4: return norm_rows<T, V, 4>(a, sh, s);
-      default: return hipErrorInvalidValue;
-    }
+// The kernels of a call.  Vectors of at least four elements that divide a row where
+// there are such; else (two channels in three are odd or twice odd) full ones, the
+// last of a row in part, from rows that start anywhere: element by element 13 x 2018
+// rows of 3377 bf16 channels took 805 us with the 8-bit input, 396 this way.  The
+// wide form's degrees above 0 wrap from row to row, where only dividing vectors do.
+struct Form {
+  int v = 0;
+  bool tail = false;
+  RowShape row{};
+  WideShape wide{};  // where row.tokens == 0
+};
+Form norm_form(int type, int C, int L, bool backward) {
+  const int K = (L + 1) * (L + 1), exact = seq_vec(type, C), full = type == SEQ_BF16 ? 8 : 4;
+  Form f;
+  f.tail = exact < 4;
+  f.v = f.tail ? full : exact;
+  f.row = backward ? row_shape(C, K, f.v, bwd_passes(f.v), kBwdRowThreads, 16384, 1.0)  // 64 KiB of gw in LDS
+                   : row_shape(C, K, f.v, kFwdPasses, 1024, 1024 * 32, 0.1);
+  if (f.row.tokens) return f;
+  if (f.tail && L > 0) {
+    f.tail = false;
+    f.v = exact;
   }
-  constexpr int kMax = fwd_values(V) / V;
-  const WideShape w = wide_shape((2 * a.L + 1) * a.C, V, kMax);
-  return by_vecs<1, kMax>(w.vecs, [&](auto r) { return norm_wide<T, V, decltype(r)::value>(a, w.threads, s); });
+  f.wide = wide_shape((2 * L + 1) * C, f.v, (backward ? kBwdValues : fwd_values(f.v)) / f.v);
+  return f;
 }
 
-template <class T, int V>
-hipError_t norm_bwd_any(const NormBwdArgs& a, hipStream_t s) {
-  const RowShape sh = bwd_row_shape(a.C, a.K, V);
-  if (sh.tokens) {
-    switch (sh.passes) {
-      case 2: return norm_rows_bwd<T, V, 2>(a, sh, s);
-      case 4: return norm_rows_bwd<T, V, V == 8 ? 2 : 4>(a, sh, s);
-      default: return hipErrorInvalidValue;
-    }
+template <class T, int V, bool TAIL>
+hipError_t norm_any(const NormArgs& a, const Form& f, hipStream_t s) {
+  if constexpr (V >= 4) {
+    if (f.row.tokens) return f.row.passes == 2 ? norm_rows<T, V, TAIL, 2>(a, f.row, s) : norm_rows<T, V, TAIL, 4>(a, f.row, s);
   }
-  constexpr int kMax = kBwdValues / V;
-  const WideShape w = wide_shape((2 * a.L + 1) * a.C, V, kMax);
-  return by_vecs<1, kMax>(w.vecs, [&](auto r) { return norm_wide_bwd<T, V, decltype(r)::value>(a, w.threads, s); });
+  return by_vecs<1, fwd_values(V) / V>(
+      f.wide.vecs, [&](auto r) { return norm_wide<T, V, TAIL, decltype(r)::value>(a, f.wide.threads, s); });
+}
+
+template <class T, int V, bool TAIL>
+hipError_t norm_any(const NormBwdArgs& a, const Form& f, hipStream_t s) {
+  if constexpr (V >= 4) {
+    if (f.row.tokens)
+      return f.row.passes == 2 ? norm_rows_bwd<T, V, TAIL, 2>(a, f.row, s)
+                               : norm_rows_bwd<T, V, TAIL, bwd_passes(V)>(a, f.row, s);
+  }
+  return by_vecs<1, kBwdValues / V>(
+      f.wide.vecs, [&](auto r) { return norm_wide_bwd<T, V, TAIL, decltype(r)::value>(a, f.wide.threads, s); });
+}
+
+template <class T, class Args>
+hipError_t norm_typed(const Args& a, const Form& f, hipStream_t s) {
+  constexpr int kFull = 16 / (int)sizeof(T);
+  if (f.tail) return norm_any<T, kFull, true>(a, f, s);
+  if constexpr (kFull == 8) {
+    if (f.v == 8) return norm_any<T, 8, false>(a, f, s);
+  }
+  switch (f.v) {
+    case 4: return norm_any<T, 4, false>(a, f, s);
+    case 2: return norm_any<T, 2, false>(a, f, s);
+    default: return norm_any<T, 1, false>(a, f, s);
+  }
 }
 
 }  // namespace
@@ -707,46 +745,21 @@ size_t norm_bwd_part_bytes(long long tokens, int L, int C) {
   const int K = (L + 1) * (L + 1);
   size_t rows = 0;
   for (int type : {SEQ_F32, SEQ_BF16}) {
-    const RowShape sh = bwd_row_shape(C, K, seq_vec(type, C));
-    const int v = seq_vec(type, C), threads = wide_shape((2 * L + 1) * C, v, kBwdValues / v).threads;
-    rows = std::max(rows, sh.tokens ? (size_t)row_bwd_blocks(tokens, sh) * (L + 2)
-                                    : (size_t)wide_bwd_blocks(tokens, L, threads) * (K + 1));
+    const Form f = norm_form(type, C, L, true);
+    rows = std::max(rows, f.row.tokens ? (size_t)row_bwd_blocks(tokens, f.row) * (L + 2)
+                                       : (size_t)wide_bwd_blocks(tokens, L, f.wide.threads) * (K + 1));
   }
   return rows * C * sizeof(float);
 }
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
-  const int v = seq_vec(a.type, a.C);
-  if (a.type == SEQ_BF16) {
-    switch (v) {
-      case 8: return norm_any<bf16, 8>(a, s);
-      case 4: return norm_any<bf16, 4>(a, s);
-      case 2: return norm_any<bf16, 2>(a, s);
-      default: return norm_any<bf16, 1>(a, s);
-    }
-  }
-  switch (v) {
-    case 4: return norm_any<float, 4>(a, s);
-    case 2: return norm_any<float, 2>(a, s);
-    default: return norm_any<float, 1>(a, s);
-  }
+  const Form f = norm_form(a.type, a.C, a.L, false);
+  return a.type == SEQ_BF16 ? norm_typed<bf16>(a, f, s) : norm_typed<float>(a, f, s);
 }
 
 hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t s) {
-  const int v = seq_vec(a.type, a.C);
-  if (a.type == SEQ_BF16) {
-    switch (v) {
-      case 8: return norm_bwd_any<bf16, 8>(a, s);
-      case 4: return norm_bwd_any<bf16, 4>(a, s);
-      case 2: return norm_bwd_any<bf16, 2>(a, s);
-      default: return norm_bwd_any<bf16, 1>(a, s);
-    }
-  }
-  switch (v) {
-    case 4: return norm_bwd_any<float, 4>(a, s);
-    case 2: return norm_bwd_any<float, 2>(a, s);
-    default: return norm_bwd_any<float, 1>(a, s);
-  }
+  const Form f = norm_form(a.type, a.C, a.L, true);
+  return a.type == SEQ_BF16 ? norm_typed<bf16>(a, f, s) : norm_typed<float>(a, f, s);
 }
 
 }  // namespace cgconv

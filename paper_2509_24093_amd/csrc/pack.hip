@@ -17,9 +17,10 @@ using namespace seqdev;
 constexpr int kThreads = 256;
 constexpr long long kPackNtBytes = 256LL << 20;
 
-// One group of V lanes-worth of elements per thread: the 32 / V lanes of a
-// scale's channels are neighbours, and a row's last group leaves lanes idle.
-template <class T, int V, bool PACK, bool NT>
+// A thread takes 16 bytes of x: the 32 / V lanes of a scale's channels are
+// neighbours, and a row's last group leaves lanes idle.  TAIL: C is no multiple of
+// V, so rows start anywhere and end inside a vector.
+template <class T, int V, bool PACK, bool NT, bool TAIL>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const T* __restrict__ x, const int8_t* __restrict__ codes_in,
                                                         const uint8_t* __restrict__ scales_in, T* __restrict__ out,
                                                         int8_t* __restrict__ codes, uint8_t* __restrict__ scales,
@@ -31,19 +32,20 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const T* __restrict__ x,
   const int j = (int)(thread % kLanes);
   const long long row = g / nb;
   const int c = (int)(g - row * nb) * kPackBlock + j * V;
-  const bool here = c < C;
+  const int n = C - c;
+  const bool here = n > 0;
   const long long at = row * C + c;
   float v[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = 0.f;
   if (PACK) {
-    if (here) load_vec<NT>(x + at, v);
+    if (here) load_part<TAIL, NT>(x + at, n, v);
     const uint32_t scale = pack_scale(group_max_bits(max_bits(v), kLanes));
-    if (here) store_codes(codes + at, v, scale);
+    if (here) store_codes<TAIL>(codes + at, n, v, scale);
     if (j == 0) scales[g] = (uint8_t)scale;
   } else if (here) {
-    load_codes(codes_in + at, scales_in[g], v);
-    store_vec<NT>(out + at, v);
+    load_codes<TAIL>(codes_in + at, n, scales_in[g], v);
+    store_part<TAIL, NT>(out + at, n, v);
   }
 }
 
@@ -58,27 +60,16 @@ hipError_t launch(const void* x, int8_t* codes, uint8_t* scales, void* out, long
                        static_cast<T*>(out), codes, scales, groups, C, nb);
     return hipGetLastError();
   };
-  return rows * C * (long long)sizeof(T) > kPackNtBytes ? run(pack_kernel<T, V, PACK, true>)
-                                                        : run(pack_kernel<T, V, PACK, false>);
+  const bool nt = rows * C * (long long)sizeof(T) > kPackNtBytes;
+  if (C % V) return nt ? run(pack_kernel<T, V, PACK, true, true>) : run(pack_kernel<T, V, PACK, false, true>);
+  return nt ? run(pack_kernel<T, V, PACK, true, false>) : run(pack_kernel<T, V, PACK, false, false>);
 }
 
 template <bool PACK>
 hipError_t launch_any(int type, const void* x, int8_t* codes, uint8_t* scales, void* out, long long rows, int C,
                       hipStream_t s) {
-  const int v = seq_vec(type, C);
-  if (type == SEQ_BF16) {
-    switch (v) {
-      case 8: return launch<bf16, 8, PACK>(x, codes, scales, out, rows, C, s);
-      case 4: return launch<bf16, 4, PACK>(x, codes, scales, out, rows, C, s);
-      case 2: return launch<bf16, 2, PACK>(x, codes, scales, out, rows, C, s);
-      default: return launch<bf16, 1, PACK>(x, codes, scales, out, rows, C, s);
-    }
-  }
-  switch (v) {
-    case 4: return launch<float, 4, PACK>(x, codes, scales, out, rows, C, s);
-    case 2: return launch<float, 2, PACK>(x, codes, scales, out, rows, C, s);
-    default: return launch<float, 1, PACK>(x, codes, scales, out, rows, C, s);
-  }
+  return type == SEQ_BF16 ? launch<bf16, 8, PACK>(x, codes, scales, out, rows, C, s)
+                          : launch<float, 4, PACK>(x, codes, scales, out, rows, C, s);
 }
 
 }  // namespace

@@ -30,38 +30,66 @@ __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(bf16 v) { return (float)v; }
 __device__ __forceinline__ float widen(int8_t v) { return (float)v; }
 
-// V consecutive elements (a power of two; the address a multiple of their size,
-// or of 16 where they take 32 bytes), in accesses of at most 16 bytes.  NT:
+// Words of V elements at an address that is a multiple of one element only (the
+// hardware's global accesses take any address).
+template <class T, int V>
+struct Words {
+  static constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16, kWords = kBytes / kWord;
+  typedef typename Word<kWord>::type W;
+  typedef W Unaligned __attribute__((aligned(alignof(T))));
+};
+
+// V consecutive elements (a power of two), in accesses of at most 16 bytes.  NT:
 // nontemporal, for what nobody reads again soon.
 template <bool NT = false, class T, int V>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[V]) {
-  constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16;
-  typedef typename Word<kWord>::type W;
+  typedef Words<T, V> S;
   T t[V];
 #pragma unroll
-  for (int i = 0; i < kBytes / kWord; ++i) {
-    const W* q = reinterpret_cast<const W*>(p) + i;
-    const W w = NT ? __builtin_nontemporal_load(q) : *q;
-    __builtin_memcpy(t + i * kWord / (int)sizeof(T), &w, sizeof w);
+  for (int i = 0; i < S::kWords; ++i) {
+    const typename S::Unaligned* q = reinterpret_cast<const typename S::Unaligned*>(p) + i;
+    const typename S::W w = NT ? __builtin_nontemporal_load(q) : *q;
+    __builtin_memcpy(t + i * S::kWord / (int)sizeof(T), &w, sizeof w);
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = widen(t[i]);
+}
+
+// The first n of V elements, zeros behind them (TAIL; else all V).
+template <bool TAIL, bool NT = false, class T, int V>
+__device__ __forceinline__ void load_part(const T* p, int n, float (&v)[V]) {
+  if (!TAIL || n >= V) {
+    load_vec<NT>(p, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = i < n ? widen(p[i]) : 0.f;
 }
 
 // V elements as they are stored, to be widened later: loads kept in flight take
 // the registers of the storage type only.
 template <class T, int V>
 struct Raw {
-  static constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16, kWords = kBytes / kWord;
-  typedef typename Word<kWord>::type W;
-  W w[kWords];
+  typedef Words<T, V> S;
+  typename S::W w[S::kWords];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const W*>(p)[i];
+    for (int i = 0; i < S::kWords; ++i) w[i] = reinterpret_cast<const typename S::Unaligned*>(p)[i];
+  }
+  template <bool TAIL>
+  __device__ __forceinline__ void load_part(const T* p, int n) {
+    if (!TAIL || n >= V) {
+      load(p);
+      return;
+    }
+    T t[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = i < n ? p[i] : (T)0;
+    __builtin_memcpy(w, t, S::kBytes);
   }
   __device__ __forceinline__ void widen_to(float (&v)[V]) const {
     T t[V];
-    __builtin_memcpy(t, w, kBytes);
+    __builtin_memcpy(t, w, S::kBytes);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = widen(t[i]);
   }
@@ -70,21 +98,31 @@ struct Raw {
 // Rounds to T to nearest, ties to even (nothing to round for float).
 template <bool NT = false, class T, int V>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[V]) {
-  constexpr int kBytes = V * (int)sizeof(T), kWord = kBytes < 16 ? kBytes : 16;
-  typedef typename Word<kWord>::type W;
+  typedef Words<T, V> S;
   T t[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) t[i] = (T)v[i];
 #pragma unroll
-  for (int i = 0; i < kBytes / kWord; ++i) {
-    W w;
-    __builtin_memcpy(&w, t + i * kWord / (int)sizeof(T), sizeof w);
-    W* q = reinterpret_cast<W*>(p) + i;
+  for (int i = 0; i < S::kWords; ++i) {
+    typename S::W w;
+    __builtin_memcpy(&w, t + i * S::kWord / (int)sizeof(T), sizeof w);
+    typename S::Unaligned* q = reinterpret_cast<typename S::Unaligned*>(p) + i;
     if (NT)
       __builtin_nontemporal_store(w, q);
     else
       *q = w;
   }
+}
+
+template <bool TAIL, bool NT = false, class T, int V>
+__device__ __forceinline__ void store_part(T* p, int n, const float (&v)[V]) {
+  if (!TAIL || n >= V) {
+    store_vec<NT>(p, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < n) p[i] = (T)v[i];
 }
 
 template <int CTRL>
@@ -155,17 +193,22 @@ __device__ __forceinline__ uint32_t max_bits(const float (&v)[V]) {
   return m;
 }
 
-// Codes of V values under the scale byte, as V bytes (zeros under byte 255).
-template <int V>
-__device__ __forceinline__ void store_codes(int8_t* p, const float (&v)[V], uint32_t scale) {
+// Codes of the first n of V values under the scale byte (zeros under byte 255).
+template <bool TAIL, int V>
+__device__ __forceinline__ void store_codes(int8_t* p, int n, const float (&v)[V], uint32_t scale) {
   const float inv = pack_inverse(scale);
   int8_t t[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) t[i] = scale == 255u ? (int8_t)0 : (int8_t)(int)__builtin_rintf(v[i] * inv);
-  typedef typename Word<V>::type W;
-  W w;
-  __builtin_memcpy(&w, t, sizeof w);
-  *reinterpret_cast<W*>(p) = w;
+  if (!TAIL || n >= V) {
+    typename Words<int8_t, V>::W w;
+    __builtin_memcpy(&w, t, sizeof w);
+    *reinterpret_cast<typename Words<int8_t, V>::Unaligned*>(p) = w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < n) p[i] = t[i];
 }
 
 template <int V>
@@ -176,16 +219,16 @@ __device__ __forceinline__ void unpack_codes(const Raw<int8_t, V>& codes, uint32
   for (int i = 0; i < V; ++i) v[i] *= s;
 }
 
-template <int V>
-__device__ __forceinline__ void load_codes(const int8_t* p, uint32_t scale, float (&v)[V]) {
+template <bool TAIL, int V>
+__device__ __forceinline__ void load_codes(const int8_t* p, int n, uint32_t scale, float (&v)[V]) {
   Raw<int8_t, V> codes;
-  codes.load(p);
+  codes.template load_part<TAIL>(p, n);
   unpack_codes(codes, scale, v);
 }
 
 }  // namespace seqdev
 
-// Widest vector of a row of C elements: 16 bytes, or what divides C.
+// Widest vector that divides a row of C elements, at most 16 bytes.
 inline int seq_vec(int type, int64_t C) {
   int v = type == SEQ_BF16 ? 8 : 4;
   while (C % v) v /= 2;
