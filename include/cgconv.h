@@ -414,7 +414,11 @@ const char* cgconv_plan_stage_name(cgconv_plan_t plan, int32_t stage);
  * call, calls only enqueue kernels (capturable), and calls of one plan share its
  * workspace, so two of them must not be in flight on different streams (nor in
  * two captured graphs that run at once).  Arrays are 16-byte aligned and
- * contiguous; what a call writes overlaps none of its other arrays.
+ * contiguous; what a call writes overlaps none of its other arrays.  A call that
+ * would take 2^32 threads in one launch is refused with CGCONV_ERR_UNSUPPORTED (none
+ * is up to 2^28 values, batch * N * K * C, and 2^25 tokens, batch * N); its outputs
+ * are undefined then.  A plan with states holds the workspace of the scan's
+ * backward, its largest part, also where only the forward is called.
  */
 typedef struct cgconv_seq_plan* cgconv_seq_plan_t;
 enum cgconv_dtype { CGCONV_F32 = 0, CGCONV_BF16 = 1 };
@@ -470,8 +474,8 @@ int cgconv_seq_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
  *   y = z, with activation != 0: the invariants y[(0,0)] = z sigmoid(z)
  *
  * weight [W][L_max+1][C], bias [C] (or NULL), fp32.  lengths: int32 [batch] or NULL
- * (N): tokens at and behind a sequence's length are not read, their outputs are
- * zero (values outside 0..N count as the nearest of them).  state_in: the W - 1
+ * (N): what tokens at and behind a sequence's length hold does not matter, their
+ * outputs are zero (values outside 0..N count as the nearest of them).  state_in: the W - 1
  * inputs before the first token, oldest first, [batch][W-1][K][C] of dtype, or
  * NULL (zeros); state_out (or NULL) receives the W - 1 inputs before every
  * sequence's end.  A prompt in pieces, each with the state of the one before, is
@@ -528,7 +532,8 @@ int cgconv_seq_scan_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
  * number, ties to even.  Every step is exact in fp32, so |x - code s| <= s/2 and
  * the codes are the same on any machine; a value of a bfloat16 tensor comes back
  * as a bfloat16 without another rounding.  A group with an infinity or NaN gets
- * the byte 255 and comes back as NaN.  x is of dtype; no plan, no workspace.
+ * the byte 255 and comes back as NaN.  x is of dtype; no plan, no workspace; at
+ * most 2^29 - 32 groups of 32 channels in a call (64 GB of fp32).
  */
 int cgconv_pack8(int32_t dtype, int64_t rows, int64_t C, const void* x, int8_t* codes, uint8_t* scales,
                  hipStream_t stream);

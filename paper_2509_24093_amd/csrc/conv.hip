@@ -393,7 +393,7 @@ template <class T, int V, int WM>
 hipError_t conv_fwd(const ConvArgs& a, hipStream_t s) {
   const ConvShape sh = conv_shape(a.B, a.N, a.K, a.C, V);
   const long long blocks = row_blocks(sh) * sh.colblocks;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((conv_kernel<T, V, WM>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, sh);
   return hipGetLastError();
 }
@@ -402,8 +402,9 @@ template <class T, int V, int WM>
 hipError_t conv_step(const ConvArgs& a, hipStream_t s) {
   const int cols = a.K * a.C / V;
   const long long threads = (long long)a.B * cols;
-  hipLaunchKernelGGL((conv_step_kernel<T, V, WM>), dim3((unsigned)((threads + kThreads - 1) / kThreads)),
-                     dim3(kThreads), 0, s, a, cols, threads);
+  const long long blocks = (threads + kThreads - 1) / kThreads;
+  if (!launch_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((conv_step_kernel<T, V, WM>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, cols, threads);
   return hipGetLastError();
 }
 
@@ -412,7 +413,7 @@ hipError_t conv_bwd(const ConvBwdArgs& g, hipStream_t s) {
   const ConvArgs& a = g.a;
   const ConvShape sh = conv_shape(a.B, a.N, a.K, a.C, V);
   const long long rows = row_blocks(sh);
-  if (rows * sh.colblocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(rows * sh.colblocks, kThreads)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((conv_bwd_kernel<T, V, WM>), dim3((unsigned)(rows * sh.colblocks)), dim3(kThreads), 0, s, g, sh);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !g.part) return e;

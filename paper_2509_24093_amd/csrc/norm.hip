@@ -597,7 +597,7 @@ size_t row_lds_floats(const RowShape& sh, int K, int L) { return (size_t)sh.toke
 template <class T, int V, bool TAIL, int R>
 hipError_t norm_rows(const NormArgs& a, const RowShape& sh, hipStream_t s) {
   const long long blocks = (a.tokens + sh.tokens - 1) / sh.tokens;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(blocks, sh.threads)) return hipErrorInvalidConfiguration;
   const size_t lds = row_lds_floats(sh, a.K, a.L) * sizeof(float);
   if (lds > 64 * 1024) return hipErrorInvalidValue;
   if (a.codes)
@@ -609,7 +609,7 @@ hipError_t norm_rows(const NormArgs& a, const RowShape& sh, hipStream_t s) {
 
 template <class T, int V, bool TAIL, int R>
 hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
-  if (a.tokens > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(a.tokens, threads)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)a.tokens, a.L + 1);
   const auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, magic_of(a.C));

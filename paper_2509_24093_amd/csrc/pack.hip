@@ -54,7 +54,7 @@ hipError_t launch(const void* x, int8_t* codes, uint8_t* scales, void* out, long
   const int nb = (int)pack_blocks(C);
   const long long groups = rows * nb;
   const long long blocks = (groups * (kPackBlock / V) + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
   const auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, static_cast<const T*>(x), codes, scales,
                        static_cast<T*>(out), codes, scales, groups, C, nb);

@@ -326,7 +326,7 @@ hipError_t run_scan(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w,
   const int threads = ids <= 64 ? 64 : ids <= 128 ? 128 : kScanThreads;
   const int colblocks = (ids + threads - 1) / threads;
   const long long blocks = (long long)colblocks * (LOCAL ? ch.chunks - 1 : ch.chunks);
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(blocks, threads)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((scan_kernel<T, KG, SP, LOCAL>), dim3((unsigned)blocks, a.B), dim3(threads), 0, s, a, ch, w,
                      colblocks);
   return hipGetLastError();
@@ -370,8 +370,9 @@ hipError_t scan_step(const ScanArgs& a, hipStream_t s) {
   int groups = 1;
   while (groups * kStepStates < a.S) groups *= 2;
   const int per = kScanThreads / groups;  // vectors per block
-  hipLaunchKernelGGL((scan_step_kernel<T, V>), dim3((unsigned)((vecs + per - 1) / per)), dim3(kScanThreads), 0, s, a,
-                     cols, vecs, groups);
+  const long long blocks = (vecs + per - 1) / per;
+  if (!launch_fits(blocks, kScanThreads)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((scan_step_kernel<T, V>), dim3((unsigned)blocks), dim3(kScanThreads), 0, s, a, cols, vecs, groups);
   return hipGetLastError();
 }
 
@@ -381,7 +382,7 @@ hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, hipStream_
   const int SP = scan_padded(a.S);
   const long long n = (long long)a.B * a.N * 2 * SP + (long long)SP * a.C;
   const long long blocks = (n + kScanThreads - 1) / kScanThreads;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(blocks, kScanThreads)) return hipErrorInvalidConfiguration;
   if (a.type == SEQ_BF16)
     hipLaunchKernelGGL(prepare_kernel<bf16>, dim3((unsigned)blocks), dim3(kScanThreads), 0, s, a, w, SP);
   else

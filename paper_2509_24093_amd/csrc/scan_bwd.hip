@@ -568,7 +568,7 @@ hipError_t run_backward(const ScanBwdArgs& g, const ScanChunks& ch, const ScanSp
   const int colblocks = bwd_colblocks(KC, a.S);
   const int columns = ((KC + colblocks - 1) / colblocks + 63) / 64 * 64;
   const long long blocks = (long long)colblocks * ch.chunks;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (!launch_fits(blocks, columns * BwdShape<SP>::kGroups)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks, a.B);
   hipError_t e;
   if (ch.chunks > 1) {
@@ -584,14 +584,14 @@ hipError_t run_backward(const ScanBwdArgs& g, const ScanChunks& ch, const ScanSp
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (g.gB || g.gC) {
     const long long n = ((long long)a.B * a.N * 2 * SP + 255) / 256;
-    if (n > INT32_MAX) return hipErrorInvalidValue;
+    if (!launch_fits(n, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(sum_bc_kernel<T>, dim3((unsigned)n), dim3(256), 0, s, g, w.gbc, colblocks, SP);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.K > 1 && (g.gdelta || g.gbias)) {
     const int width = bias_width(a.C), cbs = (a.C + width - 1) / width;
     const long long tbs = bias_blocks(a.B, a.N, a.C);
-    if (tbs * cbs > INT32_MAX) return hipErrorInvalidValue;
+    if (!launch_fits(tbs * cbs, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(delta_kernel<T>, dim3((unsigned)(tbs * cbs)), dim3(256), 0, s, g, w, width, cbs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (g.gbias && (e = sum_units(w.gbp, tbs, 1, 0, 1, a.C, nullptr, g.gbias, nullptr, s)) != hipSuccess) return e;

@@ -16,6 +16,12 @@ void set_last_error(const char* fmt, ...) __attribute__((format(printf, 1, 2)));
 void clear_last_error();
 
 enum SeqType : int { SEQ_F32 = 0, SEQ_BF16 = 1 };
+// A launch counts its threads along an axis in 32 bits.  A launcher that would pass
+// that returns hipErrorInvalidConfiguration (CGCONV_ERR_UNSUPPORTED to the caller).
+inline bool launch_fits(long long blocks, int threads) {
+  return blocks <= INT32_MAX && blocks * threads <= UINT32_MAX;
+}
+
 inline int64_t seq_type_size(int type) { return type == SEQ_BF16 ? 2 : 4; }
 
 // Channels that share one scale of an 8-bit checkpoint.

@@ -87,6 +87,10 @@ int check_plan(const cgconv_seq_plan* p, int32_t dtype) {
 
 int launched(hipError_t e) {
   if (e == hipSuccess) return CGCONV_OK;
+  if (e == hipErrorInvalidConfiguration) {
+    set_last_error("unsupported sizes: more threads than one launch takes");
+    return CGCONV_ERR_UNSUPPORTED;
+  }
   set_last_error("kernel launch failed: %s", hipGetErrorString(e));
   return CGCONV_ERR_HIP;
 }
@@ -463,7 +467,8 @@ static int check_pack(int32_t dtype, int64_t rows, int64_t C) {
     set_last_error("invalid sizes: rows=%lld C=%lld", (long long)rows, (long long)C);
     return CGCONV_ERR_INVALID_ARG;
   }
-  if (rows > ((int64_t)INT32_MAX * 8) / pack_blocks(C)) {  // one launch: 8 groups of 32 channels a block
+  constexpr int64_t kGroups = (1LL << 29) - 32;  // whole blocks of 32 groups, 8 threads each, below 2^32 threads
+  if (rows > kGroups / pack_blocks(C)) {
     set_last_error("unsupported rows=%lld at C=%lld: too many for one launch", (long long)rows, (long long)C);
     return CGCONV_ERR_UNSUPPORTED;
   }

@@ -230,3 +230,39 @@ for L in (0, 1, 2, 3, 6, 8):
                         assert 64 <= block[0] <= 1024 and block[0] % 64 == 0 and lds <= allowed and grid[1] <= 65535 and grid[2] <= 65535, (L, C, grid, block, lds)
                 P.cgconv_seq_plan_destroy(plan)
 """)
+
+
+def test_launches_of_the_largest_sizes(tmp_path):
+    """A launch counts its threads along an axis in 32 bits: what fits is launched,
+    the rest refused before its launch."""
+    run(tmp_path, """
+big = lambda i: 1 << (44 + i) if i else 1 << 43
+lib = P.library()
+def calls(plan, dtype):
+    yield lib.cgconv_seq_norm(plan, dtype, big(0), big(1), big(2), 0.0, big(3), big(4), big(5), big(6), big(7), None)
+    yield lib.cgconv_seq_norm_backward(plan, dtype, big(0), None, None, big(1), big(2), big(3), big(4), big(5), big(6), big(7), None)
+    yield lib.cgconv_seq_conv(plan, dtype, 4, big(0), big(1), big(2), 1, *(big(i) for i in range(3, 7)), None)
+    yield lib.cgconv_seq_conv_step(plan, dtype, 4, big(0), big(1), big(2), 1, big(3), big(4), None)
+    yield lib.cgconv_seq_conv_backward(plan, dtype, 4, big(0), big(1), big(2), 1, *(big(i) for i in range(3, 8)), None)
+refusals = 0
+for B, N, L, C in ((1, 2**25, 0, 8), (1, 2**25, 0, 7), (4096, 8192, 2, 1), (65535, 512, 0, 8), (65535, 1, 8, 50), (16, 2**10, 0, 16381),
+                   (1, 2**30, 0, 32), (1, 2**30, 0, 1), (1, 2**26, 0, 4096), (65535, 1, 8, 963), (1, 2**27, 3, 33)):
+    plan = P.cgconv_seq_plan_create(B, N, L, C)
+    assert plan, P.cgconv_last_error()
+    ordinary = B * N * (L + 1) ** 2 * C <= 2**28 and B * N <= 2**25
+    for dtype in (0, 1):
+        for status in calls(plan, dtype):
+            assert status in ((0,) if ordinary else (0, P.CGCONV_ERR_UNSUPPORTED)), (B, N, L, C, status, P.cgconv_last_error())
+            if status:
+                assert "more threads" in P.cgconv_last_error()
+                refusals += 1
+        for grid, block, lds, allowed in launches():
+            assert all(g * b < 2**32 for g, b in zip(grid, block)) and 0 < grid[0] < 2**31, (B, N, L, C, grid, block)
+    P.cgconv_seq_plan_destroy(plan)
+assert refusals
+for dtype in (0, 1):
+    assert lib.cgconv_pack8(dtype, 2**29 - 32, 32, big(0), big(5), big(9), None) == 0
+    assert lib.cgconv_pack8(dtype, 2**29 - 31, 32, big(0), big(5), big(9), None) == P.CGCONV_ERR_UNSUPPORTED
+for grid, block, lds, allowed in launches():
+    assert grid[0] * block[0] < 2**32
+""")
