@@ -362,8 +362,8 @@ class SequencePlan:
     def conv(self, x, weight, bias=None, lengths=None, state=None, activation: bool = True, out=None):
         """Short causal convolution over the tokens: weight [width, L_max+1, C]
         and bias [C], fp32; the invariants pass z sigmoid(z) unless activation
-        is False.  lengths (int32 [batch]): tokens behind them are not read,
-        their outputs are zero.  Returns (y, state): the width - 1 inputs before
+        is False.  lengths (int32 [batch]): what tokens behind them hold does
+        not matter, their outputs are zero.  Returns (y, state): the width - 1 inputs before
         every sequence's end, [batch, width - 1, K, C], for conv_step or the
         next piece (state=)."""
         dtype, width, args = self._conv_args(x, weight, bias, self.shape)
@@ -467,6 +467,13 @@ class SequencePlan:
 _functions = {}
 
 
+def _whole(grad):
+    """An incoming gradient as the entry points take it: contiguous, at a 16-byte
+    boundary (that of a part of a concatenation may start anywhere)."""
+    grad = grad.contiguous()
+    return grad if grad.data_ptr() % 16 == 0 else grad.clone()
+
+
 def _grad_wanted(*tensors) -> bool:
     import torch
     return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
@@ -491,7 +498,7 @@ def _norm_function():
             weight, mean, rstd, *held = ctx.saved_tensors
             need = ctx.needs_input_grad
             return ctx.plan.norm_backward(held if len(held) == 2 else held[0], weight, mean, rstd,
-                                          grad_y.contiguous(), need[0], need[1], need[2]) + (None, None, None)
+                                          _whole(grad_y), need[0], need[1], need[2]) + (None, None, None)
 
     return _NormFn
 
@@ -523,7 +530,7 @@ def _conv_function():
         def backward(ctx, grad_y):
             (x,), (weight, bias, lengths) = kept(ctx)
             need = ctx.needs_input_grad
-            return ctx.plan.conv_backward(x, weight, bias, grad_y.contiguous(), lengths, ctx.activation, need[0],
+            return ctx.plan.conv_backward(x, weight, bias, _whole(grad_y), lengths, ctx.activation, need[0],
                                           need[1], need[2]) + (None,) * 4
 
     return _ConvFn
@@ -557,7 +564,7 @@ def _scan_function():
             (x,), (delta, A, Bt, Ct, D, delta_bias, lengths) = kept(ctx)
             need = tuple(n and t is not None
                          for n, t in zip(ctx.needs_input_grad, (x, delta, A, Bt, Ct, D, delta_bias)))
-            return ctx.plan.scan_backward(x, delta, A, Bt, Ct, D, grad_y.contiguous(), delta_bias, lengths,
+            return ctx.plan.scan_backward(x, delta, A, Bt, Ct, D, _whole(grad_y), delta_bias, lengths,
                                           need) + (None,) * 3
 
     return _ScanFn

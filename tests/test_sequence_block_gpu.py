@@ -269,3 +269,26 @@ def test_gradients_reach_views_and_expanded_inputs():
     with pytest.raises(RuntimeError):
         gx.sum().backward()
     seq.close()
+
+
+def test_gradient_that_starts_off_a_vector():
+    """A part of a concatenation sends a gradient that is contiguous at one sequence
+    but starts anywhere: the same gradients as from one at its own address."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    n, c, s = 7, 5, 3
+    seq = P.SequencePlan(1, n, 0, c, s)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    f = lambda *shape: torch.randn(*shape, generator=gen, device="cuda").requires_grad_()  # noqa: E731
+    x, delta, A, Bt, Ct = f(1, n, 1, c), f(1, n, c), f(c, s), f(1, n, s), f(1, n, s)
+    w, cw, head = f(1, c), f(4, 1, c), f(1, 1, 1, c)
+    for op in (lambda: P.cgconv_norm(x, w, None, seq), lambda: P.cgconv_short_conv(x, cw, None, seq),
+               lambda: P.cgconv_scan(x, delta, -A.detach().abs(), Bt, Ct, None, seq)):
+        g = torch.randn(1, n + 1, 1, c, generator=gen, device="cuda")
+        part = g[:, 1:]
+        assert part.is_contiguous() and part.data_ptr() % 16
+        want, = torch.autograd.grad(op(), x, part.clone())
+        got, = torch.autograd.grad(torch.cat((head, op()), 1), x, g)
+        assert torch.equal(got, want)
+        got, = torch.autograd.grad(op(), x, part)
+        assert torch.equal(got, want)
