@@ -607,7 +607,7 @@ hipError_t by_states(const ScanBwdArgs& g, hipStream_t s) {
   const ScanArgs& a = g.a;
   const ScanChunks ch = backward_chunks(a.N);
   const ScanSpace w = backward_space(a.ws, a.B, a.N, a.K, a.C, a.S);
-  const hipError_t e = launch_scan_prepare(a, w, s);
+  const hipError_t e = launch_scan_prepare(a, w, scan_padded(a.S), s);
   if (e != hipSuccess) return e;
   switch (scan_padded(a.S)) {
     case 8: return run_backward<T, 8>(g, ch, w, s);

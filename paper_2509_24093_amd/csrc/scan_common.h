@@ -136,7 +136,8 @@ struct ScanSpace {
 size_t scan_forward_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
 size_t scan_backward_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
 
-hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, hipStream_t s);
+// bc and A2 for rows of SP states
+hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, int SP, hipStream_t s);
 // hs: what the chunks add to what they start with; rs (or nullptr) likewise, in reverse
 hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, const float* first, bool reverse,
                              hipStream_t s);
