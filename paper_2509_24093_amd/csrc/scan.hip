@@ -152,16 +152,15 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(ScanArgs a, ScanChun
 }
 
 // Pass (2): h <- exp(A ds) h + add from chunk to chunk, for 64 states per block;
-// each of its kCarrySlices waves first composes its own run of chunks, then
-// starts from the runs before it.  A run of at most RUN chunks stays in registers
+// each of its SLICES waves first composes its own run of chunks, then starts from
+// the runs before it.  A run of at most RUN chunks stays in registers
 // between the two, a longer one (not HELD) is read twice.  The arrays hold, in,
 // what a chunk adds and, out, what it starts with; y = 1 of the grid goes through
 // rs backwards.  The chunk at the far end adds to nobody and need not be formed.
-constexpr int kCarrySlices = 16;
-template <int RUN, bool HELD>
-__global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, ScanChunks sh, ScanSpace ws,
-                                                                  const float* first) {
-  __shared__ float scale[kCarrySlices][64], shift[kCarrySlices][64];
+template <int SLICES, int RUN, bool HELD>
+__global__ __launch_bounds__(64 * SLICES) void carry_kernel(ScanArgs a, ScanChunks sh, ScanSpace ws,
+                                                            const float* first) {
+  __shared__ float scale[SLICES][64], shift[SLICES][64];
   const long long KC = (long long)a.K * a.C;
   const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, b = blockIdx.z;
   const bool reverse = blockIdx.y;
@@ -172,7 +171,7 @@ __global__ __launch_bounds__(64 * kCarrySlices) void carry_kernel(ScanArgs a, Sc
   const float A2 = ws.A2[s * a.C + c];
   float* p = (reverse ? ws.rs : ws.hs) + (long long)b * sh.chunks * a.S * KC + id;
   const float* d = ws.ds + (long long)b * sh.chunks * a.C + c;
-  const int run = (sh.chunks + kCarrySlices - 1) / kCarrySlices;
+  const int run = (sh.chunks + SLICES - 1) / SLICES;
   const int n0 = min(slice * run, sh.chunks), n1 = min(n0 + run, sh.chunks);
   float add[RUN], e[RUN];
   auto load = [&](int n) {
@@ -400,17 +399,23 @@ hipError_t launch_scan_prepare(const ScanArgs& a, const ScanSpace& w, int SP, hi
 hipError_t launch_scan_carry(const ScanArgs& a, const ScanChunks& ch, const ScanSpace& w, const float* first, bool reverse,
                              hipStream_t s) {
   const long long n = (long long)a.S * a.K * a.C;
-  const dim3 grid((unsigned)((n + 63) / 64), reverse ? 2 : 1, a.B), block(64 * kCarrySlices);
-  const int run = (ch.chunks + kCarrySlices - 1) / kCarrySlices;
-  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, ch, w, first); };
-  if (run <= 1)
-    go(carry_kernel<1, true>);
-  else if (run <= 4)
-    go(carry_kernel<4, true>);
-  else if (run <= 16)
-    go(carry_kernel<16, true>);
+  const dim3 grid((unsigned)((n + 63) / 64), reverse ? 2 : 1, a.B);
+  const auto go = [&](auto kernel, int slices) {
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * slices), 0, s, a, ch, w, first);
+  };
+  // as many slices as leave four chunks to each, or sixteen (16 x 1024 tokens of 2048
+  // in 16 chunks, whole scan: sixteen slices 273 us, four 253; two chunks of 24 tokens
+  // of 49 x 57, both ways: the carry with sixteen 37 us, with one 7)
+  if (ch.chunks <= 4)
+    go(carry_kernel<1, 4, true>, 1);
+  else if (ch.chunks <= 16)
+    go(carry_kernel<4, 4, true>, 4);
+  else if (ch.chunks <= 64)
+    go(carry_kernel<16, 4, true>, 16);
+  else if (ch.chunks <= 256)
+    go(carry_kernel<16, 16, true>, 16);
   else
-    go(carry_kernel<16, false>);
+    go(carry_kernel<16, 16, false>, 16);
   return hipGetLastError();
 }
 
