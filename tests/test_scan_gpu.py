@@ -166,6 +166,13 @@ def test_forward_and_gradients(shape, ragged, dtype):
     plan.close()
 
 
+@pytest.mark.parametrize("N", [64, 65, 256, 257, 1024, 1025, 4096, 4097, 8225])
+def test_chunk_counts(N):
+    """Both sides of every number of chunks at which the carry takes another form
+    (chunks of 16 tokens backward, of 32 forward), with lengths."""
+    test_forward_and_gradients((2, N, 0, 3, 4), True, "fp32")
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("shape", [(1, 6, 0, 1, 3), (3, 6, 1, 10, 16), (2, 6, 2, 33, 32), (1, 6, 0, 260, 16)], ids=str)
 def test_steps(shape, dtype):
