@@ -493,7 +493,7 @@ def cgconv(q, k, plan: Plan, checkpoint=None):
             @staticmethod
             def backward(ctx, grad_out):
                 (q, k), _ = sequence.kept(ctx)
-                gq, gk = ctx.plan.backward(q, k, grad_out.contiguous(), need_q=ctx.needs_input_grad[0],
+                gq, gk = ctx.plan.backward(q, k, sequence._whole(grad_out), need_q=ctx.needs_input_grad[0],
                                            need_k=ctx.needs_input_grad[1])
                 return gq, gk, None, None
 
@@ -567,7 +567,7 @@ def cgconv_gate(u, v, plan: Plan, checkpoint=None):
             @staticmethod
             def backward(ctx, grad_f):
                 (u, v), _ = sequence.kept(ctx)
-                gu, gv = ctx.plan.gate_value_backward(u, v, grad_f.contiguous(), need_u=ctx.needs_input_grad[0],
+                gu, gv = ctx.plan.gate_value_backward(u, v, sequence._whole(grad_f), need_u=ctx.needs_input_grad[0],
                                                       need_v=ctx.needs_input_grad[1])
                 return gu, gv, None, None
 
@@ -601,7 +601,7 @@ def cgconv_graph(U, q, k, plan: GraphPlan, checkpoint=None):
             @staticmethod
             def backward(ctx, grad_out):
                 (q, k), (U,) = sequence.kept(ctx)
-                gq, gk = ctx.plan.backward(U, q, k, grad_out.contiguous(), need_q=ctx.needs_input_grad[1],
+                gq, gk = ctx.plan.backward(U, q, k, sequence._whole(grad_out), need_q=ctx.needs_input_grad[1],
                                            need_k=ctx.needs_input_grad[2])
                 return None, gq, gk, None, None
 
