@@ -3,6 +3,7 @@
 // memory, launches and function attributes are recorded and nothing runs.
 // Loaded with global visibility before libcgconv.so (tests/host_runtime.py).
 #include <hip/hip_runtime_api.h>
+#include <sys/mman.h>
 
 #include <cstdint>
 #include <cstdlib>
@@ -22,13 +23,34 @@ struct Config {
   hipStream_t stream;
 } g_config;
 constexpr int64_t kDefaultLds = 64 * 1024;
+// Workspaces beyond this size, which no host code touches, take addresses only.
+constexpr size_t kReserved = size_t{1} << 30;
+std::map<void*, size_t> g_reserved;
 }  // namespace
 
 extern "C" {
 hipError_t hipGetDevice(int* d) { *d = 0; return hipSuccess; }
 hipError_t hipGetLastError() { return hipSuccess; }
-hipError_t hipMalloc(void** p, size_t n) { *p = aligned_alloc(256, (n + 255) / 256 * 256); return *p ? hipSuccess : hipErrorOutOfMemory; }
-hipError_t hipFree(void* p) { free(p); return hipSuccess; }
+hipError_t hipMalloc(void** p, size_t n) {
+  if (n > kReserved) {
+    *p = mmap(nullptr, n, PROT_NONE, MAP_PRIVATE | MAP_ANONYMOUS | MAP_NORESERVE, -1, 0);
+    if (*p == MAP_FAILED) return hipErrorOutOfMemory;
+    g_reserved[*p] = n;
+    return hipSuccess;
+  }
+  *p = aligned_alloc(256, (n + 255) / 256 * 256);
+  return *p ? hipSuccess : hipErrorOutOfMemory;
+}
+hipError_t hipFree(void* p) {
+  const auto it = g_reserved.find(p);
+  if (it == g_reserved.end()) {
+    free(p);
+  } else {
+    munmap(p, it->second);
+    g_reserved.erase(it);
+  }
+  return hipSuccess;
+}
 hipError_t hipMemcpy(void* d, const void* s, size_t n, hipMemcpyKind) { memcpy(d, s, n); return hipSuccess; }
 hipError_t hipFuncSetAttribute(const void* f, hipFuncAttribute a, int v) {
   if (a == hipFuncAttributeMaxDynamicSharedMemorySize) g_allowed[f] = v;
