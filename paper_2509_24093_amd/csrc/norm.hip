@@ -568,12 +568,12 @@ RowShape row_shape(int C, int K, int V, int max_passes, int max_threads, int max
 struct WideShape {
   int threads = 0, vecs = 0;  // vecs: per thread, a power of two
 };
-// Wide form: about 4 vectors a thread (8 for the largest rows).
-WideShape wide_shape(int n, int V, int max_vecs) {
+// Wide form: the usual number of vectors a thread, more where 1024 threads would not do.
+WideShape wide_shape(int n, int V, int usual) {
   WideShape w;
   const int total = (n + V - 1) / V;
   for (w.threads = 64; w.threads < 1024; w.threads *= 2)
-    if (total <= w.threads * std::min(4, max_vecs)) break;
+    if (total <= w.threads * usual) break;
   w.vecs = 1;
   while (w.vecs * w.threads < total) w.vecs *= 2;
   return w;
@@ -607,6 +607,25 @@ hipError_t norm_rows(const NormArgs& a, const RowShape& sh, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Vectors that a thread of the wide form holds, and at most in a row that is longer
+// than 1024 threads of them (vectors of one or two elements).
+constexpr int usual_vecs(int V, bool backward) { return backward && V == 8 ? 2 : 4; }
+constexpr int max_vecs(int V, bool backward) { return std::max(usual_vecs(V, backward), 16 / V); }
+
+// f of the most threads a block of R vectors a thread has: fewer vectors than usual
+// are blocks of 64 threads, more blocks of 1024.  BYTES of a vector: of two, a row that
+// takes the wide form has more than 256 threads' worth.
+template <int R, int USUAL, int BYTES, class F>
+hipError_t by_threads(int threads, F f) {
+  if constexpr (R <= USUAL && BYTES > 2) {
+    if (threads <= 256) return f(std::integral_constant<int, 256>());
+  }
+  if constexpr (R >= USUAL) {
+    if (threads > 256) return f(std::integral_constant<int, 1024>());
+  }
+  return hipErrorInvalidValue;
+}
+
 template <class T, int V, bool TAIL, int R>
 hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
   if (!launch_fits(a.tokens, threads)) return hipErrorInvalidConfiguration;
@@ -615,15 +634,17 @@ hipError_t norm_wide(const NormArgs& a, int threads, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, magic_of(a.C));
     return hipGetLastError();
   };
-  if (a.codes && (a.C % kPackBlock == 0 || a.L == 0))
-    return threads <= 256 ? run(norm_wide_kernel<T, V, R, true, 256, TAIL>)
-                          : run(norm_wide_kernel<T, V, R, true, 1024, TAIL>);
-  if (a.codes) {  // a scale's channels would straddle the lanes: a pass of its own
-    const hipError_t e = launch_pack(a.type, a.x, a.codes, a.scales, a.tokens * a.K, a.C, s);
-    if (e != hipSuccess) return e;
-  }
-  return threads <= 256 ? run(norm_wide_kernel<T, V, R, false, 256, TAIL>)
-                        : run(norm_wide_kernel<T, V, R, false, 1024, TAIL>);
+  return by_threads<R, usual_vecs(V, false), V * (int)sizeof(T)>(threads, [&](auto most) {
+    constexpr int kMost = decltype(most)::value;
+    if constexpr (V >= 4) {  // narrower vectors: C no multiple of four, L > 0
+      if (a.codes && (a.C % kPackBlock == 0 || a.L == 0)) return run(norm_wide_kernel<T, V, R, true, kMost, TAIL>);
+    }
+    if (a.codes) {  // a scale's channels would straddle the lanes: a pass of its own
+      const hipError_t e = launch_pack(a.type, a.x, a.codes, a.scales, a.tokens * a.K, a.C, s);
+      if (e != hipSuccess) return e;
+    }
+    return run(norm_wide_kernel<T, V, R, false, kMost, TAIL>);
+  });
 }
 
 template <class T, int V, bool TAIL, int R>
@@ -652,25 +673,24 @@ hipError_t norm_wide_bwd(const NormBwdArgs& a, int threads, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, magic_of(a.C));
     return hipGetLastError();
   };
-  const hipError_t e =
-      a.codes ? (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, true, 256, TAIL>)
-                                : run(norm_wide_bwd_kernel<T, V, R, true, 1024, TAIL>))
-              : (threads <= 256 ? run(norm_wide_bwd_kernel<T, V, R, false, 256, TAIL>)
-                                : run(norm_wide_bwd_kernel<T, V, R, false, 1024, TAIL>));
+  const hipError_t e = by_threads<R, usual_vecs(V, true), V * (int)sizeof(T)>(threads, [&](auto most) {
+    constexpr int kMost = decltype(most)::value;
+    return a.codes ? run(norm_wide_bwd_kernel<T, V, R, true, kMost, TAIL>)
+                   : run(norm_wide_bwd_kernel<T, V, R, false, kMost, TAIL>);
+  });
   if (e != hipSuccess || !a.part) return e;
   hipLaunchKernelGGL(norm_sum_kernel, dim3(((a.L + 2) * a.C + 63) / 64), dim3(64 * kSumSlices), 0, s, a.part, blocks,
                      a.L, a.K, a.C, 0, a.gw, a.gb);
   return hipGetLastError();
 }
 
-// Values a thread holds of one array: 32 in the forward, 16 in the backward
-// (which holds four arrays).
+// Rows per thread of the row form, whose vectors have at least four elements: up to
+// 32 values of one array in the forward, 16 in the backward (which holds four arrays).
 constexpr int kFwdPasses = 4;
-constexpr int fwd_values(int V) { return V >= 4 ? 32 : 16; }
-constexpr int kBwdValues = 16;
-constexpr int bwd_passes(int V) { return V >= 4 ? kBwdValues / V : 4; }
+constexpr int bwd_passes(int V) { return 16 / V; }
 
-// f of the number of vectors per thread, a power of two up to MAX
+// f of the number of vectors per thread, a power of two from R up to MAX.  A row of
+// the wide form has more than 64 vectors, or 256 / V where they are narrower than four.
 template <int R, int MAX, class F>
 hipError_t by_vecs(int vecs, F f) {
   if (vecs == R) return f(std::integral_constant<int, R>());
@@ -701,7 +721,7 @@ Form norm_form(int type, int C, int L, bool backward) {
     f.tail = false;
     f.v = exact;
   }
-  f.wide = wide_shape((2 * L + 1) * C, f.v, (backward ? kBwdValues : fwd_values(f.v)) / f.v);
+  f.wide = wide_shape((2 * L + 1) * C, f.v, usual_vecs(f.v, backward));
   return f;
 }
 
@@ -710,7 +730,7 @@ hipError_t norm_any(const NormArgs& a, const Form& f, hipStream_t s) {
   if constexpr (V >= 4) {
     if (f.row.tokens) return f.row.passes == 2 ? norm_rows<T, V, TAIL, 2>(a, f.row, s) : norm_rows<T, V, TAIL, 4>(a, f.row, s);
   }
-  return by_vecs<1, fwd_values(V) / V>(
+  return by_vecs<(V >= 4 ? 2 : 4), max_vecs(V, false)>(
       f.wide.vecs, [&](auto r) { return norm_wide<T, V, TAIL, decltype(r)::value>(a, f.wide.threads, s); });
 }
 
@@ -721,7 +741,7 @@ hipError_t norm_any(const NormBwdArgs& a, const Form& f, hipStream_t s) {
       return f.row.passes == 2 ? norm_rows_bwd<T, V, TAIL, 2>(a, f.row, s)
                                : norm_rows_bwd<T, V, TAIL, bwd_passes(V)>(a, f.row, s);
   }
-  return by_vecs<1, kBwdValues / V>(
+  return by_vecs<(V >= 4 ? 2 : 4), max_vecs(V, true)>(
       f.wide.vecs, [&](auto r) { return norm_wide_bwd<T, V, TAIL, decltype(r)::value>(a, f.wide.threads, s); });
 }
 

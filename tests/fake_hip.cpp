@@ -9,6 +9,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <string>
 #include <vector>
 
 namespace {
@@ -17,6 +18,7 @@ struct Launch {
 };
 std::vector<Launch> g_launches;
 std::map<const void*, int64_t> g_allowed;
+std::map<const void*, std::string> g_idle;  // kernels that were never launched
 struct Config {
   dim3 grid, block;
   size_t lds;
@@ -67,7 +69,11 @@ hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipSt
   *s = g_config.stream;
   return hipSuccess;
 }
+void __hipRegisterFunction(void**, const void* f, char*, const char* name, unsigned, void*, void*, dim3*, dim3*, int*) {
+  g_idle[f] = name;
+}
 hipError_t hipLaunchKernel(const void* f, dim3 g, dim3 b, void**, size_t lds, hipStream_t) {
+  g_idle.erase(f);
   const auto it = g_allowed.find(f);
   g_launches.push_back({{g.x, g.y, g.z}, {b.x, b.y, b.z}, (int64_t)lds, it == g_allowed.end() ? kDefaultLds : it->second});
   return hipSuccess;
@@ -78,5 +84,12 @@ int64_t fake_hip_launches(int64_t* out, int64_t cap) {
   for (int64_t i = 0; i < n && i < cap; ++i) memcpy(out + 8 * i, &g_launches[i], sizeof(Launch));
   g_launches.clear();
   return n;
+}
+// the names of the library's kernels that no call has launched, one a line; returns their length
+int64_t fake_hip_idle(char* out, int64_t cap) {
+  std::string names;
+  for (const auto& k : g_idle) names += k.second + "\n";
+  if (out && cap > 0) strncpy(out, names.c_str(), (size_t)cap);
+  return (int64_t)names.size();
 }
 }
