@@ -57,13 +57,10 @@ struct NormBwdArgs {
   void* gx;               // or nullptr
   float* gw;              // [L+1][C] or nullptr
   float* gb;              // [C] or nullptr
-  float* part;            // norm_bwd_blocks(...) * (K + 1) * C floats
+  float* part;            // norm_bwd_part_bytes, or nullptr if neither gw nor gb is wanted
   long long tokens;
   int L, K, C;
 };
-
-// Longest (2L+1) C: one block holds the largest degree of a token.
-constexpr int kNormMaxSegment = 16384;
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t s);
@@ -106,7 +103,6 @@ size_t conv_bwd_part_bytes(int64_t B, int64_t N, int K, int64_t C);
 
 // ---- selective scan --------------------------------------------------------------
 
-constexpr int kScanMaxStates = 32;
 struct ScanArgs {
   int type;
   const void* x;      // [B][N][K][C] (a step: [B][K][C])
