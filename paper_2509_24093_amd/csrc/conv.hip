@@ -7,8 +7,8 @@
 // A thread takes V neighbouring columns over a chunk of tokens and keeps the
 // last inputs in registers, so x is read once but for the W - 1 tokens before
 // a chunk; the next four tokens are asked for, as stored, while four are computed
-// (bf16, 4 x 8192 tokens of 2048 channels: forward 55 -> 48 us, backward 151 ->
-// 100).  The backward walks a chunk in the same direction: it forms z again,
+// (bf16, 4 x 8192 tokens of 2048 channels: forward 71 -> 51 us, backward 157 ->
+// 104).  The backward walks a chunk in the same direction: it forms z again,
 // gz = gy y'(z), adds gz[t] x[t-j] to gw in registers and emits
 // gx[t] = sum_j w[j] gz[t+j] W - 1 tokens later; the tokens behind a chunk are
 // formed twice.  Both are streams, in fp32 bound by HBM (8 x 16384 tokens of 49 x 32:

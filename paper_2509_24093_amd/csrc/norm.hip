@@ -16,9 +16,14 @@
 // pass, all of them in registers: the sum of a row is a lane reduction, the sum
 // of a degree adds the sums of its rows through LDS.  Longer rows: a block per
 // degree of a token.  Either way every input is read once and every output
-// written once.  In the backward the threads keep their columns from token to
-// token, so gw and gb grow in registers over all tokens of a block; the blocks'
-// sums are added by a second kernel in a fixed order.
+// written once, but for an 8-bit checkpoint of rows of the second form with L > 0
+// whose channels are no multiple of 32: a pass of its own reads x again.  In the
+// backward the threads keep their columns from token to token, so gw and gb grow in
+// registers over all tokens of a block; the blocks' sums are added by a second
+// kernel in a fixed order.  Registers: where no vector of four elements divides a
+// row of the second form with L > 0, a thread of the longest rows holds 8 or 16
+// vectors and spills (16 in the forward up to 464 bytes of scratch a thread, in the
+// backward 36 to 524; the other backward kernels of that form at most 40).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(kBwdRowThreads) void norm_rows_bwd_kernel(NormBwdAr
 // loaded as it is stored while the one before is computed for bf16 rows of whole
 // vectors, where that takes 16 registers and four waves per SIMD still fit (8 x
 // 2048 tokens of 4096 channels, forward and backward: 185 -> 164 us, at three waves
-// 190; with 8-bit inputs three waves, 32768 of 1024 139 -> 107; fp32, 4 x 4096
+// 190; with 8-bit inputs three waves, the backward of 32768 of 1024 73 -> 54; fp32, 4 x 4096
 // tokens of L=2 C=512 with 32 registers ahead: 320 -> 392).
 // Partial sums: part[slot][K components, then gb][C].
 template <class T, int V, int R, bool CODES, int MAXT, bool TAIL>

@@ -7,7 +7,9 @@
 // writing y.  Where batch and channels give waves enough there is one chunk
 // and only (3).  It is bound by the vector units: per state an exponential (a
 // quarter of the rate) and its product, and three operations for each of the
-// KG components a thread holds.
+// KG components a thread holds.  Four components of 16 states and more take all 256
+// registers and 13 to 206 accumulation registers beside them in the output pass: one wave
+// per SIMD.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -289,8 +291,10 @@ __global__ __launch_bounds__(kScanThreads) void scan_step_kernel(ScanArgs a, int
   if (s0 == 0) store_vec(static_cast<T*>(a.y) + b * KC + e0, y);
 }
 
-// Waves that keep the vector units busy (4 x 8192 tokens of 2048 channels: 1024
-// 778 us, 2048 523, 4096 460, 8192 345, 16384 350), and the shortest chunk worth its
+// Waves that keep the vector units busy (4 x 8192 tokens of 2048 channels, bf16, 16
+// states: one chunk, 128 waves, 2690 us; in chunks, which form every state twice, 1024
+// 779, 2048 529, 4096 473, 8192 443, 16384 442; with lengths from half on 769, 523, 467,
+// 390, 358, for twice the chunks' states), and the shortest chunk worth its
 // states (S values written and read per chunk and column), shorter in short
 // sequences, whose time is that of one chunk (300 tokens of 9 x 16, whole call: 46 -> 31 us).
 constexpr long long kWantedWaves = 8192;

@@ -13,9 +13,9 @@
 // the kSub states of a piece in registers.  What the chunks add to the states
 // behind them and to r before them comes from one pass over the tokens: with the
 // running product P_t of the decays, sum_t P_t C_t gy_t is the chunk's own r, so
-// both take one exponential per state.  gB and gC add over the lanes: the SP
-// values of a token are halved from step to step, each lane keeping the half of
-// its bit, so 16 values take 15 exchanges and 2 more instead of 96; waves add
+// both take one exponential per state.  gB and gC add over the lanes: the
+// eight values of a token that a wave has are halved from step to step, each lane
+// keeping the half of its bit, so they take 7 exchanges and 3 more instead of 48; waves add
 // through LDS, column blocks in a last kernel.  No atomics: every sum has a fixed
 // order.
 #include <hip/hip_runtime.h>
@@ -37,7 +37,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // sums over all states go through LDS.  Tokens per chunk and per piece, columns per
 // block: the states of a piece take kSub kGroup registers, the pieces' starts
 // (chunk / sub - 1) kGroup columns groups 4 bytes of LDS (48 KiB), the sums kSub
-// columns groups 8 bytes (16 KiB): two blocks per CU, four waves per SIMD.  2 x 4096
+// columns groups 8 bytes (16 KiB): two blocks per CU, four waves per SIMD (whose 128
+// registers are 2 to 14 too few, spilled).  2 x 4096
 // x 1024 bf16, 16 states, forward and backward: all 16 states in a thread, pieces of
 // 8, two waves per SIMD 366 us; groups of 8, pieces of 8 413, of 6 360, of 5 357, of 4
 // 351, of 3 374; the next piece's inputs asked for a piece ahead, with the other

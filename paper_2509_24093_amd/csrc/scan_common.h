@@ -25,8 +25,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|) in (0, 1]; log1p(e) = 2
-// atanh(u), u = e / (2 + e) <= 1/3, by its series in u^2 <= 1/9: the first term
-// left out is u^17 2/17, below 2^-30 of the sum.
+// atanh(u), u = e / (2 + e) <= 1/3, by its series in u^2 <= 1/9: the terms
+// left out, from u^17 2/17 on, are below 2^-29 of the sum.
 __device__ __forceinline__ float softplus(float v) {
   const float e = exp2_fast(-fabsf(v) * kLog2e);
   const float u = e * __builtin_amdgcn_rcpf(2.f + e), q = u * u;
