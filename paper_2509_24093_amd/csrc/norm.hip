@@ -695,8 +695,8 @@ constexpr int kFwdPasses = 4;
 constexpr int bwd_passes(int V) { return 16 / V; }
 
 // f of the number of vectors per thread, a power of two from R up to MAX.  A row of
-// the wide form has more vectors than one for each of 64 threads; narrower ones than
-// four elements more than two, as no row of at most 64 full vectors is wide.
+// the wide form has more than 64 vectors, and more than 128 where they are narrower
+// than four elements, so that its 64 threads hold two and four of them at least.
 template <int R, int MAX, class F>
 hipError_t by_vecs(int vecs, F f) {
   if (vecs == R) return f(std::integral_constant<int, R>());
