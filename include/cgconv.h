@@ -427,6 +427,7 @@ enum cgconv_dtype { CGCONV_F32 = 0, CGCONV_BF16 = 1 };
 #define CGCONV_SEQ_SEGMENT 16384
 #define CGCONV_SEQ_STATES 32
 #define CGCONV_SEQ_WIDTH 8
+#define CGCONV_SEQ_KEY_DIM 128
 
 cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states);
 void cgconv_seq_plan_destroy(cgconv_seq_plan_t plan); /* NULL is a no-op */
@@ -523,6 +524,46 @@ int cgconv_seq_scan_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
                              const int32_t* lengths, const void* grad_y, void* grad_x, void* grad_delta,
                              float* grad_A, void* grad_Bt, void* grad_Ct, float* grad_D, float* grad_delta_bias,
                              hipStream_t stream);
+
+/*
+ * Gated delta rule: a memory per head that the keys write and the queries read.
+ * A plan of cgconv_seq_plan_create_rule is a sequence plan (states as there) whose
+ * C channels are `heads` heads of P = C / heads channels of every component;
+ * key_heads divides heads, head h reads key head h key_heads / heads; keys are of
+ * key_dim = D, 1..CGCONV_SEQ_KEY_DIM; batch * heads <= 65535.  backward != 0: with the
+ * backward's workspace (the states and values of all chunks of 64 tokens), else
+ * cgconv_seq_delta_rule_backward is refused.  Per head, S [D][K][P] in fp32:
+ *
+ *   kn = k / sqrt(|k|^2 + 1e-6), qn alike (normalize = 0: k and q as they are)
+ *   u_t = beta_t (v_t - exp(decay_t) S_{t-1}^T kn_t)
+ *   S_t = exp(decay_t) S_{t-1} + kn_t u_t^T,   y_t = scale S_t^T qn_t
+ *
+ * Keys, queries, decays and betas are invariants, so it commutes with rotations.
+ * q, k [batch][N][key_heads][D] and v, y [batch][N][K][C] of dtype; decay (a
+ * logarithm; one below -1000 counts as -1000, its factor is zero) and beta
+ * [batch][N][heads], fp32.  With keys of norm 1, decays that are not positive and
+ * betas in 0..2 the state stays bounded.  lengths as for the convolution.  state_in
+ * [batch][D][K][C] (or NULL: zeros) is the state before the first token, state_out
+ * (or NULL) receives the one after every sequence's last token.
+ * cgconv_seq_delta_rule_step: one token of every sequence (q, k [batch][key_heads][D],
+ * v, y [batch][K][C], decay, beta [batch][heads]), the state in place.  The backward
+ * takes the gradients of y and of the final state (or NULL: zeros); any of its outputs
+ * may be NULL, not all; tokens behind a length get zeros.  All sums have a fixed order.
+ */
+cgconv_seq_plan_t cgconv_seq_plan_create_rule(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states,
+                                              int32_t heads, int32_t key_heads, int32_t key_dim, int32_t backward);
+int cgconv_seq_delta_rule(cgconv_seq_plan_t plan, int32_t dtype, const void* q, const void* k, const void* v,
+                          const float* decay, const float* beta, float scale, int32_t normalize,
+                          const int32_t* lengths, const float* state_in, void* y, float* state_out,
+                          hipStream_t stream);
+int cgconv_seq_delta_rule_step(cgconv_seq_plan_t plan, int32_t dtype, const void* q, const void* k, const void* v,
+                               const float* decay, const float* beta, float scale, int32_t normalize, float* state,
+                               void* y, hipStream_t stream);
+int cgconv_seq_delta_rule_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* q, const void* k, const void* v,
+                                   const float* decay, const float* beta, float scale, int32_t normalize,
+                                   const int32_t* lengths, const float* state_in, const void* grad_y,
+                                   const float* grad_state, void* grad_q, void* grad_k, void* grad_v,
+                                   float* grad_decay, float* grad_beta, float* grad_state_in, hipStream_t stream);
 
 /*
  * Activation checkpoint in 8 bits of `rows` rows of C channels: codes int8

@@ -19,21 +19,27 @@ from . import sequence
 from .sequence import (  # noqa: F401
     CGCONV_BF16,
     CGCONV_F32,
+    CGCONV_SEQ_KEY_DIM,
     CGCONV_SEQ_SEGMENT,
     CGCONV_SEQ_STATES,
     CGCONV_SEQ_TOKENS,
     CGCONV_SEQ_VALUES,
     CGCONV_SEQ_WIDTH,
     SequencePlan,
+    cgconv_delta_rule,
     cgconv_norm,
     cgconv_pack8,
     cgconv_scan,
     cgconv_seq_conv,
     cgconv_seq_conv_backward,
     cgconv_seq_conv_step,
+    cgconv_seq_delta_rule,
+    cgconv_seq_delta_rule_backward,
+    cgconv_seq_delta_rule_step,
     cgconv_seq_norm,
     cgconv_seq_norm_backward,
     cgconv_seq_plan_create,
+    cgconv_seq_plan_create_rule,
     cgconv_seq_plan_destroy,
     cgconv_seq_plan_info,
     cgconv_seq_scan,

@@ -1,0 +1,315 @@
+// Device helpers and the workspace of the gated delta rule (delta_rule.hip,
+// delta_rule_bwd.hip).
+//
+// Products in 32 bits on the bfloat16 matrix cores: a float is the sum of three
+// bfloat16, x = h + m + l, each the leading 8 bits of what is left (24 bits in
+// all: exact, but for parts below the smallest normal).  Of the nine products of
+// two such sums the three smallest, up to 2^-24 of the result, are left out; a
+// bfloat16 operand is its own first part, and nothing is left out.  An output's
+// error is then that of sums in 32 bits.  Six v_mfma_f32_16x16x32_bf16 take 96
+// cycles where the fp32 instructions of the same product take 256.
+//
+// Lanes: m = lane & 15, q = lane >> 4.  Accumulators hold column m, rows 4 q .. 4 q + 3
+// of a 16 x 16 tile.  The order of the products' inner index is free as long as
+// both operands keep to it: element e of lane group q is index 4 q + e (e < 4) of
+// the first 16 and 4 q + e - 4 of the second 16, so two accumulator tiles one
+// below the other are an operand of the next product as they are.
+#pragma once
+
+#include "seq_common.h"
+
+namespace cgconv {
+namespace ruledev {
+
+using namespace seqdev;
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int kT = kRuleChunk;          // tokens of a chunk: four tiles of 16
+constexpr int kTiles = kT / 16;
+constexpr int kBlocks = kRuleTriangle;  // 16 x 16 blocks on and below the diagonal of kT x kT
+__host__ __device__ constexpr int block_of(int i, int j) { return i * (i + 1) / 2 + j; }
+
+// Parts of an operand of storage type T.
+template <class T>
+constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+
+// Eight values of one lane (one part).
+union Frag {
+  uint32_t w[4];
+  uint2 h[2];
+  v8bf f;
+};
+
+__device__ __forceinline__ uint32_t top_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+}
+__device__ __forceinline__ float without_top(float x) {
+  return x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+}
+// The parts of two values, each pair in one word.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& h, uint32_t& m, uint32_t& l) {
+  h = top_halves(a, b);
+  a = without_top(a);
+  b = without_top(b);
+  m = top_halves(a, b);
+  l = top_halves(without_top(a), without_top(b));
+}
+__device__ __forceinline__ void split8(const float (&x)[8], Frag (&f)[3]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) split2(x[2 * e], x[2 * e + 1], f[0].w[e], f[1].w[e], f[2].w[e]);
+}
+__device__ __forceinline__ void split_tiles(const v4f& a, const v4f& b, Frag (&f)[3]) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  split8(x, f);
+}
+// Values of storage type T widened to x: exact in its own parts.
+template <class T>
+__device__ __forceinline__ void parts8(const float (&x)[8], Frag (&f)[kParts<T>]) {
+  if constexpr (kParts<T> == 3) {
+    split8(x, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[0].w[e] = top_halves(x[2 * e], x[2 * e + 1]);
+  }
+}
+
+// acc += A B, the smallest products first.
+template <int NA, int NB>
+__device__ __forceinline__ v4f mma(const Frag (&a)[NA], const Frag (&b)[NB], v4f acc) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int p = 0; p < NA; ++p)
+      if (s - p >= 0 && s - p < NB)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[p].f, b[s - p].f, acc, 0, 0, 0);
+  return acc;
+}
+
+// Eight elements of a row from p on, n of them there (any n), zeros behind.
+template <class T>
+__device__ __forceinline__ void row8(const T* p, int n, float (&x)[8]) {
+  Raw<T, 8> raw;
+  raw.template load_part<true>(p, n);
+  raw.widen_to(x);
+}
+
+// Rows of 64 tokens in LDS, one array a part.  Row stride in elements: 8 bytes
+// beyond a multiple of 32 banks' words, so that 16 rows at one column take 32 banks.
+constexpr int row_stride(int KB) { return 32 * KB + 4; }
+
+__device__ __forceinline__ uint2 lds2(const bf16* p) { return *reinterpret_cast<const uint2*>(p); }
+
+// Operand with rows 16 i + m of a row-major array, inner index 32 kb + ...
+template <int NP, int ST>
+__device__ __forceinline__ void rows_frag(const bf16 (&buf)[NP][kT * ST], int i, int kb, int m, int q, Frag (&f)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const bf16* at = buf[p] + (16 * i + m) * ST + 32 * kb + 4 * q;
+    f[p].h[0] = lds2(at);
+    f[p].h[1] = lds2(at + 16);
+  }
+}
+
+// Operand with rows (columns of the array) 16 i + m, whose inner index is the
+// array's row 32 kb + ...: transposed reads, the 16 lanes of a group fetch four
+// rows of 16 elements and get a column of them each.
+template <int NP, int ST>
+__device__ __forceinline__ void columns_frag(const bf16 (&buf)[NP][kT * ST], int i, int kb, int m, int q,
+                                             Frag (&f)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16* at = buf[p] + (32 * kb + 16 * half + 4 * q + (m >> 2)) * ST + 16 * i + 4 * (m & 3);
+      const v4s t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at);
+      __builtin_memcpy(&f[p].h[half], &t, 8);
+    }
+}
+
+// Triangle blocks in LDS, a lane's four values of a block in 8 bytes a part; block
+// (i, j) holds rows i, or of the transposed triangle rows j.
+typedef uint2 TriangleParts[3][kBlocks][64];
+__device__ __forceinline__ void put_block(TriangleParts& t, int block, int lane, float x, float y, float z, float w) {
+  uint2 h, m, l;
+  split2(x, y, h.x, m.x, l.x);
+  split2(z, w, h.y, m.y, l.y);
+  t[0][block][lane] = h;
+  t[1][block][lane] = m;
+  t[2][block][lane] = l;
+}
+// Rows 16 i + m, inner index 32 kb + ... of the lower triangle; UPPER: of its transpose.
+template <bool UPPER>
+__device__ __forceinline__ void triangle_frag(const TriangleParts& t, int i, int kb, int lane, Frag (&f)[3]) {
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int j = 2 * kb + half;
+      if (UPPER ? j >= i : j <= i)
+        f[p].h[half] = t[p][UPPER ? block_of(j, i) : block_of(i, j)][lane];
+      else
+        f[p].h[half] = make_uint2(0, 0);
+    }
+}
+template <bool UPPER>
+__device__ __forceinline__ constexpr bool triangle_has(int i, int kb) {
+  return UPPER ? 2 * kb + 1 >= i : 2 * kb <= i;
+}
+
+// The numbers of a token that its chunk's kernels need, made by rule_prepare_kernel:
+// x = beta, y = rk e^G, z = rk e^(G_end - G), w = scale rq e^G with G the sum of the
+// decays of the chunk up to the token, rk and rq the factors that norm key and query.
+// Second: x = rk, y = rq, z + w = G.
+struct Token {
+  float4 a, b;
+};
+__device__ __forceinline__ float decay_between(const float4& i, const float4& j) {
+  return __expf((i.z - j.z) + (i.w - j.w));
+}
+
+// A head's column (component, channel) in a token's row; columns past V: none.
+struct Column {
+  int at;
+  bool there;
+  __device__ __forceinline__ Column(int col, int V, int P, int C, int h) {
+    there = col < V;
+    const int k = there ? col / P : 0;
+    at = k * C + h * P + (there ? col - k * P : 0);
+  }
+};
+
+// Loads on the way from global memory to LDS or to the products, a chunk ahead of their
+// use.  They are not masked, which would take a branch and a wait each: what is not there
+// is read from a place that is, and left out where the values are used.
+
+// A chunk's key or query rows, tokens >= 1 of them.
+template <class T, int KB>
+struct RowStage {
+  Raw<T, 8> raw[KB];
+  __device__ __forceinline__ void load(const T* base, int stride, int tokens, int D, int tid) {
+    if (D % 8 == 0) {
+#pragma unroll
+      for (int p = 0; p < KB; ++p) {
+        const int at = p * 256 + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
+        raw[p].load(base + (uint32_t)(min(row, tokens - 1) * stride + (c < D ? c : 0)));
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < KB; ++p) {
+        const int at = p * 256 + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
+        const T* from = base + (uint32_t)(min(row, tokens - 1) * stride);
+        T t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = from[min(c + e, D - 1)];
+        __builtin_memcpy(raw[p].w, t, sizeof t);
+      }
+    }
+  }
+  template <int NP, int N>
+  __device__ __forceinline__ void store(bf16 (&buf)[NP][N], int tokens, int D, int tid) const {
+    constexpr int ST = row_stride(KB);
+#pragma unroll
+    for (int p = 0; p < KB; ++p) {
+      const int at = p * 256 + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
+      const int n = row < tokens ? D - c : 0;
+      Frag f[NP];
+      if constexpr (NP == 1) {
+        __builtin_memcpy(&f[0], raw[p].w, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          f[0].w[e] = n >= 2 * e + 2 ? f[0].w[e] : n > 2 * e ? f[0].w[e] & 0xFFFFu : 0u;
+      } else {
+        float x[8];
+        raw[p].widen_to(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < n ? x[e] : 0.f;
+        split8(x, f);
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        uint2* to = reinterpret_cast<uint2*>(buf[i] + row * ST + c);
+        to[0] = f[i].h[0];
+        to[1] = f[i].h[1];
+      }
+    }
+  }
+};
+
+// Blocks of a triangle: 640 quadruples for 256 threads.
+struct BlockStage {
+  float4 v[3];
+  __device__ __forceinline__ void load(const float4* base, int tid) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p) v[p] = base[min(p * 256 + tid, kBlocks * 64 - 1)];
+  }
+  __device__ __forceinline__ void store(TriangleParts& t, int tid) const {
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      const int at = p * 256 + tid;
+      if (at < kBlocks * 64) put_block(t, at >> 6, at & 63, v[p].x, v[p].y, v[p].z, v[p].w);
+    }
+  }
+};
+
+// The 16 values of a lane's column in a chunk: tokens 16 i + 4 q + r.
+template <class T>
+struct ColumnStage {
+  T v[kTiles][4];
+  __device__ __forceinline__ void load(const T* base, int stride, int tokens, const Column& c, int q) {
+    if (tokens >= kT) {
+      const uint32_t at = 4 * q * stride + c.at;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[i][r] = (base + (uint32_t)((16 * i + r) * stride))[at];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          v[i][r] = base[(uint32_t)(min(16 * i + 4 * q + r, tokens - 1) * stride + c.at)];
+    }
+  }
+  __device__ __forceinline__ float get(int i, int r, int tokens, const Column& c, int q) const {
+    return c.there && 16 * i + 4 * q + r < tokens ? widen(v[i][r]) : 0.f;
+  }
+};
+
+// The same 16 values to a tensor of N tokens, the first `left` of them from the chunk's first
+// on; zeros from `tokens` on.
+template <class T>
+__device__ __forceinline__ void store_column(T* base, int stride, int left, int tokens, const Column& c, int q,
+                                             const v4f (&x)[kTiles]) {
+  if (!c.there) return;
+  const uint32_t at = 4 * q * stride + c.at;
+  if (tokens >= kT) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) (base + (uint32_t)((16 * i + r) * stride))[at] = (T)x[i][r];
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = 16 * i + 4 * q + r;
+      if (t < left) (base + (uint32_t)((16 * i + r) * stride))[at] = t < tokens ? (T)x[i][r] : (T)0.f;
+    }
+}
+
+// Accumulator tiles one below the other to rows of a workspace array, `at` the lane's place
+// in the first.
+template <int TILES>
+__device__ __forceinline__ void store_tiles(float* base, int stride, uint32_t at, const v4f (&x)[TILES]) {
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) (base + (uint32_t)((16 * i + r) * stride))[at] = x[i][r];
+}
+
+}  // namespace ruledev
+}  // namespace cgconv

@@ -1,0 +1,52 @@
+// Workspace of the gated delta rule: unit = (sequence, head), chunk by chunk.
+#pragma once
+
+#include "seq.h"
+
+namespace cgconv {
+
+struct RuleWs {
+  float4* token;   // [unit][chunk][64][2]: see Token in rule_common.h
+  float* whole;    // [unit][chunk]: decay of the whole chunk
+  float4* inv;     // [unit][chunk][10 blocks][64 lanes]: (1 + A)^-1, rows
+  float4* invT;    // the same, columns (backward)
+  float* state;    // [unit][chunk][DP][VP]: the state before every chunk (backward)
+  float* gstate;   // [unit][chunk][DP][VP]: gradient of the state after every chunk
+  float* value;    // [unit][chunk][64][VP]: what the tokens write, V'
+  float* gvalue;   // [unit][chunk][64][VP]: its gradient through (1 + A)^-T, dY
+  int units, chunks, KB, V, VP;  // DP = 32 KB; VP: V in whole tiles of 32
+};
+
+inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size_t* bytes) {
+  RuleWs w{};
+  w.units = n.B * n.H;
+  w.chunks = (n.N + kRuleChunk - 1) / kRuleChunk;
+  w.KB = (n.D + 31) / 32;
+  w.V = n.K * (n.C / n.H);
+  w.VP = (w.V + 31) / 32 * 32;
+  const size_t count = (size_t)w.units * w.chunks;
+  size_t at = 0;
+  const auto take = [&](auto*& p, size_t n) {
+    p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
+    at += (n * sizeof(*p) + 255) / 256 * 256;
+  };
+  take(w.token, count * kRuleChunk * 2);
+  take(w.whole, count);
+  take(w.inv, count * kRuleTriangle * 64);
+  if (backward) {
+    take(w.invT, count * kRuleTriangle * 64);
+    take(w.state, count * 32 * w.KB * w.VP);
+    take(w.gstate, count * 32 * w.KB * w.VP);
+    take(w.value, count * kRuleChunk * w.VP);
+    take(w.gvalue, count * kRuleChunk * w.VP);
+  }
+  if (bytes) *bytes = at;
+  return w;
+}
+
+// (1 + A)^-1 and the numbers of every token, of all chunks at once.
+hipError_t launch_rule_prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
+// The states from chunk to chunk; for the backward they and V' are kept and no output is formed.
+hipError_t launch_rule_states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
+
+}  // namespace cgconv

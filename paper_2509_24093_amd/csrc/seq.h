@@ -1,7 +1,7 @@
 // Internal interface between the sequence plan (sequence.cpp) and its kernels:
 // layer norm by degree (norm.hip), 8-bit checkpoints (pack.hip), the short
-// causal convolution (conv.hip) and the selective scan (scan.hip,
-// scan_bwd.hip).  Features x, y are [B][N][K][C], channel fastest, in fp32 or
+// causal convolution (conv.hip), the selective scan (scan.hip, scan_bwd.hip) and
+// the gated delta rule (delta_rule.hip, delta_rule_bwd.hip).  Features x, y are [B][N][K][C], channel fastest, in fp32 or
 // bfloat16; parameters, states and statistics are fp32.
 #pragma once
 
@@ -135,5 +135,48 @@ hipError_t launch_scan_step(const ScanArgs& a, hipStream_t s);
 hipError_t launch_scan_backward(const ScanBwdArgs& g, hipStream_t s);
 // workspace of both directions
 size_t scan_workspace_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
+
+// ---- gated delta rule ---------------------------------------------------------------
+
+constexpr int kRuleMaxDim = 128;   // key width
+constexpr float kRuleNormEps = 1e-6f;  // under the root of a key's norm
+constexpr int kRuleChunk = 64;     // tokens whose products are formed at once
+constexpr int kRuleTriangle = 10;  // 16 x 16 blocks on and below the diagonal of a chunk
+
+struct RuleSizes {
+  int B, N, K, C;  // C = H P: P channels of every component a head
+  int H, Hk, D;    // heads, key heads (Hk divides H), key width
+};
+struct RuleArgs {
+  int type;
+  RuleSizes n;
+  const void* q;       // [B][N][Hk][D] (a step: [B][Hk][D])
+  const void* k;
+  const void* v;       // [B][N][K][C]
+  const float* decay;  // [B][N][H], logarithms
+  const float* beta;   // [B][N][H]
+  const int* lengths;  // [B] or nullptr
+  const float* state_in;  // [B][D][K][C] or nullptr (zeros)
+  void* y;
+  float* state_out;  // or nullptr; a step's state, in place
+  float scale;
+  int normalize;
+  char* ws;  // rule_workspace_bytes
+};
+struct RuleBwdArgs {
+  RuleArgs a;  // y and state_out unused
+  const void* gy;
+  const float* gstate;  // [B][D][K][C] or nullptr (zeros)
+  void* gq;             // any may be nullptr
+  void* gk;
+  void* gv;
+  float* gdecay;
+  float* gbeta;
+  float* gstate_in;
+};
+hipError_t launch_rule(const RuleArgs& a, hipStream_t s);
+hipError_t launch_rule_step(const RuleArgs& a, hipStream_t s);
+hipError_t launch_rule_backward(const RuleBwdArgs& g, hipStream_t s);
+size_t rule_workspace_bytes(const RuleSizes& n, bool backward);
 
 }  // namespace cgconv

@@ -1,7 +1,7 @@
 // Sequence plan and the entry points of the operators around the convolution
 // (see include/cgconv.h, "Sequence operators"): checks of arguments, the
 // plan's workspace, launches.  Kernels: norm.hip, pack.hip, conv.hip, scan.hip,
-// scan_bwd.hip.
+// scan_bwd.hip, delta_rule.hip, delta_rule_bwd.hip.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,6 +16,8 @@ using namespace cgconv;
 struct cgconv_seq_plan {
   int64_t B = 0, N = 0, C = 0;
   int L = 0, K = 0, S = 0;
+  int H = 0, Hk = 0, D = 0;     // the delta rule's heads, key heads and key width; H = 0: none
+  bool rule_backward = false;   // its backward's workspace is there
   int device = 0;
   size_t ws_bytes = 0;
   void* ws = nullptr;
@@ -95,11 +97,12 @@ int launched(hipError_t e) {
   return CGCONV_ERR_HIP;
 }
 
-}  // namespace
+RuleSizes rule_sizes(const cgconv_seq_plan* p) {
+  return {(int)p->B, (int)p->N, p->K, (int)p->C, p->H, p->Hk, p->D};
+}
 
-extern "C" {
-
-cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states) {
+cgconv_seq_plan* create_plan(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states, int32_t heads,
+                             int32_t key_heads, int32_t key_dim, bool rule_backward) {
   clear_last_error();
   if (batch < 1 || batch > 65535 || N < 1 || C < 1 || states < 0) {
     set_last_error("invalid sizes: batch=%lld N=%lld C=%lld states=%d (need 1 <= batch <= 65535, N >= 1, C >= 1, "
@@ -139,6 +142,10 @@ cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max
   p->L = L_max;
   p->K = K;
   p->S = states;
+  p->H = heads;
+  p->Hk = key_heads;
+  p->D = key_dim;
+  p->rule_backward = rule_backward;
   hipError_t e = hipGetDevice(&p->device);
   if (e != hipSuccess) {
     set_last_error("hipGetDevice failed: %s", hipGetErrorString(e));
@@ -147,6 +154,7 @@ cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max
   }
   p->ws_bytes = std::max(norm_bwd_part_bytes(batch * N, L_max, (int)C), conv_bwd_part_bytes(batch, N, K, C));
   if (states) p->ws_bytes = std::max(p->ws_bytes, scan_workspace_bytes(batch, N, K, C, states));
+  if (heads) p->ws_bytes = std::max(p->ws_bytes, rule_workspace_bytes(rule_sizes(p), rule_backward));
   if ((e = hipMalloc(&p->ws, p->ws_bytes)) != hipSuccess) {
     set_last_error("workspace allocation of %zu bytes failed: %s", p->ws_bytes, hipGetErrorString(e));
     (void)hipGetLastError();
@@ -154,6 +162,37 @@ cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max
     return nullptr;
   }
   return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+cgconv_seq_plan_t cgconv_seq_plan_create(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states) {
+  return create_plan(batch, N, L_max, C, states, 0, 0, 0, false);
+}
+
+cgconv_seq_plan_t cgconv_seq_plan_create_rule(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states,
+                                              int32_t heads, int32_t key_heads, int32_t key_dim, int32_t backward) {
+  clear_last_error();
+  if (heads < 1 || key_heads < 1 || key_dim < 1) {
+    set_last_error("invalid sizes: heads=%d key_heads=%d key_dim=%d (need at least 1 each)", heads, key_heads, key_dim);
+    return nullptr;
+  }
+  if (C % heads != 0 || heads % key_heads != 0) {
+    set_last_error("invalid sizes: C=%lld must be a multiple of heads=%d, heads a multiple of key_heads=%d",
+                   (long long)C, heads, key_heads);
+    return nullptr;
+  }
+  if (key_dim > CGCONV_SEQ_KEY_DIM) {
+    set_last_error("unsupported key_dim=%d: at most %d", key_dim, CGCONV_SEQ_KEY_DIM);
+    return nullptr;
+  }
+  if (batch >= 1 && batch > 65535 / heads) {
+    set_last_error("unsupported batch*heads: at most 65535");
+    return nullptr;
+  }
+  return create_plan(batch, N, L_max, C, states, heads, key_heads, key_dim, backward != 0);
 }
 
 void cgconv_seq_plan_destroy(cgconv_seq_plan_t plan) {
@@ -458,6 +497,132 @@ int cgconv_seq_scan_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
   g.gD = grad_D;
   g.gbias = grad_delta_bias;
   return launched(launch_scan_backward(g, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_rule_plan(const cgconv_seq_plan* p, int32_t dtype) {
+  const int st = check_plan(p, dtype);
+  if (st == CGCONV_OK && p->H == 0) {
+    set_last_error("the plan has no delta rule (cgconv_seq_plan_create_rule)");
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  return st;
+}
+
+RuleArgs rule_args(const cgconv_seq_plan* p, int32_t dtype, const void* q, const void* k, const void* v,
+                   const float* decay, const float* beta, float scale, int32_t normalize, const int32_t* lengths) {
+  RuleArgs a{};
+  a.type = dtype;
+  a.n = rule_sizes(p);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.decay = decay;
+  a.beta = beta;
+  a.lengths = lengths;
+  a.scale = scale;
+  a.normalize = normalize != 0;
+  a.ws = static_cast<char*>(p->ws);
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int cgconv_seq_delta_rule(cgconv_seq_plan_t plan, int32_t dtype, const void* q, const void* k, const void* v,
+                          const float* decay, const float* beta, float scale, int32_t normalize,
+                          const int32_t* lengths, const float* state_in, void* y, float* state_out,
+                          hipStream_t stream) {
+  int st = check_rule_plan(plan, dtype);
+  if (st != CGCONV_OK) return st;
+  const size_t ts = seq_type_size(dtype), tokens = plan->B * plan->N, row = (size_t)plan->K * plan->C;
+  const size_t keys = tokens * plan->Hk * plan->D * ts, gates = tokens * plan->H * 4, state = plan->B * plan->D * row * 4;
+  const Arg args[] = {{"q", q, keys, true, false},
+                      {"k", k, keys, true, false},
+                      {"v", v, tokens * row * ts, true, false},
+                      {"decay", decay, gates, true, false},
+                      {"beta", beta, gates, true, false},
+                      {"lengths", lengths, (size_t)plan->B * 4, false, false},
+                      {"state_in", state_in, state, false, false},
+                      {"y", y, tokens * row * ts, true, true},
+                      {"state_out", state_out, state, false, true}};
+  if ((st = check_arrays(args, 9)) != CGCONV_OK) return st;
+  RuleArgs a = rule_args(plan, dtype, q, k, v, decay, beta, scale, normalize, lengths);
+  a.state_in = state_in;
+  a.y = y;
+  a.state_out = state_out;
+  return launched(launch_rule(a, stream));
+}
+
+int cgconv_seq_delta_rule_step(cgconv_seq_plan_t plan, int32_t dtype, const void* q, const void* k, const void* v,
+                               const float* decay, const float* beta, float scale, int32_t normalize, float* state,
+                               void* y, hipStream_t stream) {
+  int st = check_rule_plan(plan, dtype);
+  if (st != CGCONV_OK) return st;
+  const size_t ts = seq_type_size(dtype), B = plan->B, row = (size_t)plan->K * plan->C;
+  const Arg args[] = {{"q", q, B * plan->Hk * plan->D * ts, true, false},
+                      {"k", k, B * plan->Hk * plan->D * ts, true, false},
+                      {"v", v, B * row * ts, true, false},
+                      {"decay", decay, B * plan->H * 4, true, false},
+                      {"beta", beta, B * plan->H * 4, true, false},
+                      {"state", state, B * plan->D * row * 4, true, true},
+                      {"y", y, B * row * ts, true, true}};
+  if ((st = check_arrays(args, 7)) != CGCONV_OK) return st;
+  RuleArgs a = rule_args(plan, dtype, q, k, v, decay, beta, scale, normalize, nullptr);
+  a.y = y;
+  a.state_out = state;
+  return launched(launch_rule_step(a, stream));
+}
+
+int cgconv_seq_delta_rule_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* q, const void* k, const void* v,
+                                   const float* decay, const float* beta, float scale, int32_t normalize,
+                                   const int32_t* lengths, const float* state_in, const void* grad_y,
+                                   const float* grad_state, void* grad_q, void* grad_k, void* grad_v,
+                                   float* grad_decay, float* grad_beta, float* grad_state_in, hipStream_t stream) {
+  int st = check_rule_plan(plan, dtype);
+  if (st != CGCONV_OK) return st;
+  if (!plan->rule_backward) {
+    set_last_error("the plan has no workspace for the delta rule's backward (cgconv_seq_plan_create_rule with backward)");
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  if (!grad_q && !grad_k && !grad_v && !grad_decay && !grad_beta && !grad_state_in) {
+    set_last_error("at least one gradient must be given");
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  const size_t ts = seq_type_size(dtype), tokens = plan->B * plan->N, row = (size_t)plan->K * plan->C;
+  const size_t keys = tokens * plan->Hk * plan->D * ts, gates = tokens * plan->H * 4, state = plan->B * plan->D * row * 4;
+  const Arg args[] = {{"q", q, keys, true, false},
+                      {"k", k, keys, true, false},
+                      {"v", v, tokens * row * ts, true, false},
+                      {"decay", decay, gates, true, false},
+                      {"beta", beta, gates, true, false},
+                      {"lengths", lengths, (size_t)plan->B * 4, false, false},
+                      {"state_in", state_in, state, false, false},
+                      {"grad_y", grad_y, tokens * row * ts, true, false},
+                      {"grad_state", grad_state, state, false, false},
+                      {"grad_q", grad_q, keys, false, true},
+                      {"grad_k", grad_k, keys, false, true},
+                      {"grad_v", grad_v, tokens * row * ts, false, true},
+                      {"grad_decay", grad_decay, gates, false, true},
+                      {"grad_beta", grad_beta, gates, false, true},
+                      {"grad_state_in", grad_state_in, state, false, true}};
+  if ((st = check_arrays(args, 15)) != CGCONV_OK) return st;
+  RuleBwdArgs g{};
+  g.a = rule_args(plan, dtype, q, k, v, decay, beta, scale, normalize, lengths);
+  g.a.state_in = state_in;
+  g.gy = grad_y;
+  g.gstate = grad_state;
+  g.gq = grad_q;
+  g.gk = grad_k;
+  g.gv = grad_v;
+  g.gdecay = grad_decay;
+  g.gbeta = grad_beta;
+  g.gstate_in = grad_state_in;
+  return launched(launch_rule_backward(g, stream));
 }
 
 static int check_pack(int32_t dtype, int64_t rows, int64_t C) {

@@ -8,6 +8,7 @@ library's HIP kernels; this module checks and marshals arguments.
 from __future__ import annotations
 
 import ctypes
+import math
 
 CGCONV_F32 = 0
 CGCONV_BF16 = 1
@@ -16,6 +17,7 @@ CGCONV_SEQ_VALUES = 1 << 38
 CGCONV_SEQ_SEGMENT = 16384
 CGCONV_SEQ_STATES = 32
 CGCONV_SEQ_WIDTH = 8
+CGCONV_SEQ_KEY_DIM = 128
 
 _vp, _i64, _i32, _f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
 
@@ -32,6 +34,10 @@ SIGNATURES = {
     "cgconv_seq_scan": ([_vp, _i32] + [_vp] * 12, ctypes.c_int),
     "cgconv_seq_scan_step": ([_vp, _i32] + [_vp] * 10, ctypes.c_int),
     "cgconv_seq_scan_backward": ([_vp, _i32] + [_vp] * 17, ctypes.c_int),
+    "cgconv_seq_plan_create_rule": ([_i64, _i64, _i32, _i64] + [_i32] * 5, _vp),
+    "cgconv_seq_delta_rule": ([_vp, _i32] + [_vp] * 5 + [_f32, _i32] + [_vp] * 5, ctypes.c_int),
+    "cgconv_seq_delta_rule_step": ([_vp, _i32] + [_vp] * 5 + [_f32, _i32] + [_vp] * 3, ctypes.c_int),
+    "cgconv_seq_delta_rule_backward": ([_vp, _i32] + [_vp] * 5 + [_f32, _i32] + [_vp] * 11, ctypes.c_int),
     "cgconv_pack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
     "cgconv_unpack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
 }
@@ -54,6 +60,15 @@ def _main():
 def cgconv_seq_plan_create(batch: int, N: int, L_max: int, C: int, states: int = 0) -> int:
     P = _main()
     h = P.library().cgconv_seq_plan_create(batch, N, L_max, C, states)
+    if not h:
+        raise P.CgconvError(P.CGCONV_ERR_INVALID_ARG, P.cgconv_last_error())
+    return h
+
+
+def cgconv_seq_plan_create_rule(batch: int, N: int, L_max: int, C: int, states: int, heads: int, key_heads: int,
+                                key_dim: int, backward: bool = True) -> int:
+    P = _main()
+    h = P.library().cgconv_seq_plan_create_rule(batch, N, L_max, C, states, heads, key_heads, key_dim, int(backward))
     if not h:
         raise P.CgconvError(P.CGCONV_ERR_INVALID_ARG, P.cgconv_last_error())
     return h
@@ -124,6 +139,29 @@ def cgconv_seq_scan_backward(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, le
     return P._check(P.library().cgconv_seq_scan_backward(plan, dtype, x, delta, A, Bt, Ct, D, delta_bias, lengths,
                                                          grad_y, grad_x, grad_delta, grad_A, grad_Bt, grad_Ct, grad_D,
                                                          grad_delta_bias, stream))
+
+
+def cgconv_seq_delta_rule(plan, dtype, q, k, v, decay, beta, scale, normalize, lengths, state_in, y, state_out,
+                          stream) -> int:
+    """Gated delta rule (lengths and the states may be None)."""
+    P = _main()
+    return P._check(P.library().cgconv_seq_delta_rule(plan, dtype, q, k, v, decay, beta, scale, normalize, lengths,
+                                                      state_in, y, state_out, stream))
+
+
+def cgconv_seq_delta_rule_step(plan, dtype, q, k, v, decay, beta, scale, normalize, state, y, stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_delta_rule_step(plan, dtype, q, k, v, decay, beta, scale, normalize, state,
+                                                           y, stream))
+
+
+def cgconv_seq_delta_rule_backward(plan, dtype, q, k, v, decay, beta, scale, normalize, lengths, state_in, grad_y,
+                                   grad_state, grad_q, grad_k, grad_v, grad_decay, grad_beta, grad_state_in,
+                                   stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_delta_rule_backward(plan, dtype, q, k, v, decay, beta, scale, normalize,
+                                                               lengths, state_in, grad_y, grad_state, grad_q, grad_k,
+                                                               grad_v, grad_decay, grad_beta, grad_state_in, stream))
 
 
 def cgconv_pack8(dtype, rows, C, x, codes, scales, stream) -> int:
@@ -253,18 +291,29 @@ def kept(ctx):
 class SequencePlan:
     """Sizes and workspace of the sequence operators for features
     [batch, N, (L_max+1)^2, C] (fp32 or bf16) on the current GPU; states: S of
-    the selective scan (0: no scans, a smaller workspace)."""
+    the selective scan (0: no scans, a smaller workspace).  heads, key_heads
+    (default: heads) and key_dim: of the gated delta rule (0: none), with the
+    workspace of its backward unless backward is False."""
 
-    def __init__(self, batch: int, N: int, L_max: int, C: int, states: int = 0):
+    def __init__(self, batch: int, N: int, L_max: int, C: int, states: int = 0, heads: int = 0, key_heads: int = None,
+                 key_dim: int = 0, backward: bool = True):
         import torch
         self._h = None
-        self._h = cgconv_seq_plan_create(int(batch), int(N), int(L_max), int(C), int(states))
+        self.heads, self.key_dim = int(heads), int(key_dim)
+        self.key_heads = self.heads if key_heads is None else int(key_heads)
+        if self.heads or self.key_heads or self.key_dim:
+            self._h = cgconv_seq_plan_create_rule(int(batch), int(N), int(L_max), int(C), int(states), self.heads,
+                                                  self.key_heads, self.key_dim, bool(backward))
+        else:
+            self._h = cgconv_seq_plan_create(int(batch), int(N), int(L_max), int(C), int(states))
         self._lib = _main().library()
         self.device = torch.cuda.current_device()
         self.batch, self.N, self.L_max, self.C, self.states = int(batch), int(N), int(L_max), int(C), int(states)
         self.shape = (self.batch, self.N, (self.L_max + 1) ** 2, self.C)
         self.token_shape = (self.batch,) + self.shape[2:]  # of a step
         self.state_shape = (self.batch, self.states) + self.shape[2:]  # of a scan
+        self.memory_shape = (self.batch, self.key_dim) + self.shape[2:]  # of a delta rule's state
+        self._scale = 1.0 / math.sqrt(self.key_dim) if self.key_dim > 0 else 1.0
         self._on = torch.device("cuda", self.device)
         self._f32, self._empty = torch.float32, torch.empty
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -452,6 +501,63 @@ class SequencePlan:
                                                       self._raw_stream(self.device)))
         return grads
 
+    # ---- gated delta rule
+
+    def _rule_args(self, q, k, v, decay, beta, scale, normalize, lead, shape):
+        dtype, code = _features_dtype("v", v)
+        dev, f32 = self.device, self._f32
+        keys, gates = lead + (self.key_heads, self.key_dim), lead + (self.heads,)
+        return dtype, (self._h, code, _tensor("q", q, keys, dtype, dev), _tensor("k", k, keys, dtype, dev),
+                       _tensor("v", v, shape, dtype, dev), _tensor("decay", decay, gates, f32, dev),
+                       _tensor("beta", beta, gates, f32, dev), self._scale if scale is None else scale,
+                       1 if normalize else 0)
+
+    def delta_rule_state(self):
+        """The state before the first token: fp32 zeros [batch, key_dim, K, C]."""
+        return self._new(self.memory_shape, self._f32).zero_()
+
+    def delta_rule(self, q, k, v, decay, beta, scale=None, normalize: bool = True, lengths=None, state=None, out=None):
+        """Gated delta rule of whole sequences: q and k [batch, N, key_heads,
+        key_dim], v [batch, N, K, C] (head h: channels h C / heads and on), decay
+        (logarithms) and beta [batch, N, heads] in fp32; scale: 1 / sqrt(key_dim)
+        if None; normalize: q and k are taken at norm 1.  Returns (y, state): the
+        state [batch, key_dim, K, C] (fp32) after every sequence's last token, for
+        delta_rule_step or the next piece (state=)."""
+        _, args = self._rule_args(q, k, v, decay, beta, scale, normalize, self.shape[:2], self.shape)
+        pl, ps = self._lengths(lengths), _tensor("state", state, self.memory_shape, self._f32, self.device)
+        out, po = self._out(out, v, self.shape)
+        last = self._new(self.memory_shape, self._f32)
+        self._done(self._lib.cgconv_seq_delta_rule(*args, pl, ps, po, last.data_ptr(), self._raw_stream(self.device)))
+        return out, last
+
+    def delta_rule_step(self, q, k, v, decay, beta, state, scale=None, normalize: bool = True, out=None):
+        """One token of every sequence: q and k [batch, key_heads, key_dim], v
+        [batch, K, C], decay and beta [batch, heads]; state is moved on in place.
+        Returns y [batch, K, C]."""
+        _, args = self._rule_args(q, k, v, decay, beta, scale, normalize, self.shape[:1], self.token_shape)
+        ps = _tensor("state", state, self.memory_shape, self._f32, self.device)
+        out, po = self._out(out, v, self.token_shape)
+        self._done(self._lib.cgconv_seq_delta_rule_step(*args, ps, po, self._raw_stream(self.device)))
+        return out
+
+    def delta_rule_backward(self, q, k, v, decay, beta, grad_y, scale=None, normalize: bool = True, lengths=None,
+                            state=None, grad_state=None, need=(True,) * 6):
+        """Gradients of (q, k, v, decay, beta, state) given those of y and, if
+        there is one, of the final state; None where ``need`` is False."""
+        if not any(need):
+            return (None,) * 6
+        dtype, args = self._rule_args(q, k, v, decay, beta, scale, normalize, self.shape[:2], self.shape)
+        dev, f32, lead = self.device, self._f32, self.shape[:2]
+        args += (self._lengths(lengths), _tensor("state", state, self.memory_shape, f32, dev),
+                 _tensor("grad_y", grad_y, self.shape, dtype, dev),
+                 _tensor("grad_state", grad_state, self.memory_shape, f32, dev))
+        keys, gates = (lead + (self.key_heads, self.key_dim), dtype), (lead + (self.heads,), f32)
+        shapes = (keys, keys, (self.shape, dtype), gates, gates, (self.memory_shape, f32))
+        grads = tuple(self._new(*s, n) for s, n in zip(shapes, need))
+        self._done(self._lib.cgconv_seq_delta_rule_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
+                                                            self._raw_stream(dev)))
+        return grads
+
     def close(self):
         if getattr(self, "_h", None):
             cgconv_seq_plan_destroy(self._h)
@@ -578,3 +684,42 @@ def cgconv_scan(x, delta, A, Bt, Ct, D, plan: SequencePlan, delta_bias=None, len
     if "scan" not in _functions:
         _functions["scan"] = _scan_function()
     return _functions["scan"].apply(x, delta, A, Bt, Ct, D, delta_bias, lengths, plan, packed)
+
+
+def _rule_function():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _RuleFn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, decay, beta, state, lengths, plan, scale, normalize, packed):
+            y, last = plan.delta_rule(q, k, v, decay, beta, scale, normalize, lengths, state)
+            keep(ctx, packed, (v,), (q, k, decay, beta, state, lengths))
+            ctx.plan, ctx.scale, ctx.normalize = plan, scale, normalize
+            ctx.set_materialize_grads(False)
+            return y, last
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_y, grad_state):
+            (v,), (q, k, decay, beta, state, lengths) = kept(ctx)
+            grad_y = torch.zeros_like(v) if grad_y is None else _whole(grad_y)
+            grad_state = None if grad_state is None else _whole(grad_state)
+            need = tuple(n and t is not None for n, t in zip(ctx.needs_input_grad, (q, k, v, decay, beta, state)))
+            return ctx.plan.delta_rule_backward(q, k, v, decay, beta, grad_y, ctx.scale, ctx.normalize, lengths, state,
+                                                grad_state, need) + (None,) * 5
+
+    return _RuleFn
+
+
+def cgconv_delta_rule(q, k, v, decay, beta, plan: SequencePlan, scale=None, normalize: bool = True, lengths=None,
+                      state=None, return_state: bool = False, checkpoint=None):
+    """Differentiable gated delta rule (:meth:`SequencePlan.delta_rule`) in q, k,
+    v, decay, beta and state; returns y, or (y, the final state), which is then
+    differentiable too.  checkpoint="int8": v is kept for the backward pass in 8
+    bits (q, k, decay and beta whole)."""
+    packed = _want_checkpoint(checkpoint) and _grad_wanted(q, k, v, decay, beta, state)
+    if "rule" not in _functions:
+        _functions["rule"] = _rule_function()
+    y, last = _functions["rule"].apply(q, k, v, decay, beta, state, lengths, plan, scale, normalize, packed)
+    return (y, last) if return_state else y
