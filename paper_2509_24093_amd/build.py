@@ -68,6 +68,7 @@ def build(jobs: int | None = None, verbose: bool = True) -> str:
         ([HIPCC, "-c"] + HIP_FLAGS, "scan_bwd.hip", "scan_bwd.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "delta_rule.hip", "delta_rule.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "delta_rule_bwd.hip", "delta_rule_bwd.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "rule_join.hip", "rule_join.o", []),
     ]
     for P in (3, 5, 7):
         units.append(([HIPCC, "-c"] + HIP_FLAGS, "fft_odd.hip", "fft_odd_P%d.o" % P, ["-DCGCONV_TU_P=%d" % P]))

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
   }
   const long long at = (long long)unit * ws.chunks + chunk;
   for (int n = wave; n < kBlocks; n += 4) {
-    const int i = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3, j = n - block_of(i, 0);
+    const int i = row_of(n), j = n - block_of(i, 0);
     const float* p = inv + (16 * i + m) * kRow + 16 * j + 4 * q;
     ws.inv[(at * kBlocks + n) * 64 + lane] = make_float4(p[0], p[1], p[2], p[3]);
     if (TRANSPOSED) {
@@ -190,28 +190,40 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
 
 // ---- the states, chunk after chunk ------------------------------------------------------
 
-// Block (group of 64 columns, unit).  KEEP: the state before every chunk and V' are
-// written for the backward, no output is formed.
-template <class T, int KB, bool KEEP>
-__global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) {
-  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB;
-  constexpr int kQ = KEEP ? 1 : kT * ST;
+// What a walk over the chunks leaves.
+enum Walk {
+  kOutputs,  // the outputs, and the last state
+  kKeep,     // the state before every chunk and V', for the backward
+  kSpan,     // of a segment of the chunks: its last state from zero, and from every unit
+             // vector with no values written, which is the segment's matrix
+};
+
+// Block (group of 16 NW columns, unit, segment).  The columns of kSpan are the VP of the
+// values, then those of the matrix.
+template <class T, int KB, int NW, int WALK>
+__global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs ws) {
+  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, kThreads = 64 * NW;
+  constexpr bool kOut = WALK == kOutputs;
   __shared__ __attribute__((aligned(16))) bf16 kbuf[NP][kT * ST];
-  __shared__ __attribute__((aligned(16))) bf16 qbuf[KEEP ? 1 : NP][kQ];
+  __shared__ __attribute__((aligned(16))) bf16 qbuf[kOut ? NP : 1][kOut ? kT * ST : 1];
   __shared__ TriangleParts inv, inside;
   __shared__ float4 ta[kT], tb[kT];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
-  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H;
+  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int col = (blockIdx.x * 4 + wave) * 16 + m;
-  const bool active = (blockIdx.x * 4 + wave) * 16 < (KEEP ? ws.VP : ws.V);
+  const int first = (blockIdx.x * NW + wave) * 16, col = first + m;
+  const bool active = first < (kOut ? ws.V : WALK == kKeep ? ws.VP : ws.VP + 32 * KB);
+  const bool matrix = WALK == kSpan && first >= ws.VP;
   const Column column(col, ws.V, C / a.n.H, C, h);
-  const int length = tokens_of(a, b), chunks = (length + kT - 1) / kT;
+  const int length = tokens_of(a, b);
+  const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
+  const int end = min((length + kT - 1) / kT, last);
   const int stride = a.n.Hk * D;
   const T* K = static_cast<const T*>(a.k) + (long long)b * N * stride + (long long)hk * D;
   const T* Q = static_cast<const T*>(a.q) + (long long)b * N * stride + (long long)hk * D;
   const T* v = static_cast<const T*>(a.v) + (long long)b * N * KC;
-  T* y = static_cast<T*>(a.y) + (KEEP ? 0 : (long long)b * N * KC);
+  T* y = static_cast<T*>(a.y) + (kOut ? (long long)b * N * KC : 0);
+  const long long start = ((long long)unit * ws.segments + seg) * (32 * KB);  // row of a segment's state
 
   v4f S[DT];
 #pragma unroll
@@ -219,50 +231,60 @@ __global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) 
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * d + 4 * q + r;
-      S[d][r] = a.state_in && column.there && row < D ? a.state_in[((long long)b * D + row) * KC + column.at] : 0.f;
+      float x = 0.f;
+      if (WALK == kSpan) {
+        x = matrix && row == col - ws.VP ? 1.f : 0.f;
+      } else if (seg > 0) {
+        if (first < ws.VP) x = ws.start[(start + row) * ws.VP + col];
+      } else if (a.state_in && column.there && row < D) {
+        x = a.state_in[((long long)b * D + row) * KC + column.at];
+      }
+      S[d][r] = x;
     }
 
-  RowStage<T, KB> sk, sq;
-  BlockStage si;
+  RowStage<T, KB, kThreads> sk, sq;
+  BlockStage<kThreads> si;
   float4 st;
   ColumnStage<T> sv;
   const auto fetch = [&](int c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
     sk.load(K + (long long)c * kT * stride, stride, tokens, D, tid);
-    if (!KEEP) sq.load(Q + (long long)c * kT * stride, stride, tokens, D, tid);
+    if (kOut) sq.load(Q + (long long)c * kT * stride, stride, tokens, D, tid);
     si.load(ws.inv + at * kBlocks * 64, tid);
     st = ws.token[at * 2 * kT + (tid & (2 * kT - 1))];
   };
-  if (chunks > 0) {
-    fetch(0);
-    sv.load(v, KC, min(length, kT), column, q);
+  const auto fetch_values = [&](int c) {
+    sv.load(v + (long long)c * kT * KC, KC, min(length - c * kT, kT), column, q);
+  };
+  if (begin < end) {
+    fetch(begin);
+    fetch_values(begin);
   }
-  for (int c = 0; c < chunks; ++c) {
+  for (int c = begin; c < end; ++c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
     __syncthreads();  // the chunk before has been read
     sk.store(kbuf, tokens, D, tid);
-    if constexpr (!KEEP) sq.store(qbuf, tokens, D, tid);
+    if constexpr (kOut) sq.store(qbuf, tokens, D, tid);
     si.store(inv, tid);
     if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = st;
     const float whole = ws.whole[at];
     __syncthreads();
-    if (c + 1 < chunks) fetch(c + 1);
+    if (c + 1 < end) fetch(c + 1);
     // P, transposed: rows j, columns i, so that a lane has four j of its row
-    if constexpr (!KEEP) {
-#pragma unroll
-      for (int j = 0; j < kTiles; ++j) {
-        if (j > wave) continue;
+    if constexpr (kOut) {
+      for (int n = wave; n < kBlocks; n += NW) {
+        const int ib = row_of(n), j = n - block_of(ib, 0);
         v4f p{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           Frag fk[NP], fq[NP];
           rows_frag<NP, ST>(kbuf, j, kb, m, q, fk);
-          rows_frag<NP, ST>(qbuf, wave, kb, m, q, fq);
+          rows_frag<NP, ST>(qbuf, ib, kb, m, q, fq);
           p = mma(fk, fq, p);
         }
-        const int i = 16 * wave + m;
+        const int i = 16 * ib + m;
         const float4 me = tb[i];
         const float f = a.scale * me.y;
 #pragma unroll
@@ -271,14 +293,12 @@ __global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) 
           const float4 other = tb[u];
           p[r] = i >= u ? p[r] * (f * other.x) * decay_between(me, other) : 0.f;
         }
-        put_block(inside, block_of(wave, j), lane, p[0], p[1], p[2], p[3]);
+        put_block(inside, n, lane, p[0], p[1], p[2], p[3]);
       }
     }
     v4f X[kTiles], O[kTiles];
     if (active) {
-      if constexpr (KEEP) {
-        store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, 4 * q * ws.VP + col, S);
-      }
+      if constexpr (WALK == kKeep) store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, col, q, S);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) X[i] = O[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -290,7 +310,7 @@ __global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) 
           Frag f[NP];
           rows_frag<NP, ST>(kbuf, i, kb, m, q, f);
           X[i] = mma(f, s, X[i]);
-          if constexpr (!KEEP) {
+          if constexpr (kOut) {
             rows_frag<NP, ST>(qbuf, i, kb, m, q, f);
             O[i] = mma(f, s, O[i]);
           }
@@ -302,10 +322,10 @@ __global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float4 t = ta[16 * i + 4 * q + r];
-          X[i][r] = t.x * fmaf(-t.y, X[i][r], sv.get(i, r, tokens, column, q));
+          X[i][r] = t.x * fmaf(-t.y, X[i][r], sv.get(i, r, column));
           O[i][r] *= t.w;
         }
-      if (c + 1 < chunks) sv.load(v + (long long)(c + 1) * kT * KC, KC, min(length - (c + 1) * kT, kT), column, q);
+      if (c + 1 < end) fetch_values(c + 1);
       Frag fy[2][3];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fy[kb]);
@@ -321,11 +341,10 @@ __global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) 
           }
       }
     }
-    if constexpr (!KEEP) __syncthreads();  // P is there
+    if constexpr (kOut) __syncthreads();  // P is there
     if (!active) continue;
-    if constexpr (KEEP) {
-      store_tiles(ws.value + at * kT * ws.VP, ws.VP, 4 * q * ws.VP + col, X);
-    } else {
+    if constexpr (WALK == kKeep) store_tiles(ws.value + at * kT * ws.VP, ws.VP, col, q, X);
+    if constexpr (kOut) {
       Frag fv[2][3];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fv[kb]);
@@ -360,10 +379,21 @@ __global__ __launch_bounds__(256) void rule_state_kernel(RuleArgs a, RuleWs ws) 
       }
     }
   }
-  if constexpr (!KEEP) {
+  if constexpr (WALK == kSpan) {
+    if (!active) return;
+    if (!matrix) {
+      store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S);
+    } else {
+      float* to = ws.span_matrix + (start + col - ws.VP) * (32 * KB) + 4 * q;  // its columns are rows here
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<v4f*>(to + 16 * d) = S[d];
+    }
+  }
+  if constexpr (kOut) {
     if (!column.there) return;
-    for (long long t = (long long)chunks * kT + q; t < N; t += 4) y[t * KC + column.at] = (T)0.f;
-    if (!a.state_out) return;
+    const long long stop = min((long long)last * kT, (long long)N);
+    for (long long t = (long long)max(end, begin) * kT + q; t < stop; t += 4) y[t * KC + column.at] = (T)0.f;
+    if (!a.state_out || last != ws.chunks) return;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -494,17 +524,26 @@ hipError_t prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_
   });
 }
 
-template <class T>
-hipError_t states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s) {
-  const dim3 grid(((backward ? w.VP : w.V) + 63) / 64, w.units);
+template <class T, int NW, int WALK>
+hipError_t walk(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
+  const int columns = WALK == kOutputs ? w.V : WALK == kKeep ? w.VP : w.VP + 32 * w.KB;
+  const dim3 grid((columns + 16 * NW - 1) / (16 * NW), w.units, w.segments);
   return by_width(w.KB, [&](auto kb) {
-    constexpr int KB = decltype(kb)::value;
-    if (backward)
-      hipLaunchKernelGGL((rule_state_kernel<T, KB, true>), grid, dim3(256), 0, s, a, w);
-    else
-      hipLaunchKernelGGL((rule_state_kernel<T, KB, false>), grid, dim3(256), 0, s, a, w);
+    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, NW, WALK>), grid, dim3(64 * NW), 0, s, a, w);
     return hipGetLastError();
   });
+}
+
+template <class T>
+hipError_t states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (w.segments > 1) {
+    e = walk<T, 8, kSpan>(a, w, s);
+    if (e == hipSuccess) e = launch_rule_join(a.state_in, w, a.n, false, s);
+    if (e != hipSuccess) return e;
+  }
+  if (w.V <= 64) return backward ? walk<T, 4, kKeep>(a, w, s) : walk<T, 4, kOutputs>(a, w, s);
+  return backward ? walk<T, 8, kKeep>(a, w, s) : walk<T, 8, kOutputs>(a, w, s);
 }
 
 template <class T>

@@ -40,22 +40,26 @@ __device__ __forceinline__ int tokens_of(const RuleArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.n.N) : a.n.N;
 }
 
-// Block (group of 64 columns, unit).
-template <class T, int KB>
-__global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
-  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB;
+// Block (group of 16 NW columns, unit, segment).  SPAN: only what the segment adds to the
+// state's gradient.
+template <class T, int KB, int NW, bool SPAN>
+__global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
+  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, kThreads = 64 * NW;
   __shared__ __attribute__((aligned(16))) bf16 kbuf[NP][kT * ST];
   __shared__ __attribute__((aligned(16))) bf16 qbuf[NP][kT * ST];
   __shared__ TriangleParts inv, inside;  // the transposed triangles
   __shared__ float4 ta[kT], tb[kT];
   const RuleArgs& a = g.a;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
-  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H;
+  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int col = (blockIdx.x * 4 + wave) * 16 + m;
-  const bool active = (blockIdx.x * 4 + wave) * 16 < ws.VP;
+  const int col = (blockIdx.x * NW + wave) * 16 + m;
+  const bool active = (blockIdx.x * NW + wave) * 16 < ws.VP;
   const Column column(col, ws.V, C / a.n.H, C, h);
-  const int length = tokens_of(a, b), chunks = (length + kT - 1) / kT;
+  const int length = tokens_of(a, b);
+  const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
+  const int end = min((length + kT - 1) / kT, last);
+  const long long start = ((long long)unit * ws.segments + seg) * (32 * KB);  // row of a segment's state
   const int stride = a.n.Hk * D;
   const T* K = static_cast<const T*>(a.k) + (long long)b * N * stride + (long long)hk * D;
   const T* Q = static_cast<const T*>(a.q) + (long long)b * N * stride + (long long)hk * D;
@@ -68,11 +72,18 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * d + 4 * q + r;
-      S[d][r] = g.gstate && column.there && row < D ? g.gstate[((long long)b * D + row) * KC + column.at] : 0.f;
+      float x = 0.f;
+      if (SPAN) {
+      } else if (ws.segments > 1) {
+        if (active) x = ws.start[(start + row) * ws.VP + col];
+      } else if (g.gstate && column.there && row < D) {
+        x = g.gstate[((long long)b * D + row) * KC + column.at];
+      }
+      S[d][r] = x;
     }
 
-  RowStage<T, KB> sk, sq;
-  BlockStage si;
+  RowStage<T, KB, kThreads> sk, sq;
+  BlockStage<kThreads> si;
   float4 st;
   ColumnStage<T> so;
   const auto fetch = [&](int c) {
@@ -83,11 +94,11 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
     si.load(ws.invT + at * kBlocks * 64, tid);
     st = ws.token[at * 2 * kT + (tid & (2 * kT - 1))];
   };
-  if (chunks > 0) {
-    fetch(chunks - 1);
-    so.load(gy + (long long)(chunks - 1) * kT * KC, KC, length - (chunks - 1) * kT, column, q);
+  if (begin < end) {
+    fetch(end - 1);
+    so.load(gy + (long long)(end - 1) * kT * KC, KC, min(length - (end - 1) * kT, kT), column, q);
   }
-  for (int c = chunks - 1; c >= 0; --c) {
+  for (int c = end - 1; c >= begin; --c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
     __syncthreads();  // the chunk before has been read
@@ -97,20 +108,19 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
     if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = st;
     const float whole = ws.whole[at];
     __syncthreads();
-    if (c > 0) fetch(c - 1);
+    if (c > begin) fetch(c - 1);
     // P: rows i, columns j, so that a lane has four i of its column
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      if (i < wave) continue;
+    for (int n = wave; n < kBlocks; n += NW) {
+      const int i = row_of(n), jb = n - block_of(i, 0);
       v4f p{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         Frag fk[NP], fq[NP];
-        rows_frag<NP, ST>(kbuf, wave, kb, m, q, fk);
+        rows_frag<NP, ST>(kbuf, jb, kb, m, q, fk);
         rows_frag<NP, ST>(qbuf, i, kb, m, q, fq);
         p = mma(fq, fk, p);
       }
-      const int j = 16 * wave + m;
+      const int j = 16 * jb + m;
       const float4 me = tb[j];
       const float f = a.scale * me.x;
 #pragma unroll
@@ -119,11 +129,11 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
         const float4 other = tb[u];
         p[r] = u >= j ? p[r] * (f * other.y) * decay_between(other, me) : 0.f;
       }
-      put_block(inside, block_of(i, wave), lane, p[0], p[1], p[2], p[3]);
+      put_block(inside, n, lane, p[0], p[1], p[2], p[3]);
     }
     v4f X[kTiles];
     if (active) {
-      store_tiles(ws.gstate + at * (32 * KB) * ws.VP, ws.VP, 4 * q * ws.VP + col, S);
+      if (!SPAN) store_tiles(ws.gstate + at * (32 * KB) * ws.VP, ws.VP, col, q, S);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) X[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -150,7 +160,7 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
     for (int kb = 0; kb < 2; ++kb) {
       float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = so.get(2 * kb + e / 4, e % 4, tokens, column, q);
+      for (int e = 0; e < 8; ++e) x[e] = so.get(2 * kb + e / 4, e % 4, column);
       parts8<T>(x, fo[kb]);
     }
 #pragma unroll
@@ -176,7 +186,7 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
           X[i] = mma(f, fx[kb], X[i]);
         }
     }
-    store_tiles(ws.gvalue + at * kT * ws.VP, ws.VP, 4 * q * ws.VP + col, X);
+    if (!SPAN) store_tiles(ws.gvalue + at * kT * ws.VP, ws.VP, col, q, X);
     // gS <- e^{G_end} gS + Q^T (o gO) - K^T (a gv)
     v4f o[kTiles];
 #pragma unroll
@@ -185,14 +195,14 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
       for (int r = 0; r < 4; ++r) {
         const float4 tok = ta[16 * i + 4 * q + r];
         X[i][r] *= tok.x;
-        o[i][r] = tok.w * so.get(i, r, tokens, column, q);
+        o[i][r] = tok.w * so.get(i, r, column);
       }
-    if (gv) store_column(gv + (long long)c * kT * KC, KC, N - c * kT, tokens, column, q, X);
+    if (!SPAN && gv) store_column(gv + (long long)c * kT * KC, KC, N - c * kT, tokens, column, q, X);
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) X[i][r] *= -ta[16 * i + 4 * q + r].y;
-    if (c > 0) so.load(gy + (long long)(c - 1) * kT * KC, KC, kT, column, q);
+    if (c > begin) so.load(gy + (long long)(c - 1) * kT * KC, KC, kT, column, q);
     Frag fz[2][3];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -213,10 +223,16 @@ __global__ __launch_bounds__(256) void rule_reverse_kernel(RuleBwdArgs g, RuleWs
       }
     }
   }
+  if constexpr (SPAN) {
+    if (active) store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S);
+    return;
+  }
   if (!column.there) return;
-  if (gv)
-    for (long long t = (long long)chunks * kT + q; t < N; t += 4) gv[t * KC + column.at] = (T)0.f;
-  if (!g.gstate_in) return;
+  if (gv) {
+    const long long stop = min((long long)last * kT, (long long)N);
+    for (long long t = (long long)max(end, begin) * kT + q; t < stop; t += 4) gv[t * KC + column.at] = (T)0.f;
+  }
+  if (!g.gstate_in || seg > 0) return;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -312,7 +328,7 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     return;
   }
   {
-    RowStage<T, KB> s;
+    RowStage<T, KB, 256> s;
     s.load(static_cast<const T*>(a.k) + key0, stride, tokens, D, tid);
     s.store(kbuf, tokens, D, tid);
     s.load(static_cast<const T*>(a.q) + key0, stride, tokens, D, tid);
@@ -651,8 +667,18 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
 
 template <class T, int KB>
 hipError_t backward(const RuleBwdArgs& g, const RuleWs& w, hipStream_t s) {
-  hipLaunchKernelGGL((rule_reverse_kernel<T, KB>), dim3((w.VP + 63) / 64, w.units), dim3(256), 0, s, g, w);
-  hipError_t e = hipGetLastError();
+  const auto walk = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3((w.VP + 16 * waves - 1) / (16 * waves), w.units, w.segments), dim3(64 * waves), 0, s,
+                       g, w);
+    return hipGetLastError();
+  };
+  hipError_t e = hipSuccess;
+  if (w.segments > 1) {
+    e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, true>, 4) : walk(rule_reverse_kernel<T, KB, 8, true>, 8);
+    if (e == hipSuccess) e = launch_rule_join(g.gstate, w, g.a.n, true, s);
+    if (e != hipSuccess) return e;
+  }
+  e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, false>, 4) : walk(rule_reverse_kernel<T, KB, 8, false>, 8);
   if (e != hipSuccess || !(g.gq || g.gk || g.gdecay || g.gbeta)) return e;
   hipLaunchKernelGGL((rule_grads_kernel<T, KB>), dim3(w.chunks, g.a.n.B * g.a.n.Hk), dim3(256), 0, s, g, w);
   return hipGetLastError();

@@ -16,6 +16,8 @@
 // below the other are an operand of the next product as they are.
 #pragma once
 
+#include <type_traits>
+
 #include "seq_common.h"
 
 namespace cgconv {
@@ -31,6 +33,7 @@ constexpr int kT = kRuleChunk;          // tokens of a chunk: four tiles of 16
 constexpr int kTiles = kT / 16;
 constexpr int kBlocks = kRuleTriangle;  // 16 x 16 blocks on and below the diagonal of kT x kT
 __host__ __device__ constexpr int block_of(int i, int j) { return i * (i + 1) / 2 + j; }
+__host__ __device__ constexpr int row_of(int block) { return block < 1 ? 0 : block < 3 ? 1 : block < 6 ? 2 : 3; }
 
 // Parts of an operand of storage type T.
 template <class T>
@@ -185,25 +188,36 @@ struct Column {
 // use.  They are not masked, which would take a branch and a wait each: what is not there
 // is read from a place that is, and left out where the values are used.
 
+// A place in bytes from a uniform base: 32 bits a lane.  The largest, a chunk of the widest
+// rows, is below 2^28; a row has less than 2^24 bytes.
+template <class T>
+__device__ __forceinline__ T& place(T* base, uint32_t bytes) {
+  typedef typename std::conditional<std::is_const<T>::value, const char, char>::type Byte;
+  return *reinterpret_cast<T*>(reinterpret_cast<Byte*>(base) + bytes);
+}
+// x as a number the compiler knows nothing of: what is computed from it stays where it is,
+// instead of waiting in registers for every turn of a loop.
+__device__ __forceinline__ int afresh(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
 // A chunk's key or query rows, tokens >= 1 of them.
-template <class T, int KB>
+template <class T, int KB, int THREADS>
 struct RowStage {
-  Raw<T, 8> raw[KB];
+  static constexpr int kAll = 256 * KB, kEach = (kAll + THREADS - 1) / THREADS;  // pieces of eight
+  Raw<T, 8> raw[kEach];
   __device__ __forceinline__ void load(const T* base, int stride, int tokens, int D, int tid) {
-    if (D % 8 == 0) {
 #pragma unroll
-      for (int p = 0; p < KB; ++p) {
-        const int at = p * 256 + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
-        raw[p].load(base + (uint32_t)(min(row, tokens - 1) * stride + (c < D ? c : 0)));
-      }
-    } else {
-#pragma unroll
-      for (int p = 0; p < KB; ++p) {
-        const int at = p * 256 + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
-        const T* from = base + (uint32_t)(min(row, tokens - 1) * stride);
+    for (int p = 0; p < kEach; ++p) {
+      const int at = p * THREADS + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
+      const uint32_t o = __umul24(min(row, tokens - 1), stride * (int)sizeof(T));
+      if (D % 8 == 0) {
+        raw[p].load(&place(base, o + (c < D ? c : 0) * (int)sizeof(T)));
+      } else {
         T t[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = from[min(c + e, D - 1)];
+        for (int e = 0; e < 8; ++e) t[e] = place(base, o + min(c + e, D - 1) * (int)sizeof(T));
         __builtin_memcpy(raw[p].w, t, sizeof t);
       }
     }
@@ -212,15 +226,21 @@ struct RowStage {
   __device__ __forceinline__ void store(bf16 (&buf)[NP][N], int tokens, int D, int tid) const {
     constexpr int ST = row_stride(KB);
 #pragma unroll
-    for (int p = 0; p < KB; ++p) {
-      const int at = p * 256 + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
+    for (int p = 0; p < kEach; ++p) {
+      const int at = p * THREADS + tid, row = at / (4 * KB), c = at % (4 * KB) * 8;
+      if (kAll % THREADS && at >= kAll) break;
       const int n = row < tokens ? D - c : 0;
       Frag f[NP];
       if constexpr (NP == 1) {
         __builtin_memcpy(&f[0], raw[p].w, 16);
+        if (D % 8 == 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          f[0].w[e] = n >= 2 * e + 2 ? f[0].w[e] : n > 2 * e ? f[0].w[e] & 0xFFFFu : 0u;
+          for (int e = 0; e < 4; ++e) f[0].w[e] = n > 0 ? f[0].w[e] : 0u;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            f[0].w[e] = n >= 2 * e + 2 ? f[0].w[e] : n > 2 * e ? f[0].w[e] & 0xFFFFu : 0u;
+        }
       } else {
         float x[8];
         raw[p].widen_to(x);
@@ -238,58 +258,54 @@ struct RowStage {
   }
 };
 
-// Blocks of a triangle: 640 quadruples for 256 threads.
+// Blocks of a triangle, 640 quadruples.
+template <int THREADS>
 struct BlockStage {
-  float4 v[3];
+  static constexpr int kEach = (kBlocks * 64 + THREADS - 1) / THREADS;
+  float4 v[kEach];
   __device__ __forceinline__ void load(const float4* base, int tid) {
 #pragma unroll
-    for (int p = 0; p < 3; ++p) v[p] = base[min(p * 256 + tid, kBlocks * 64 - 1)];
+    for (int p = 0; p < kEach; ++p) v[p] = base[min(p * THREADS + tid, kBlocks * 64 - 1)];
   }
   __device__ __forceinline__ void store(TriangleParts& t, int tid) const {
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      const int at = p * 256 + tid;
+    for (int p = 0; p < kEach; ++p) {
+      const int at = p * THREADS + tid;
       if (at < kBlocks * 64) put_block(t, at >> 6, at & 63, v[p].x, v[p].y, v[p].z, v[p].w);
     }
   }
 };
 
-// The 16 values of a lane's column in a chunk: tokens 16 i + 4 q + r.
+// The 16 values of a lane's column in a chunk: tokens 16 i + 4 q + r.  In place of a token
+// that is not there comes the last one, whose products with the zero key, query and beta of
+// that row are as harmless as they are in its own row.
 template <class T>
 struct ColumnStage {
   T v[kTiles][4];
   __device__ __forceinline__ void load(const T* base, int stride, int tokens, const Column& c, int q) {
-    if (tokens >= kT) {
-      const uint32_t at = 4 * q * stride + c.at;
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i)
+    for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[i][r] = (base + (uint32_t)((16 * i + r) * stride))[at];
-    } else {
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          v[i][r] = base[(uint32_t)(min(16 * i + 4 * q + r, tokens - 1) * stride + c.at)];
-    }
+      for (int r = 0; r < 4; ++r)
+        v[i][r] = place(base, __umul24(min(16 * i + 4 * q + r, tokens - 1), stride * (int)sizeof(T)) +
+                                  c.at * (int)sizeof(T));
   }
-  __device__ __forceinline__ float get(int i, int r, int tokens, const Column& c, int q) const {
-    return c.there && 16 * i + 4 * q + r < tokens ? widen(v[i][r]) : 0.f;
-  }
+  __device__ __forceinline__ float get(int i, int r, const Column& c) const { return c.there ? widen(v[i][r]) : 0.f; }
 };
 
-// The same 16 values to a tensor of N tokens, the first `left` of them from the chunk's first
-// on; zeros from `tokens` on.
+// The same 16 values to a tensor of which `left` tokens are left from the chunk's first on;
+// zeros from `tokens` on.
 template <class T>
 __device__ __forceinline__ void store_column(T* base, int stride, int left, int tokens, const Column& c, int q,
                                              const v4f (&x)[kTiles]) {
   if (!c.there) return;
-  const uint32_t at = 4 * q * stride + c.at;
+  const int row = afresh(stride) * (int)sizeof(T);
+  const uint32_t at = __umul24(4 * q, row) + c.at * (int)sizeof(T);
   if (tokens >= kT) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) (base + (uint32_t)((16 * i + r) * stride))[at] = (T)x[i][r];
+      for (int r = 0; r < 4; ++r) place(base, at + (16 * i + r) * row) = (T)x[i][r];
     return;
   }
 #pragma unroll
@@ -297,18 +313,19 @@ __device__ __forceinline__ void store_column(T* base, int stride, int left, int 
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int t = 16 * i + 4 * q + r;
-      if (t < left) (base + (uint32_t)((16 * i + r) * stride))[at] = t < tokens ? (T)x[i][r] : (T)0.f;
+      if (t < left) place(base, at + (16 * i + r) * row) = t < tokens ? (T)x[i][r] : (T)0.f;
     }
 }
 
-// Accumulator tiles one below the other to rows of a workspace array, `at` the lane's place
-// in the first.
+// Accumulator tiles one below the other to columns `col` of rows of a workspace array.
 template <int TILES>
-__device__ __forceinline__ void store_tiles(float* base, int stride, uint32_t at, const v4f (&x)[TILES]) {
+__device__ __forceinline__ void store_tiles(float* base, int stride, int col, int q, const v4f (&x)[TILES]) {
+  const int row = afresh(stride) * 4;
+  const uint32_t at = __umul24(4 * q, row) + col * 4;
 #pragma unroll
   for (int i = 0; i < TILES; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) (base + (uint32_t)((16 * i + r) * stride))[at] = x[i][r];
+    for (int r = 0; r < 4; ++r) place(base, at + (16 * i + r) * row) = x[i][r];
 }
 
 }  // namespace ruledev

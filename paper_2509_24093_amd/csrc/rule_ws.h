@@ -1,6 +1,9 @@
 // Workspace of the gated delta rule: unit = (sequence, head), chunk by chunk.
 #pragma once
 
+#include <algorithm>
+#include <type_traits>
+
 #include "seq.h"
 
 namespace cgconv {
@@ -14,8 +17,20 @@ struct RuleWs {
   float* gstate;   // [unit][chunk][DP][VP]: gradient of the state after every chunk
   float* value;    // [unit][chunk][64][VP]: what the tokens write, V'
   float* gvalue;   // [unit][chunk][64][VP]: its gradient through (1 + A)^-T, dY
+  float* start;        // [unit][segment][DP][VP]: the state before every segment (its gradient behind it)
+  float* span_state;   // [unit][segment][DP][VP]: what a segment adds to the state
+  float* span_matrix;  // [unit][segment][DP][DP]: and by what it multiplies it, columns as rows
   int units, chunks, KB, V, VP;  // DP = 32 KB; VP: V in whole tiles of 32
+  int segments, span;            // the chunks in segments of `span`, walked at once
 };
+
+// Chunks of a segment.
+inline int rule_span(int chunks, int units, int VP) {
+  const long long blocks = (long long)units * ((VP + 127) / 128);
+  if (blocks >= 128 || chunks < 8) return chunks;
+  const int segments = (int)std::min<long long>(chunks / 4, (256 + blocks - 1) / blocks);
+  return (chunks + segments - 1) / segments;
+}
 
 inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size_t* bytes) {
   RuleWs w{};
@@ -40,6 +55,13 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
     take(w.value, count * kRuleChunk * w.VP);
     take(w.gvalue, count * kRuleChunk * w.VP);
   }
+  w.span = rule_span(w.chunks, w.units, w.VP);
+  w.segments = (w.chunks + w.span - 1) / w.span;
+  if (w.segments > 1) {
+    take(w.start, (size_t)w.units * w.segments * 32 * w.KB * w.VP);
+    take(w.span_state, (size_t)w.units * w.segments * 32 * w.KB * w.VP);
+    take(w.span_matrix, (size_t)w.units * w.segments * 1024 * w.KB * w.KB);
+  }
   if (bytes) *bytes = at;
   return w;
 }
@@ -48,5 +70,8 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
 hipError_t launch_rule_prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
 // The states from chunk to chunk; for the backward they and V' are kept and no output is formed.
 hipError_t launch_rule_states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
+// From what every segment adds and multiplies by, the state before every segment, or in
+// reverse the gradient of the state behind it; `first`: [B][D][K][C] or nullptr (zeros).
+hipError_t launch_rule_join(const float* first, const RuleWs& w, const RuleSizes& n, bool reverse, hipStream_t s);
 
 }  // namespace cgconv
