@@ -468,6 +468,32 @@ int cgconv_seq_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
                              hipStream_t stream);
 
 /*
+ * The norms on both sides of a residual connection in one pass, token by token: of a
+ * block's output u, which a gate and a scale weigh before it is added to the stream x,
+ * and of the stream behind it, for the next block.  With norm(.) the norm by degree
+ * above, without weight and bias:
+ *
+ *   r[(l,m),c] = x + scale[c] silu(gate[c]) post_weight[l,c] norm(u)
+ *   y[(l,m),c] = weight[l,c] norm(r) + [l = 0] bias[c],    silu(z) = z / (1 + exp(-z))
+ *
+ * x, u, r, y [batch][N][K][C] and gate [batch][N][C] of dtype; gate may be NULL (no
+ * factor); post_weight, weight [L_max+1][C], scale and bias [C], fp32, may be NULL (ones,
+ * zeros); eps >= 0.  y is of the r that has not been rounded to dtype.  stats
+ * [batch][N][2 (L_max+2)], fp32, or NULL: mean of u, 1 / deviation of its degrees, mean of
+ * r, 1 / deviation of its degrees, for the backward.  The backward takes the gradients
+ * of r (or NULL: zeros) and y; any of its outputs may be NULL, not all.  The sums over
+ * tokens have a fixed order.
+ */
+int cgconv_seq_residual_norm(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* u, const void* gate,
+                             const float* post_weight, const float* scale, const float* weight, const float* bias,
+                             float eps, void* r, void* y, float* stats, hipStream_t stream);
+int cgconv_seq_residual_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* u,
+                                      const void* gate, const float* post_weight, const float* scale,
+                                      const float* weight, const float* stats, const void* grad_r, const void* grad_y,
+                                      void* grad_x, void* grad_u, void* grad_gate, float* grad_post_weight,
+                                      float* grad_scale, float* grad_weight, float* grad_bias, hipStream_t stream);
+
+/*
  * Short causal convolution of every component and channel over the tokens,
  * width W = 2..CGCONV_SEQ_WIDTH, depthwise, one filter per degree and channel:
  *
@@ -580,6 +606,27 @@ int cgconv_pack8(int32_t dtype, int64_t rows, int64_t C, const void* x, int8_t* 
                  hipStream_t stream);
 int cgconv_unpack8(int32_t dtype, int64_t rows, int64_t C, const int8_t* codes, const uint8_t* scales, void* x,
                    hipStream_t stream);
+
+/*
+ * Clipping of n tensors (n >= 0, at most CGCONV_CLIP_TENSORS) by their global norm:
+ *
+ *   norm = sqrt(sum of the squares of all values),   out = g min(1, max_norm / (norm + eps))
+ *
+ * dtypes, counts, grads and out are host arrays of n, read during the call: each tensor has
+ * its type, its number of values (0 is allowed), its device address and that of its output,
+ * aligned to its values and otherwise as they come.  An output may be its own gradient's
+ * place (then nothing is written where the factor is 1) and overlaps nothing else.  The
+ * squares are added in 64 bits and in a fixed order; norm (device, one float) receives the
+ * norm, an output is rounded once.  An infinity in a gradient makes the norm infinite and
+ * the factor zero (0 x infinity is NaN); a NaN makes everything NaN.  max_norm, eps >= 0;
+ * max_norm infinite: only the norm.  workspace: device, 8-byte aligned, of
+ * cgconv_clip_workspace(n, counts) bytes (a negative status where the list is refused); its
+ * use by two calls at once is the caller's to avoid.  No plan.
+ */
+#define CGCONV_CLIP_TENSORS (1 << 20)
+int64_t cgconv_clip_workspace(int64_t n, const int64_t* counts);
+int cgconv_clip(int64_t n, const int32_t* dtypes, const int64_t* counts, const void* const* grads, void* const* out,
+                float max_norm, float eps, float* norm, void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /* Thread-local message describing the last error on this thread ("" if none). */
 const char* cgconv_last_error(void);

@@ -29,6 +29,7 @@ from .sequence import (  # noqa: F401
     cgconv_delta_rule,
     cgconv_norm,
     cgconv_pack8,
+    cgconv_residual_norm,
     cgconv_scan,
     cgconv_seq_conv,
     cgconv_seq_conv_backward,
@@ -42,13 +43,18 @@ from .sequence import (  # noqa: F401
     cgconv_seq_plan_create_rule,
     cgconv_seq_plan_destroy,
     cgconv_seq_plan_info,
+    cgconv_seq_residual_norm,
+    cgconv_seq_residual_norm_backward,
     cgconv_seq_scan,
     cgconv_seq_scan_backward,
     cgconv_seq_scan_step,
     cgconv_short_conv,
     cgconv_unpack8,
+    cgconv_clip,
+    cgconv_clip_workspace,
     checkpoint_pack,
     checkpoint_unpack,
+    clip_gradients,
 )
 
 _HERE = os.path.dirname(os.path.abspath(__file__))

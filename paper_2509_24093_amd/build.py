@@ -62,6 +62,8 @@ def build(jobs: int | None = None, verbose: bool = True) -> str:
         ([HIPCC, "-c"] + HIP_FLAGS, "gft.hip", "gft.o", []),
         ([HIPCC, "-x", "hip", "-c"] + HIP_FLAGS, "sequence.cpp", "sequence.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "norm.hip", "norm.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "residual.hip", "residual.o", []),
+        ([HIPCC, "-c"] + HIP_FLAGS, "clip.hip", "clip.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "pack.hip", "pack.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "conv.hip", "conv.o", []),
         ([HIPCC, "-c"] + HIP_FLAGS, "scan.hip", "scan.o", []),

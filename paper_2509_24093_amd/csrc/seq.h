@@ -1,8 +1,11 @@
 // Internal interface between the sequence plan (sequence.cpp) and its kernels:
-// layer norm by degree (norm.hip), 8-bit checkpoints (pack.hip), the short
-// causal convolution (conv.hip), the selective scan (scan.hip, scan_bwd.hip) and
-// the gated delta rule (delta_rule.hip, delta_rule_bwd.hip).  Features x, y are [B][N][K][C], channel fastest, in fp32 or
-// bfloat16; parameters, states and statistics are fp32.
+// layer norm by degree (norm.hip), alone and around a residual connection
+// (residual.hip), 8-bit checkpoints (pack.hip), the short causal convolution
+// (conv.hip), the selective scan (scan.hip, scan_bwd.hip), the gated delta rule
+// (delta_rule.hip, delta_rule_bwd.hip, rule_join.hip) and the clipping of gradients
+// (clip.hip).  Features x, y are
+// [B][N][K][C], channel fastest, in fp32 or bfloat16; parameters, states and
+// statistics are fp32.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -66,6 +69,41 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_backward(const NormBwdArgs& a, hipStream_t s);
 // bytes of NormBwdArgs::part
 size_t norm_bwd_part_bytes(long long tokens, int L, int C);
+
+// ---- norms around a residual connection -------------------------------------------
+
+struct ResidualArgs {
+  int type;
+  const void* x;             // [tokens][K][C]
+  const void* u;
+  const void* gate;          // [tokens][C] or nullptr (ones in place of its silu)
+  const float* post_weight;  // [L+1][C] or nullptr (ones)
+  const float* scale;        // [C] or nullptr (ones)
+  const float* weight;       // [L+1][C] or nullptr (ones)
+  const float* bias;         // [C] or nullptr (zeros)
+  float eps;
+  void* r;
+  void* y;
+  float* stats;  // [tokens][2 (L+2)]: mean of u, its factors, mean of r, its factors; or nullptr
+  long long tokens;
+  int L, K, C;
+};
+struct ResidualBwdArgs {
+  ResidualArgs a;  // r, y, bias and eps unused
+  const void* gr;  // or nullptr (zeros)
+  const void* gy;
+  void* gx;        // any may be nullptr
+  void* gu;
+  void* ggate;
+  float* gpost;
+  float* gscale;
+  float* gw;
+  float* gb;
+  float* part;  // residual_part_bytes, or nullptr if no parameter's gradient is wanted
+};
+hipError_t launch_residual(const ResidualArgs& a, hipStream_t s);
+hipError_t launch_residual_backward(const ResidualBwdArgs& g, hipStream_t s);
+size_t residual_part_bytes(long long tokens, int L, int C);
 
 // ---- 8-bit checkpoints ---------------------------------------------------------
 
@@ -135,6 +173,21 @@ hipError_t launch_scan_step(const ScanArgs& a, hipStream_t s);
 hipError_t launch_scan_backward(const ScanBwdArgs& g, hipStream_t s);
 // workspace of both directions
 size_t scan_workspace_bytes(int64_t B, int64_t N, int K, int64_t C, int S);
+
+// ---- clipping by the global norm ------------------------------------------------------
+
+struct ClipArgs {
+  long long n;             // tensors; the arrays are the host's
+  const int32_t* types;
+  const int64_t* counts;
+  const void* const* grads;
+  void* const* out;        // each its gradient's own address, or an array of its own
+  float max_norm, eps;
+  float* norm;
+  double* ws;  // clip_workspace_bytes
+};
+hipError_t launch_clip(const ClipArgs& a, hipStream_t s);
+size_t clip_workspace_bytes(long long n, const int64_t* counts);
 
 // ---- gated delta rule ---------------------------------------------------------------
 

@@ -1,12 +1,14 @@
 // Sequence plan and the entry points of the operators around the convolution
 // (see include/cgconv.h, "Sequence operators"): checks of arguments, the
-// plan's workspace, launches.  Kernels: norm.hip, pack.hip, conv.hip, scan.hip,
-// scan_bwd.hip, delta_rule.hip, delta_rule_bwd.hip.
+// plan's workspace, launches.  Kernels: norm.hip, residual.hip, pack.hip, conv.hip,
+// scan.hip, scan_bwd.hip, delta_rule.hip, delta_rule_bwd.hip, rule_join.hip,
+// clip.hip.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstdint>
 #include <new>
+#include <vector>
 
 #include "cgconv.h"
 #include "seq.h"
@@ -153,6 +155,7 @@ cgconv_seq_plan* create_plan(int64_t batch, int64_t N, int32_t L_max, int64_t C,
     return nullptr;
   }
   p->ws_bytes = std::max(norm_bwd_part_bytes(batch * N, L_max, (int)C), conv_bwd_part_bytes(batch, N, K, C));
+  p->ws_bytes = std::max(p->ws_bytes, residual_part_bytes(batch * N, L_max, (int)C));
   if (states) p->ws_bytes = std::max(p->ws_bytes, scan_workspace_bytes(batch, N, K, C, states));
   if (heads) p->ws_bytes = std::max(p->ws_bytes, rule_workspace_bytes(rule_sizes(p), rule_backward));
   if ((e = hipMalloc(&p->ws, p->ws_bytes)) != hipSuccess) {
@@ -273,6 +276,83 @@ int cgconv_seq_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
                 grad_weight || grad_bias ? static_cast<float*>(plan->ws) : nullptr, (long long)tokens, plan->L,
                 plan->K, (int)plan->C};
   return launched(launch_norm_backward(a, stream));
+}
+
+int cgconv_seq_residual_norm(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* u, const void* gate,
+                             const float* post_weight, const float* scale, const float* weight, const float* bias,
+                             float eps, void* r, void* y, float* stats, hipStream_t stream) {
+  int st = check_plan(plan, dtype);
+  if (st != CGCONV_OK) return st;
+  if (!(eps >= 0.f)) {
+    set_last_error("eps=%g must be >= 0", (double)eps);
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  const size_t tokens = plan->B * plan->N, C = plan->C, n = tokens * plan->K * C * seq_type_size(dtype);
+  const size_t nw = (plan->L + 1) * C * 4;
+  const Arg args[] = {{"x", x, n, true, false},
+                      {"u", u, n, true, false},
+                      {"gate", gate, tokens * C * seq_type_size(dtype), false, false},
+                      {"post_weight", post_weight, nw, false, false},
+                      {"scale", scale, C * 4, false, false},
+                      {"weight", weight, nw, false, false},
+                      {"bias", bias, C * 4, false, false},
+                      {"r", r, n, true, true},
+                      {"y", y, n, true, true},
+                      {"stats", stats, tokens * 2 * (plan->L + 2) * 4, false, true}};
+  if ((st = check_arrays(args, 10)) != CGCONV_OK) return st;
+  ResidualArgs a{dtype, x, u, gate, post_weight, scale, weight, bias, eps, r, y, stats, (long long)tokens, plan->L,
+                 plan->K, (int)C};
+  return launched(launch_residual(a, stream));
+}
+
+int cgconv_seq_residual_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* x, const void* u,
+                                      const void* gate, const float* post_weight, const float* scale,
+                                      const float* weight, const float* stats, const void* grad_r, const void* grad_y,
+                                      void* grad_x, void* grad_u, void* grad_gate, float* grad_post_weight,
+                                      float* grad_scale, float* grad_weight, float* grad_bias, hipStream_t stream) {
+  int st = check_plan(plan, dtype);
+  if (st != CGCONV_OK) return st;
+  if (!grad_x && !grad_u && !grad_gate && !grad_post_weight && !grad_scale && !grad_weight && !grad_bias) {
+    set_last_error("at least one gradient must be given");
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  if (grad_gate && !gate) {
+    set_last_error("grad_gate is given without a gate");
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  const size_t tokens = plan->B * plan->N, C = plan->C, n = tokens * plan->K * C * seq_type_size(dtype);
+  const size_t nw = (plan->L + 1) * C * 4, ng = tokens * C * seq_type_size(dtype);
+  const Arg args[] = {{"x", x, n, true, false},
+                      {"u", u, n, true, false},
+                      {"gate", gate, ng, false, false},
+                      {"post_weight", post_weight, nw, false, false},
+                      {"scale", scale, C * 4, false, false},
+                      {"weight", weight, nw, false, false},
+                      {"stats", stats, tokens * 2 * (plan->L + 2) * 4, true, false},
+                      {"grad_r", grad_r, n, false, false},
+                      {"grad_y", grad_y, n, true, false},
+                      {"grad_x", grad_x, n, false, true},
+                      {"grad_u", grad_u, n, false, true},
+                      {"grad_gate", grad_gate, ng, false, true},
+                      {"grad_post_weight", grad_post_weight, nw, false, true},
+                      {"grad_scale", grad_scale, C * 4, false, true},
+                      {"grad_weight", grad_weight, nw, false, true},
+                      {"grad_bias", grad_bias, C * 4, false, true}};
+  if ((st = check_arrays(args, 16)) != CGCONV_OK) return st;
+  ResidualBwdArgs g{};
+  g.a = {dtype, x, u, gate, post_weight, scale, weight, nullptr, 0.f, nullptr, nullptr, const_cast<float*>(stats),
+         (long long)tokens, plan->L, plan->K, (int)C};
+  g.gr = grad_r;
+  g.gy = grad_y;
+  g.gx = grad_x;
+  g.gu = grad_u;
+  g.ggate = grad_gate;
+  g.gpost = grad_post_weight;
+  g.gscale = grad_scale;
+  g.gw = grad_weight;
+  g.gb = grad_bias;
+  g.part = grad_post_weight || grad_scale || grad_weight || grad_bias ? static_cast<float*>(plan->ws) : nullptr;
+  return launched(launch_residual_backward(g, stream));
 }
 
 }  // extern "C"
@@ -664,6 +744,122 @@ int cgconv_unpack8(int32_t dtype, int64_t rows, int64_t C, const int8_t* codes, 
                       {"x", x, n * seq_type_size(dtype), true, true}};
   if ((st = check_arrays(args, 3)) != CGCONV_OK) return st;
   return launched(launch_unpack(dtype, codes, scales, x, rows, (int)C, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+// Sizes of a list of tensors: whole, and together below 2^60 values.
+int check_counts(int64_t n, const int64_t* counts) {
+  if (n < 0 || (n > 0 && !counts)) {
+    set_last_error("invalid list of tensors: n=%lld", (long long)n);
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  int64_t total = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (counts[i] < 0 || counts[i] > (1LL << 60) - total) {
+      set_last_error("invalid number of values of tensor %lld: %lld", (long long)i, (long long)counts[i]);
+      return CGCONV_ERR_INVALID_ARG;
+    }
+    total += counts[i];
+  }
+  if (n > CGCONV_CLIP_TENSORS) {
+    set_last_error("unsupported n=%lld: at most %d tensors", (long long)n, CGCONV_CLIP_TENSORS);
+    return CGCONV_ERR_UNSUPPORTED;
+  }
+  return CGCONV_OK;
+}
+
+// What a list's call writes shares no byte with anything else of the call, but for an output
+// in its own gradient's place: the spans in the order of their addresses, each against the
+// ends of those before it.
+int check_spans(const ClipArgs& a, size_t ws_bytes) {
+  struct Span {
+    uintptr_t from, to;
+    bool written;
+  };
+  std::vector<Span> spans;
+  try {
+    spans.reserve(2 * (size_t)a.n + 2);
+  } catch (const std::bad_alloc&) {
+    set_last_error("host allocation failed");
+    return CGCONV_ERR_OUT_OF_MEMORY;
+  }
+  const auto add = [&](const void* p, size_t bytes, bool written) {
+    if (bytes) spans.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
+  };
+  for (int64_t i = 0; i < a.n; ++i) {
+    const size_t bytes = (size_t)a.counts[i] * seq_type_size(a.types[i]);
+    add(a.out[i], bytes, true);
+    if (a.grads[i] != a.out[i]) add(a.grads[i], bytes, false);
+  }
+  add(a.norm, 4, true);
+  add(a.ws, ws_bytes, true);
+  std::sort(spans.begin(), spans.end(), [](const Span& x, const Span& y) { return x.from < y.from; });
+  uintptr_t any = 0, written = 0;
+  for (const Span& s : spans) {
+    if (s.from < (s.written ? any : written)) {
+      set_last_error("what is written must not overlap another array of the call");
+      return CGCONV_ERR_INVALID_ARG;
+    }
+    any = std::max(any, s.to);
+    if (s.written) written = std::max(written, s.to);
+  }
+  return CGCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t cgconv_clip_workspace(int64_t n, const int64_t* counts) {
+  clear_last_error();
+  const int st = check_counts(n, counts);
+  return st != CGCONV_OK ? st : (int64_t)clip_workspace_bytes(n, counts);
+}
+
+int cgconv_clip(int64_t n, const int32_t* dtypes, const int64_t* counts, const void* const* grads, void* const* out,
+                float max_norm, float eps, float* norm, void* workspace, int64_t workspace_bytes,
+                hipStream_t stream) {
+  clear_last_error();
+  int st = check_counts(n, counts);
+  if (st != CGCONV_OK) return st;
+  if (n > 0 && (!dtypes || !grads || !out)) {
+    set_last_error("dtypes, grads and out must be given");
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  if (!(max_norm >= 0.f) || !(eps >= 0.f)) {
+    set_last_error("max_norm=%g and eps=%g must be >= 0", (double)max_norm, (double)eps);
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  const Arg args[] = {{"norm", norm, 4, true, true}, {"workspace", workspace, 0, true, true}};
+  if ((st = check_arrays(args, 2, 4)) != CGCONV_OK) return st;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 7) != 0) {
+    set_last_error("workspace must be 8-byte aligned");
+    return CGCONV_ERR_ALIGNMENT;
+  }
+  const size_t needed = clip_workspace_bytes(n, counts);
+  if (workspace_bytes < 0 || (size_t)workspace_bytes < needed) {
+    set_last_error("workspace of %lld bytes, %zu are needed", (long long)workspace_bytes, needed);
+    return CGCONV_ERR_INVALID_ARG;
+  }
+  for (int64_t i = 0; i < n; ++i) {
+    if ((st = check_type(dtypes[i])) != CGCONV_OK) return st;
+    if (counts[i] == 0) continue;
+    if (!grads[i] || !out[i]) {
+      set_last_error("tensor %lld must be a non-NULL device pointer", (long long)i);
+      return CGCONV_ERR_INVALID_ARG;
+    }
+    const uintptr_t low = (reinterpret_cast<uintptr_t>(grads[i]) | reinterpret_cast<uintptr_t>(out[i]));
+    if (low & (seq_type_size(dtypes[i]) - 1)) {
+      set_last_error("tensor %lld must be aligned to its values", (long long)i);
+      return CGCONV_ERR_ALIGNMENT;
+    }
+  }
+  const ClipArgs a{n, dtypes, counts, grads, out, max_norm, eps, norm, static_cast<double*>(workspace)};
+  if ((st = check_spans(a, needed)) != CGCONV_OK) return st;
+  return launched(launch_clip(a, stream));
 }
 
 }  // extern "C"

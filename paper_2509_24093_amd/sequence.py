@@ -38,6 +38,10 @@ SIGNATURES = {
     "cgconv_seq_delta_rule": ([_vp, _i32] + [_vp] * 5 + [_f32, _i32] + [_vp] * 5, ctypes.c_int),
     "cgconv_seq_delta_rule_step": ([_vp, _i32] + [_vp] * 5 + [_f32, _i32] + [_vp] * 3, ctypes.c_int),
     "cgconv_seq_delta_rule_backward": ([_vp, _i32] + [_vp] * 5 + [_f32, _i32] + [_vp] * 11, ctypes.c_int),
+    "cgconv_seq_residual_norm": ([_vp, _i32] + [_vp] * 7 + [_f32] + [_vp] * 4, ctypes.c_int),
+    "cgconv_seq_residual_norm_backward": ([_vp, _i32] + [_vp] * 17, ctypes.c_int),
+    "cgconv_clip_workspace": ([_i64, _vp], _i64),
+    "cgconv_clip": ([_i64] + [_vp] * 4 + [_f32, _f32, _vp, _vp, _i64, _vp], ctypes.c_int),
     "cgconv_pack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
     "cgconv_unpack8": ([_i32, _i64, _i64] + [_vp] * 4, ctypes.c_int),
 }
@@ -99,6 +103,22 @@ def cgconv_seq_norm_backward(plan, dtype, x, codes, scales, weight, mean, rstd, 
     P = _main()
     return P._check(P.library().cgconv_seq_norm_backward(plan, dtype, x, codes, scales, weight, mean, rstd, grad_y,
                                                          grad_x, grad_weight, grad_bias, stream))
+
+
+def cgconv_seq_residual_norm(plan, dtype, x, u, gate, post_weight, scale, weight, bias, eps, r, y, stats, stream) -> int:
+    """Norms around a residual connection (gate, parameters and stats may be None)."""
+    P = _main()
+    return P._check(P.library().cgconv_seq_residual_norm(plan, dtype, x, u, gate, post_weight, scale, weight, bias, eps,
+                                                         r, y, stats, stream))
+
+
+def cgconv_seq_residual_norm_backward(plan, dtype, x, u, gate, post_weight, scale, weight, stats, grad_r, grad_y,
+                                      grad_x, grad_u, grad_gate, grad_post_weight, grad_scale, grad_weight, grad_bias,
+                                      stream) -> int:
+    P = _main()
+    return P._check(P.library().cgconv_seq_residual_norm_backward(
+        plan, dtype, x, u, gate, post_weight, scale, weight, stats, grad_r, grad_y, grad_x, grad_u, grad_gate,
+        grad_post_weight, grad_scale, grad_weight, grad_bias, stream))
 
 
 def cgconv_seq_conv(plan, dtype, width, x, weight, bias, activation, lengths, state_in, y, state_out, stream) -> int:
@@ -172,6 +192,23 @@ def cgconv_pack8(dtype, rows, C, x, codes, scales, stream) -> int:
 def cgconv_unpack8(dtype, rows, C, codes, scales, x, stream) -> int:
     P = _main()
     return P._check(P.library().cgconv_unpack8(dtype, rows, C, codes, scales, x, stream))
+
+
+def cgconv_clip_workspace(counts) -> int:
+    """Workspace bytes of a clipping of tensors of these numbers of values."""
+    P = _main()
+    n = P.library().cgconv_clip_workspace(len(counts), (ctypes.c_int64 * len(counts))(*counts))
+    P._check(min(n, 0))
+    return n
+
+
+def cgconv_clip(dtypes, counts, grads, out, max_norm, eps, norm, workspace, workspace_bytes, stream) -> int:
+    """Clipping of a list of tensors by their global norm (lists of type codes,
+    numbers of values and device pointers)."""
+    P, n = _main(), len(counts)
+    return P._check(P.library().cgconv_clip(
+        n, (ctypes.c_int32 * n)(*dtypes), (ctypes.c_int64 * n)(*counts), (_vp * n)(*grads), (_vp * n)(*out), max_norm, eps,
+        norm, workspace, workspace_bytes, stream))
 
 
 # ---- tensors -------------------------------------------------------------------
@@ -258,6 +295,45 @@ def checkpoint_unpack(codes, scales, dtype=None, out=None):
     C = codes.shape[-1]
     cgconv_unpack8(code, codes.numel() // C, C, *args, P._current_stream(torch))
     return out
+
+
+def _list_of(name, tensors, device):
+    """Type codes, sizes and addresses of a list of contiguous GPU tensors."""
+    import torch
+    codes, counts, addresses = [], [], []
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name}[{i}] must be a contiguous GPU tensor")
+        if t.get_device() != device:
+            raise ValueError(f"{name}[{i}] is on GPU {t.get_device()}, which is not current")
+        codes.append(_dtype_code(f"{name}[{i}]", t.dtype))
+        counts.append(t.numel())
+        addresses.append(t.data_ptr())
+    return codes, counts, addresses
+
+
+def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None):
+    """Clips contiguous fp32 or bf16 GPU tensors of any shapes by their global
+    norm: each is multiplied by min(1, max_norm / (norm + eps)), in place or into
+    the tensors of ``out``.  Returns the norm before, a float32 tensor of no
+    dimensions (nothing waits for the GPU).  max_norm = inf: the norm alone."""
+    import torch
+    P = _main()
+    grads = list(grads)
+    device = torch.cuda.current_device()
+    codes, counts, addresses = _list_of("grads", grads, device)
+    to = addresses
+    if out is not None:
+        out = list(out)
+        out_codes, out_counts, to = _list_of("out", out, device)
+        if out_codes != codes or out_counts != counts:
+            raise ValueError("out must hold tensors of the gradients' types and sizes")
+    on = torch.device("cuda", device)
+    size = cgconv_clip_workspace(counts)
+    workspace, norm = torch.empty(size, dtype=torch.uint8, device=on), torch.empty((), dtype=torch.float32, device=on)
+    cgconv_clip(codes, counts, addresses, to, max_norm, eps, norm.data_ptr(), workspace.data_ptr(), size,
+                P._current_stream(torch))
+    return norm
 
 
 def _want_checkpoint(checkpoint) -> bool:
@@ -383,6 +459,48 @@ class SequencePlan:
                  self._new((self.C,), f32, need_bias))
         self._done(self._lib.cgconv_seq_norm_backward(*args, *(None if t is None else t.data_ptr() for t in grads),
                                                       self._raw_stream(dev)))
+        return grads
+
+    # ---- norms around a residual connection
+
+    def _residual_args(self, x, u, gate, post_weight, scale, weight):
+        dtype, code = _features_dtype("x", x)
+        dev, f32, per = self.device, self._f32, (self.L_max + 1, self.C)
+        return dtype, (self._h, code, _tensor("x", x, self.shape, dtype, dev), _tensor("u", u, self.shape, dtype, dev),
+                       _tensor("gate", gate, self.shape[:2] + (self.C,), dtype, dev),
+                       _tensor("post_weight", post_weight, per, f32, dev), _tensor("scale", scale, (self.C,), f32, dev),
+                       _tensor("weight", weight, per, f32, dev))
+
+    def residual_norm(self, x, u, gate=None, post_weight=None, scale=None, weight=None, bias=None, eps: float = 1e-5,
+                      out_r=None, out_y=None):
+        """The norms on both sides of a residual connection: r = x + scale
+        silu(gate) post_weight norm(u) and y = weight norm(r) + bias, norms by
+        degree.  gate [batch, N, C] of x's type, post_weight and weight [L_max+1,
+        C], scale and bias [C] in fp32; each may be None.  Returns (r, y, stats
+        [batch, N, 2 (L_max+2)])."""
+        dtype, args = self._residual_args(x, u, gate, post_weight, scale, weight)
+        pb = _tensor("bias", bias, (self.C,), self._f32, self.device)
+        r, pr = self._out(out_r, x, self.shape)
+        y, py = self._out(out_y, x, self.shape)
+        stats = self._new(self.shape[:2] + (2 * (self.L_max + 2),), self._f32)
+        self._done(self._lib.cgconv_seq_residual_norm(*args, pb, eps, pr, py, stats.data_ptr(),
+                                                      self._raw_stream(self.device)))
+        return r, y, stats
+
+    def residual_norm_backward(self, x, u, gate, post_weight, scale, weight, stats, grad_r, grad_y, need=(True,) * 7):
+        """Gradients of (x, u, gate, post_weight, scale, weight, bias) given those
+        of r (or None) and y and the forward's stats; None where ``need`` is False."""
+        if not any(need):
+            return (None,) * 7
+        dtype, args = self._residual_args(x, u, gate, post_weight, scale, weight)
+        dev, f32, lead = self.device, self._f32, self.shape[:2]
+        args += (_tensor("stats", stats, lead + (2 * (self.L_max + 2),), f32, dev),
+                 _tensor("grad_r", grad_r, self.shape, dtype, dev), _tensor("grad_y", grad_y, self.shape, dtype, dev))
+        per, one = ((self.L_max + 1, self.C), f32), ((self.C,), f32)
+        shapes = ((self.shape, dtype), (self.shape, dtype), (lead + (self.C,), dtype), per, one, per, one)
+        grads = tuple(self._new(*s, n) for s, n in zip(shapes, need))
+        self._done(self._lib.cgconv_seq_residual_norm_backward(
+            *args, *(None if t is None else t.data_ptr() for t in grads), self._raw_stream(dev)))
         return grads
 
     # ---- short causal convolution
@@ -723,3 +841,41 @@ def cgconv_delta_rule(q, k, v, decay, beta, plan: SequencePlan, scale=None, norm
         _functions["rule"] = _rule_function()
     y, last = _functions["rule"].apply(q, k, v, decay, beta, state, lengths, plan, scale, normalize, packed)
     return (y, last) if return_state else y
+
+
+def _residual_function():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class _ResidualFn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, u, gate, post_weight, scale, weight, bias, plan, eps, packed):
+            r, y, stats = plan.residual_norm(x, u, gate, post_weight, scale, weight, bias, eps)
+            keep(ctx, packed, (x, u), (gate, post_weight, scale, weight, bias, stats))
+            ctx.plan = plan
+            ctx.set_materialize_grads(False)
+            return r, y
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_r, grad_y):
+            (x, u), (gate, post_weight, scale, weight, bias, stats) = kept(ctx)
+            grad_r = None if grad_r is None else _whole(grad_r)
+            grad_y = torch.zeros_like(x) if grad_y is None else _whole(grad_y)
+            need = tuple(n and t is not None
+                         for n, t in zip(ctx.needs_input_grad, (x, u, gate, post_weight, scale, weight, bias)))
+            return ctx.plan.residual_norm_backward(x, u, gate, post_weight, scale, weight, stats, grad_r, grad_y,
+                                                   need) + (None,) * 3
+
+    return _ResidualFn
+
+
+def cgconv_residual_norm(x, u, gate, post_weight, scale, weight, bias, plan: SequencePlan, eps: float = 1e-5,
+                         checkpoint=None):
+    """Differentiable norms around a residual connection
+    (:meth:`SequencePlan.residual_norm`): (r, y).  checkpoint="int8": x and u are
+    kept for the backward pass in 8 bits."""
+    packed = _want_checkpoint(checkpoint) and _grad_wanted(x, u, gate, post_weight, scale, weight, bias)
+    if "residual" not in _functions:
+        _functions["residual"] = _residual_function()
+    return _functions["residual"].apply(x, u, gate, post_weight, scale, weight, bias, plan, eps, packed)
