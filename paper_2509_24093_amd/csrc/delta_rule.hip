@@ -513,6 +513,7 @@ hipError_t by_width(int KB, F f) {
 
 template <class T>
 hipError_t prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s) {
+  if (!launch_fits(w.chunks, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid(w.chunks, w.units);
   return by_width(w.KB, [&](auto kb) {
     constexpr int KB = decltype(kb)::value;
