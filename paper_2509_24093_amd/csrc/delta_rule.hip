@@ -39,109 +39,150 @@ __device__ __forceinline__ int tokens_of(const RuleArgs& a, int b) {
 
 // ---- the triangles ------------------------------------------------------------------
 
-// Eight elements of a token's row as an operand, and their sum of squares.
-template <class T>
-__device__ __forceinline__ float operand_row(const T* p, int n, Frag (&f)[kParts<T>]) {
-  float x[8], s = 0.f;
-  row8(p, n, x);
-  parts8<T>(x, f);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
-  return s;
-}
-
-// Block (chunk, unit) of four waves; wave w has the tile of rows 16 w.
-// Bound by latency: a chunk is 20 products of 16 x 16 and a chain of 15 + 3 steps.
-template <class T, int KB, bool TRANSPOSED>
+// Block (chunk, unit) of four waves; wave w has the tile of rows 16 w.  BACKWARD: the inverse
+// also transposed, P only transposed.  Bound by latency: a chunk is 24 products of 16 x 16
+// over D and a chain of 3 + 3 joined blocks.
+template <class T, int KB, bool BACKWARD>
 __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws) {
-  constexpr int NP = kParts<T>, kRow = kT + 1;
-  __shared__ float tri[kT * kRow], inv[kT * kRow];
-  __shared__ float rk[kT], rq[kT], beta[kT];
+  constexpr int NP = kParts<T>, ST = row_stride(KB), kRow = kT + 4;
+  constexpr int kRows = 2 * NP * kT * ST * 2, kTriangles = 2 * kT * kRow * 4;
+  // the keys and queries, and the triangle and its inverse where they have been
+  __shared__ __attribute__((aligned(16))) char space[kRows > kTriangles ? kRows : kTriangles];
+  __shared__ float4 tok[kT];  // beta, rk; the second of Token's z, w
+  __shared__ float rq[kT];
   __shared__ double sum[kT];
+  auto& kbuf = reinterpret_cast<bf16(*)[NP][kT * ST]>(space)[0];
+  auto& qbuf = reinterpret_cast<bf16(*)[NP][kT * ST]>(space)[1];
+  float* tri = reinterpret_cast<float*>(space);
+  float* inv = tri + kT * kRow;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
   const int chunk = blockIdx.x, unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H;
   const int t0 = chunk * kT, tokens = min(tokens_of(a, b) - t0, kT);
   if (tokens <= 0) return;
-  const int D = a.n.D, hk = h / (a.n.H / a.n.Hk);
-  const long long stride = (long long)a.n.Hk * D;
+  const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), stride = a.n.Hk * D;
   const long long row0 = ((long long)b * a.n.N + t0) * stride + (long long)hk * D;
-  const T* K = static_cast<const T*>(a.k) + row0;
-  const T* Q = static_cast<const T*>(a.q) + row0;
-  // the own tile's keys, as columns of the product and for the norms
-  Frag own[KB][NP];
-  const int t = 16 * wave + m;
-  float sk = 0.f, sq = 0.f;
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb) {
-    const int d = 32 * kb + 8 * q, n = t < tokens ? max(0, D - d) : 0;
-    sk += operand_row(K + t * stride + d, n, own[kb]);
-    Frag f[NP];
-    sq += operand_row(Q + t * stride + d, n, f);
-  }
+  const long long at = (long long)unit * ws.chunks + chunk;
+  RowStage<T, KB, 256> sk, sq;
+  sk.load(static_cast<const T*>(a.k) + row0, stride, tokens, D, tid);
+  sq.load(static_cast<const T*>(a.q) + row0, stride, tokens, D, tid);
   if (wave == 0) {
-    double g = 0.0;
-    float bt = 0.f;
-    if (lane < tokens) {
-      const long long at = ((long long)b * a.n.N + t0 + lane) * a.n.H + h;
-      const float x = a.decay[at];
-      g = x < kLowestDecay ? kLowestDecay : x;
-      bt = a.beta[at];
-    }
-    beta[lane] = bt;
+    const long long gate = ((long long)b * a.n.N + t0 + min(lane, tokens - 1)) * a.n.H + h;
+    const float x = a.decay[gate], bt = a.beta[gate];
+    double g = lane < tokens ? x < kLowestDecay ? kLowestDecay : x : 0.f;
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) {
       const double o = __shfl_up(g, s);
       if (lane >= s) g += o;
     }
+    g *= 1.4426950408889634;  // log2(e)
     sum[lane] = g;
+    const float hi = (float)g;
+    tok[lane] = make_float4(lane < tokens ? bt : 0.f, 0.f, hi, (float)(g - hi));
   }
-  sk += __shfl_xor(sk, 16);
-  sk += __shfl_xor(sk, 32);
-  sq += __shfl_xor(sq, 16);
-  sq += __shfl_xor(sq, 32);
-  if (q == 0) {
-    rk[t] = a.normalize ? 1.f / __builtin_sqrtf(sk + kRuleNormEps) : 1.f;
-    rq[t] = a.normalize ? 1.f / __builtin_sqrtf(sq + kRuleNormEps) : 1.f;
+  sk.store(kbuf, tokens, D, tid);
+  sq.store(qbuf, tokens, D, tid);
+  __syncthreads();
+  const int t = 16 * wave + m;
+  // products of all pairs on and below the diagonal: kk and (forward) qk with rows j and the own
+  // tile's columns i, (backward) kq with rows i and the own tile's columns j; a lane has four of its row
+  v4f kk[kTiles], pq[kTiles], qq{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kTiles; ++j) kk[j] = pq[j] = qq;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    Frag ownk[NP], ownq[NP];
+    rows_frag<NP, ST>(kbuf, wave, kb, m, q, ownk);
+    rows_frag<NP, ST>(qbuf, wave, kb, m, q, ownq);
+    qq = mma(ownq, ownq, qq);
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) {
+      Frag f[NP];
+      if (j <= wave) {
+        rows_frag<NP, ST>(kbuf, j, kb, m, q, f);
+        kk[j] = mma(f, ownk, kk[j]);
+        if (!BACKWARD) pq[j] = mma(f, ownq, pq[j]);
+      }
+      if (BACKWARD && j >= wave) {
+        rows_frag<NP, ST>(qbuf, j, kb, m, q, f);
+        pq[j] = mma(f, ownk, pq[j]);
+      }
+    }
   }
-  v4f acc[kTiles];
+  // the norms are the diagonals
+#pragma unroll
+  for (int j = 0; j < kTiles; ++j)
+    if (j == wave) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * q + r == m) {
+          tok[t].y = a.normalize ? 1.f / __builtin_sqrtf(kk[j][r] + kRuleNormEps) : 1.f;
+          rq[t] = a.normalize ? 1.f / __builtin_sqrtf(qq[r] + kRuleNormEps) : 1.f;
+        }
+    }
+  __syncthreads();
+  const float4 me = tok[t];
+  const float sq_ = a.scale * (BACKWARD ? 1.f : rq[t]);
 #pragma unroll
   for (int j = 0; j < kTiles; ++j) {
-    acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
-    if (j > wave) continue;
+    v4f p = pq[j];
+    if (j <= wave) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int u = 16 * j + m, d = 32 * kb + 8 * q;
-      Frag f[NP];
-      operand_row(K + u * stride + d, u < tokens ? max(0, D - d) : 0, f);
-      acc[j] = mma(f, own[kb], acc[j]);  // rows j, columns of the own tile: a lane has four j of its row
+      for (int r = 0; r < 4; ++r) {
+        const int u = 16 * j + 4 * q + r;
+        const float4 other = tok[u];
+        const float f = decay_between(me, other) * other.y;
+        tri[t * kRow + u] = t > u ? me.x * me.y * f * kk[j][r] : 0.f;
+        if (!BACKWARD) p[r] = t >= u ? p[r] * f * sq_ : 0.f;
+      }
+      if (!BACKWARD)
+        ws.inside[(at * kBlocks + block_of(wave, j)) * 64 + lane] = make_float4(p[0], p[1], p[2], p[3]);
+    }
+    if (BACKWARD && j >= wave) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int u = 16 * j + 4 * q + r;
+        p[r] = u >= t ? p[r] * decay_between(tok[u], me) * (rq[u] * me.y * sq_) : 0.f;
+      }
+      ws.inside[(at * kBlocks + block_of(j, wave)) * 64 + lane] = make_float4(p[0], p[1], p[2], p[3]);
     }
   }
   __syncthreads();
-  const double mine = sum[t];
-#pragma unroll
-  for (int j = 0; j < kTiles; ++j) {
-    if (j > wave) continue;
+  // Diagonal blocks: the inverse of blocks twice as large, X <- X - X C X with C the part of A
+  // that joins two of them.  X is held as it accumulates and transposed: the one is an operand
+  // of the other's products as it is.
+  {
+    v4f row, col;  // A: row m, columns 4 q + r; column m, rows 4 q + r
+    const float* at = tri + 16 * wave * kRow + 16 * wave;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int u = 16 * j + 4 * q + r;
-      tri[t * kRow + u] = t > u ? beta[t] * (rk[t] * rk[u]) * expf((float)(mine - sum[u])) * acc[j][r] : 0.f;
+      row[r] = at[m * kRow + 4 * q + r];
+      col[r] = at[(4 * q + r) * kRow + m];
     }
-  }
-  __syncthreads();
-  // diagonal blocks: column m of the inverse, row after row
-  {
-    float x[16];
+    const auto joins = [](int i, int j, int size) { return ((i ^ j) & -size) == size && (i & size); };
+    v4f X, Xt;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float s = r == m ? 1.f : 0.f;
-#pragma unroll
-      for (int c = 0; c < r; ++c) s = fmaf(-tri[(16 * wave + r) * kRow + 16 * wave + c], x[c], s);
-      x[r] = s;
+    for (int r = 0; r < 4; ++r) {
+      const int i = 4 * q + r;
+      X[r] = (i == m ? 1.f : 0.f) - (joins(i, m, 1) ? col[r] : 0.f);
+      Xt[r] = (i == m ? 1.f : 0.f) - (joins(m, i, 1) ? row[r] : 0.f);
     }
-    if (q == 0) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) inv[(16 * wave + r) * kRow + 16 * wave + m] = x[r];
+    for (int size = 2; size < 16; size *= 2) {
+      v4f P{0.f, 0.f, 0.f, 0.f}, Q = P;  // C X and its transpose's counterpart
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        P = __builtin_amdgcn_mfma_f32_16x16x4f32(joins(m, 4 * q + e, size) ? row[e] : 0.f, X[e], P, 0, 0, 0);
+        Q = __builtin_amdgcn_mfma_f32_16x16x4f32(joins(4 * q + e, m, size) ? col[e] : 0.f, Xt[e], Q, 0, 0, 0);
+      }
+      const v4f x = X, xt = Xt;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        X = __builtin_amdgcn_mfma_f32_16x16x4f32(-xt[e], P[e], X, 0, 0, 0);
+        Xt = __builtin_amdgcn_mfma_f32_16x16x4f32(-x[e], Q[e], Xt, 0, 0, 0);
+      }
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) inv[(16 * wave + 4 * q + r) * kRow + 16 * wave + m] = X[r];
   }
   __syncthreads();
   // block (i, j) = - inv(i, i) sum_{j <= c < i} A(i, c) inv(c, j), by distance i - j
@@ -150,11 +191,13 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
     if (wave >= dist) {
       const int i = wave, j = wave - dist;
       v4f s{0.f, 0.f, 0.f, 0.f};
-      for (int c = j; c < i; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(tri[(16 * i + m) * kRow + 16 * c + 4 * q + e],
-                                                   inv[(16 * c + 4 * q + e) * kRow + 16 * j + m], s, 0, 0, 0);
+      for (int n = 0; n < dist; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = 16 * (j + n) + 4 * q + e;
+          s = __builtin_amdgcn_mfma_f32_16x16x4f32(tri[(16 * i + m) * kRow + c], inv[c * kRow + 16 * j + m], s, 0, 0, 0);
+        }
       v4f o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -164,27 +207,25 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
     }
     __syncthreads();
   }
-  const long long at = (long long)unit * ws.chunks + chunk;
   for (int n = wave; n < kBlocks; n += 4) {
     const int i = row_of(n), j = n - block_of(i, 0);
     const float* p = inv + (16 * i + m) * kRow + 16 * j + 4 * q;
     ws.inv[(at * kBlocks + n) * 64 + lane] = make_float4(p[0], p[1], p[2], p[3]);
-    if (TRANSPOSED) {
+    if (BACKWARD) {
       const float* c = inv + (16 * i + 4 * q) * kRow + 16 * j + m;
       ws.invT[(at * kBlocks + n) * 64 + lane] = make_float4(c[0], c[kRow], c[2 * kRow], c[3 * kRow]);
     }
   }
   if (wave == 0) {
-    const double g = sum[lane], end = sum[kT - 1];
-    const float hi = (float)g;
+    const float4 x = tok[lane];
+    const double end = sum[kT - 1];
+    // a float's exponential is off by its rounding times the number: the rest of the sum makes up for it
+    const float e = __builtin_amdgcn_exp2f(x.z) * fmaf(x.w, 0.6931472f, 1.f), eh = (float)end;
+    const float until = __builtin_amdgcn_exp2f((float)(end - sum[lane]));
     float4* to = ws.token + (at * kT + lane) * 2;
-    const float e = expf(hi) * (1.f + (float)(g - hi));
-    to[0] = make_float4(beta[lane], rk[lane] * e, rk[lane] * expf((float)(end - g)), a.scale * rq[lane] * e);
-    to[1] = make_float4(rk[lane], rq[lane], hi, (float)(g - hi));
-    if (lane == 0) {
-      const float eh = (float)end;
-      ws.whole[at] = expf(eh) * (1.f + (float)(end - eh));
-    }
+    to[0] = make_float4(x.x, x.y * e, x.y * until, a.scale * rq[lane] * e);
+    to[1] = make_float4(x.y, rq[lane], x.z, x.w);
+    if (lane == 0) ws.whole[at] = __builtin_amdgcn_exp2f(eh) * fmaf((float)(end - eh), 0.6931472f, 1.f);
   }
 }
 
@@ -198,23 +239,24 @@ enum Walk {
              // vector with no values written, which is the segment's matrix
 };
 
-// Block (group of 16 NW columns, unit, segment).  The columns of kSpan are the VP of the
+// Block (group of 16 NW CT columns, unit, segment); a wave has CT tiles of 16 side by side.  The columns of kSpan are the VP of the
 // values, then those of the matrix.
-template <class T, int KB, int NW, int WALK>
+template <class T, int KB, int NW, int CT, int WALK>
 __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs ws) {
-  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, kThreads = 64 * NW;
+  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * NW;
   constexpr bool kOut = WALK == kOutputs;
-  __shared__ __attribute__((aligned(16))) bf16 kbuf[NP][kT * ST];
-  __shared__ __attribute__((aligned(16))) bf16 qbuf[kOut ? NP : 1][kOut ? kT * ST : 1];
-  __shared__ TriangleParts inv, inside;
-  __shared__ float4 ta[kT], tb[kT];
+  typedef Stage<T, KB, kOut, kOut> Buffer;
+  constexpr int ST = Buffer::ST;
+  __shared__ Buffer buffers[Buffer::kCount];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int first = (blockIdx.x * NW + wave) * 16, col = first + m;
+  const int first = (blockIdx.x * NW + wave) * 16 * CT;
   const bool active = first < (kOut ? ws.V : WALK == kKeep ? ws.VP : ws.VP + 32 * KB);
   const bool matrix = WALK == kSpan && first >= ws.VP;
-  const Column column(col, ws.V, C / a.n.H, C, h);
+  Column column[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) column[t] = Column(first + 16 * t + m, ws.V, C / a.n.H, C, h);
   const int length = tokens_of(a, b);
   const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
   const int end = min((length + kT - 1) / kT, last);
@@ -225,95 +267,100 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
   T* y = static_cast<T*>(a.y) + (kOut ? (long long)b * N * KC : 0);
   const long long start = ((long long)unit * ws.segments + seg) * (32 * KB);  // row of a segment's state
 
-  v4f S[DT];
+  v4f S[CT][DT];
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
+  for (int t = 0; t < CT; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = 16 * d + 4 * q + r;
-      float x = 0.f;
-      if (WALK == kSpan) {
-        x = matrix && row == col - ws.VP ? 1.f : 0.f;
-      } else if (seg > 0) {
-        if (first < ws.VP) x = ws.start[(start + row) * ws.VP + col];
-      } else if (a.state_in && column.there && row < D) {
-        x = a.state_in[((long long)b * D + row) * KC + column.at];
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * d + 4 * q + r, col = first + 16 * t + m;
+        float x = 0.f;
+        if (WALK == kSpan) {
+          x = matrix && row == col - ws.VP ? 1.f : 0.f;
+        } else if (seg > 0) {
+          if (col < ws.VP) x = ws.start[(start + row) * ws.VP + col];
+        } else if (a.state_in && column[t].there && row < D) {
+          x = a.state_in[((long long)b * D + row) * KC + column[t].at];
+        }
+        S[t][d][r] = x;
       }
-      S[d][r] = x;
-    }
 
   RowStage<T, KB, kThreads> sk, sq;
-  BlockStage<kThreads> si;
+  BlockStage<kThreads> si, sp;
   float4 st;
-  ColumnStage<T> sv;
+  ColumnStage<T> sv[CT];
   const auto fetch = [&](int c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
     sk.load(K + (long long)c * kT * stride, stride, tokens, D, tid);
     if (kOut) sq.load(Q + (long long)c * kT * stride, stride, tokens, D, tid);
     si.load(ws.inv + at * kBlocks * 64, tid);
-    st = ws.token[at * 2 * kT + (tid & (2 * kT - 1))];
+    if (kOut) sp.load(ws.inside + at * kBlocks * 64, tid);
+    st = ws.token[(at * kT + (tid & (kT - 1))) * 2];
+  };
+  const auto put = [&](int c, Buffer& to) {
+    const int tokens = min(length - c * kT, kT);
+    sk.store(to.k, tokens, D, tid);
+    if constexpr (kOut) sq.store(to.q, tokens, D, tid);
+    si.store(to.inv, tid);
+    if constexpr (kOut) sp.store(to.inside, tid);
+    if (tid < kT) to.token[tid] = st;
   };
   const auto fetch_values = [&](int c) {
-    sv.load(v + (long long)c * kT * KC, KC, min(length - c * kT, kT), column, q);
+#pragma unroll
+    for (int t = 0; t < CT; ++t) sv[t].load(v + (long long)c * kT * KC, KC, min(length - c * kT, kT), column[t], q);
   };
   if (begin < end) {
     fetch(begin);
     fetch_values(begin);
+    if (Buffer::kCount == 2) {
+      put(begin, buffers[0]);
+      if (begin + 1 < end) fetch(begin + 1);
+    }
   }
   for (int c = begin; c < end; ++c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
-    __syncthreads();  // the chunk before has been read
-    sk.store(kbuf, tokens, D, tid);
-    if constexpr (kOut) sq.store(qbuf, tokens, D, tid);
-    si.store(inv, tid);
-    if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = st;
+    Buffer& buf = buffers[(c - begin) & (Buffer::kCount - 1)];
     const float whole = ws.whole[at];
-    __syncthreads();
-    if (c + 1 < end) fetch(c + 1);
-    // P, transposed: rows j, columns i, so that a lane has four j of its row
-    if constexpr (kOut) {
-      for (int n = wave; n < kBlocks; n += NW) {
-        const int ib = row_of(n), j = n - block_of(ib, 0);
-        v4f p{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          Frag fk[NP], fq[NP];
-          rows_frag<NP, ST>(kbuf, j, kb, m, q, fk);
-          rows_frag<NP, ST>(qbuf, ib, kb, m, q, fq);
-          p = mma(fk, fq, p);
-        }
-        const int i = 16 * ib + m;
-        const float4 me = tb[i];
-        const float f = a.scale * me.y;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int u = 16 * j + 4 * q + r;
-          const float4 other = tb[u];
-          p[r] = i >= u ? p[r] * (f * other.x) * decay_between(me, other) : 0.f;
-        }
-        put_block(inside, n, lane, p[0], p[1], p[2], p[3]);
-      }
+    __syncthreads();  // the chunk is there; the one before has been read
+    if (Buffer::kCount == 1) {
+      put(c, buf);
+      __syncthreads();
+      if (c + 1 < end) fetch(c + 1);
     }
-    v4f X[kTiles], O[kTiles];
+    const auto& kbuf = buf.k;
+    const auto& qbuf = buf.q;
+    const auto& inv = buf.inv;
+    const auto& inside = buf.inside;
+    const float4* ta = buf.token;
+    v4f X[CT][kTiles], O[CT][kTiles];
     if (active) {
-      if constexpr (WALK == kKeep) store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, col, q, S);
+      if constexpr (WALK == kKeep) {
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) X[i] = O[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < CT; ++t)
+          store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, first + 16 * t + m, q, S[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) X[t][i] = O[t][i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        Frag s[3];
-        split_tiles(S[2 * kb], S[2 * kb + 1], s);
+        Frag s[CT][3];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          Frag f[NP];
-          rows_frag<NP, ST>(kbuf, i, kb, m, q, f);
-          X[i] = mma(f, s, X[i]);
-          if constexpr (kOut) {
-            rows_frag<NP, ST>(qbuf, i, kb, m, q, f);
-            O[i] = mma(f, s, O[i]);
-          }
+        for (int t = 0; t < CT; ++t) split_tiles(S[t][2 * kb], S[t][2 * kb + 1], s[t]);
+        Frag f[kTiles][NP];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) rows_frag<NP, ST>(kbuf, i, kb, m, q, f[i]);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) mma_all(f, s[t], X[t]);
+        if constexpr (kOut) {
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) rows_frag<NP, ST>(qbuf, i, kb, m, q, f[i]);
+#pragma unroll
+          for (int t = 0; t < CT; ++t) mma_all(f, s[t], O[t]);
         }
       }
       // Y, then V' = (1 + A)^-1 Y
@@ -321,86 +368,108 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float4 t = ta[16 * i + 4 * q + r];
-          X[i][r] = t.x * fmaf(-t.y, X[i][r], sv.get(i, r, column));
-          O[i][r] *= t.w;
+          const float4 tok = ta[16 * i + 4 * q + r];
+#pragma unroll
+          for (int t = 0; t < CT; ++t) {
+            X[t][i][r] = tok.x * fmaf(-tok.y, X[t][i][r], sv[t].get(i, r, column[t]));
+            O[t][i][r] *= tok.w;
+          }
         }
       if (c + 1 < end) fetch_values(c + 1);
-      Frag fy[2][3];
+      Frag fy[CT][2][3];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fy[kb]);
+      for (int t = 0; t < CT; ++t)
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        X[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int kb = 0; kb < 2; ++kb) split_tiles(X[t][2 * kb], X[t][2 * kb + 1], fy[t][kb]);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-          if (triangle_has<false>(i, kb)) {
-            Frag f[3];
-            triangle_frag<false>(inv, i, kb, lane, f);
-            X[i] = mma(f, fy[kb], X[i]);
-          }
+      for (int t = 0; t < CT; ++t) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) X[t][i] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inv, kb, lane, fy[t][kb], X[t]);
       }
     }
-    if constexpr (kOut) __syncthreads();  // P is there
+    if (Buffer::kCount == 2 && c + 1 < end) {
+      put(c + 1, buffers[(c + 1 - begin) & 1]);
+      if (c + 2 < end) fetch(c + 2);
+    }
     if (!active) continue;
-    if constexpr (WALK == kKeep) store_tiles(ws.value + at * kT * ws.VP, ws.VP, col, q, X);
+    if constexpr (WALK == kKeep) {
+#pragma unroll
+      for (int t = 0; t < CT; ++t) store_tiles(ws.value + at * kT * ws.VP, ws.VP, first + 16 * t + m, q, X[t]);
+    }
     if constexpr (kOut) {
-      Frag fv[2][3];
+      Frag fv[CT][2][3];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fv[kb]);
+      for (int t = 0; t < CT; ++t)
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i)
+        for (int kb = 0; kb < 2; ++kb) split_tiles(X[t][2 * kb], X[t][2 * kb + 1], fv[t][kb]);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-          if (triangle_has<false>(i, kb)) {
-            Frag f[3];
-            triangle_frag<false>(inside, i, kb, lane, f);
-            O[i] = mma(f, fv[kb], O[i]);
-          }
-      store_column(y + (long long)c * kT * KC, KC, N - c * kT, tokens, column, q, O);
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inside, kb, lane, fv[t][kb], O[t]);
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+        store_column(y + (long long)c * kT * KC, KC, N - c * kT, tokens, column[t], q, O[t]);
     }
     // S <- e^{G_end} S + K^T (e^{G_end - G} rk V')
-    Frag fz[2][3];
+    Frag fz[CT][2][3];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) X[i][r] *= ta[16 * i + 4 * q + r].z;
+      for (int r = 0; r < 4; ++r) {
+        const float z = ta[16 * i + 4 * q + r].z;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fz[kb]);
-#pragma unroll
-    for (int d = 0; d < DT; ++d) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) S[d][r] *= whole;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        Frag f[NP];
-        columns_frag<NP, ST>(kbuf, d, kb, m, q, f);
-        S[d] = mma(f, fz[kb], S[d]);
+        for (int t = 0; t < CT; ++t) X[t][i][r] *= z;
       }
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) split_tiles(X[t][2 * kb], X[t][2 * kb + 1], fz[t][kb]);
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][d][r] *= whole;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      Frag f[DT][NP];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) columns_frag<NP, ST>(kbuf, d, kb, m, q, f[d]);
+#pragma unroll
+      for (int t = 0; t < CT; ++t) mma_all(f, fz[t][kb], S[t]);
     }
   }
   if constexpr (WALK == kSpan) {
     if (!active) return;
-    if (!matrix) {
-      store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S);
-    } else {
-      float* to = ws.span_matrix + (start + col - ws.VP) * (32 * KB) + 4 * q;  // its columns are rows here
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<v4f*>(to + 16 * d) = S[d];
+    for (int t = 0; t < CT; ++t) {
+      const int col = first + 16 * t + m;
+      if (!matrix) {
+        store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S[t]);
+      } else {
+        float* to = ws.span_matrix + (start + col - ws.VP) * (32 * KB) + 4 * q;  // its columns are rows here
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<v4f*>(to + 16 * d) = S[t][d];
+      }
     }
   }
   if constexpr (kOut) {
-    if (!column.there) return;
-    const long long stop = min((long long)last * kT, (long long)N);
-    for (long long t = (long long)max(end, begin) * kT + q; t < stop; t += 4) y[t * KC + column.at] = (T)0.f;
-    if (!a.state_out || last != ws.chunks) return;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int t = 0; t < CT; ++t) {
+      if (!column[t].there) continue;
+      const long long stop = min((long long)last * kT, (long long)N);
+      for (long long n = (long long)max(end, begin) * kT + q; n < stop; n += 4) y[n * KC + column[t].at] = (T)0.f;
+      if (!a.state_out || last != ws.chunks) continue;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * d + 4 * q + r;
-        if (row < D) a.state_out[((long long)b * D + row) * KC + column.at] = S[d][r];
-      }
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * d + 4 * q + r;
+          if (row < D) a.state_out[((long long)b * D + row) * KC + column[t].at] = S[t][d][r];
+        }
+    }
   }
 }
 
@@ -525,26 +594,31 @@ hipError_t prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_
   });
 }
 
-template <class T, int NW, int WALK>
+template <class T, int NW, int CT, int WALK>
 hipError_t walk(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
+  constexpr int kColumns = 16 * NW * CT;
   const int columns = WALK == kOutputs ? w.V : WALK == kKeep ? w.VP : w.VP + 32 * w.KB;
-  const dim3 grid((columns + 16 * NW - 1) / (16 * NW), w.units, w.segments);
+  const dim3 grid((columns + kColumns - 1) / kColumns, w.units, w.segments);
   return by_width(w.KB, [&](auto kb) {
-    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, NW, WALK>), grid, dim3(64 * NW), 0, s, a, w);
+    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, NW, CT, WALK>), grid, dim3(64 * NW), 0, s, a, w);
     return hipGetLastError();
   });
 }
 
+template <class T, int WALK>
+hipError_t walk_any(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
+  if (WALK != kSpan && w.V <= 64) return walk<T, 4, 1, WALK>(a, w, s);
+  return walk<T, 8, 1, WALK>(a, w, s);
+}
+
 template <class T>
 hipError_t states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s) {
-  hipError_t e = hipSuccess;
   if (w.segments > 1) {
-    e = walk<T, 8, kSpan>(a, w, s);
+    hipError_t e = walk_any<T, kSpan>(a, w, s);
     if (e == hipSuccess) e = launch_rule_join(a.state_in, w, a.n, false, s);
     if (e != hipSuccess) return e;
   }
-  if (w.V <= 64) return backward ? walk<T, 4, kKeep>(a, w, s) : walk<T, 4, kOutputs>(a, w, s);
-  return backward ? walk<T, 8, kKeep>(a, w, s) : walk<T, 8, kOutputs>(a, w, s);
+  return backward ? walk_any<T, kKeep>(a, w, s) : walk_any<T, kOutputs>(a, w, s);
 }
 
 template <class T>

@@ -44,11 +44,10 @@ __device__ __forceinline__ int tokens_of(const RuleArgs& a, int b) {
 // state's gradient.
 template <class T, int KB, int NW, bool SPAN>
 __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
-  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, kThreads = 64 * NW;
-  __shared__ __attribute__((aligned(16))) bf16 kbuf[NP][kT * ST];
-  __shared__ __attribute__((aligned(16))) bf16 qbuf[NP][kT * ST];
-  __shared__ TriangleParts inv, inside;  // the transposed triangles
-  __shared__ float4 ta[kT], tb[kT];
+  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * NW;
+  typedef Stage<T, KB, true, true> Buffer;  // the transposed triangles
+  constexpr int ST = Buffer::ST;
+  __shared__ Buffer buffers[Buffer::kCount];
   const RuleArgs& a = g.a;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
@@ -83,7 +82,7 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
     }
 
   RowStage<T, KB, kThreads> sk, sq;
-  BlockStage<kThreads> si;
+  BlockStage<kThreads> si, sp;
   float4 st;
   ColumnStage<T> so;
   const auto fetch = [&](int c) {
@@ -92,45 +91,41 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
     sk.load(K + (long long)c * kT * stride, stride, tokens, D, tid);
     sq.load(Q + (long long)c * kT * stride, stride, tokens, D, tid);
     si.load(ws.invT + at * kBlocks * 64, tid);
-    st = ws.token[at * 2 * kT + (tid & (2 * kT - 1))];
+    sp.load(ws.inside + at * kBlocks * 64, tid);
+    st = ws.token[(at * kT + (tid & (kT - 1))) * 2];
+  };
+  const auto put = [&](int c, Buffer& to) {
+    const int tokens = min(length - c * kT, kT);
+    sk.store(to.k, tokens, D, tid);
+    sq.store(to.q, tokens, D, tid);
+    si.store(to.inv, tid);
+    sp.store(to.inside, tid);
+    if (tid < kT) to.token[tid] = st;
   };
   if (begin < end) {
     fetch(end - 1);
     so.load(gy + (long long)(end - 1) * kT * KC, KC, min(length - (end - 1) * kT, kT), column, q);
+    if (Buffer::kCount == 2) {
+      put(end - 1, buffers[0]);
+      if (end - 2 >= begin) fetch(end - 2);
+    }
   }
   for (int c = end - 1; c >= begin; --c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
-    __syncthreads();  // the chunk before has been read
-    sk.store(kbuf, tokens, D, tid);
-    sq.store(qbuf, tokens, D, tid);
-    si.store(inv, tid);
-    if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = st;
+    Buffer& buf = buffers[(end - 1 - c) & (Buffer::kCount - 1)];
     const float whole = ws.whole[at];
-    __syncthreads();
-    if (c > begin) fetch(c - 1);
-    // P: rows i, columns j, so that a lane has four i of its column
-    for (int n = wave; n < kBlocks; n += NW) {
-      const int i = row_of(n), jb = n - block_of(i, 0);
-      v4f p{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        Frag fk[NP], fq[NP];
-        rows_frag<NP, ST>(kbuf, jb, kb, m, q, fk);
-        rows_frag<NP, ST>(qbuf, i, kb, m, q, fq);
-        p = mma(fq, fk, p);
-      }
-      const int j = 16 * jb + m;
-      const float4 me = tb[j];
-      const float f = a.scale * me.x;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int u = 16 * i + 4 * q + r;
-        const float4 other = tb[u];
-        p[r] = u >= j ? p[r] * (f * other.y) * decay_between(other, me) : 0.f;
-      }
-      put_block(inside, n, lane, p[0], p[1], p[2], p[3]);
+    __syncthreads();  // the chunk is there; the one before has been read
+    if (Buffer::kCount == 1) {
+      put(c, buf);
+      __syncthreads();
+      if (c > begin) fetch(c - 1);
     }
+    const auto& kbuf = buf.k;
+    const auto& qbuf = buf.q;
+    const auto& inv = buf.inv;
+    const auto& inside = buf.inside;
+    const float4* ta = buf.token;
     v4f X[kTiles];
     if (active) {
       if (!SPAN) store_tiles(ws.gstate + at * (32 * KB) * ws.VP, ws.VP, col, q, S);
@@ -140,19 +135,20 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
       for (int kb = 0; kb < KB; ++kb) {
         Frag s[3];
         split_tiles(S[2 * kb], S[2 * kb + 1], s);
+        Frag f[kTiles][NP];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          Frag f[NP];
-          rows_frag<NP, ST>(kbuf, i, kb, m, q, f);
-          X[i] = mma(f, s, X[i]);
-        }
+        for (int i = 0; i < kTiles; ++i) rows_frag<NP, ST>(kbuf, i, kb, m, q, f[i]);
+        mma_all(f, s, X);
       }
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) X[i][r] *= ta[16 * i + 4 * q + r].z;
     }
-    __syncthreads();  // P is there
+    if (Buffer::kCount == 2 && c > begin) {
+      put(c - 1, buffers[(end - c) & 1]);
+      if (c - 1 > begin) fetch(c - 2);
+    }
     if (!active) continue;
     // gV', gY
     Frag fo[2][NP];
@@ -164,28 +160,14 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
       parts8<T>(x, fo[kb]);
     }
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-        if (triangle_has<true>(i, kb)) {
-          Frag f[3];
-          triangle_frag<true>(inside, i, kb, lane, f);
-          X[i] = mma(f, fo[kb], X[i]);
-        }
+    for (int kb = 0; kb < 2; ++kb) mma_triangle<true>(inside, kb, lane, fo[kb], X);
     Frag fx[2][3];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fx[kb]);
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      X[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < kTiles; ++i) X[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-        if (triangle_has<true>(i, kb)) {
-          Frag f[3];
-          triangle_frag<true>(inv, i, kb, lane, f);
-          X[i] = mma(f, fx[kb], X[i]);
-        }
-    }
+    for (int kb = 0; kb < 2; ++kb) mma_triangle<true>(inv, kb, lane, fx[kb], X);
     if (!SPAN) store_tiles(ws.gvalue + at * kT * ws.VP, ws.VP, col, q, X);
     // gS <- e^{G_end} gS + Q^T (o gO) - K^T (a gv)
     v4f o[kTiles];
@@ -210,17 +192,18 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
       split_tiles(o[2 * kb], o[2 * kb + 1], fz[kb]);
     }
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int r = 0; r < 4; ++r) S[d][r] *= whole;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        Frag f[NP];
-        columns_frag<NP, ST>(kbuf, d, kb, m, q, f);
-        S[d] = mma(f, fx[kb], S[d]);
-        columns_frag<NP, ST>(qbuf, d, kb, m, q, f);
-        S[d] = mma(f, fz[kb], S[d]);
-      }
+    for (int kb = 0; kb < 2; ++kb) {
+      Frag f[DT][NP];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) columns_frag<NP, ST>(kbuf, d, kb, m, q, f[d]);
+      mma_all(f, fx[kb], S);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) columns_frag<NP, ST>(qbuf, d, kb, m, q, f[d]);
+      mma_all(f, fz[kb], S);
     }
   }
   if constexpr (SPAN) {
@@ -274,7 +257,7 @@ __device__ __forceinline__ void columns8(const T* row, int t, int tokens, int st
   }
 }
 
-constexpr int kMStride = kT + 4;
+constexpr int kMStride = kT + 8;  // as row_stride
 typedef bf16 Square[3][kT * kMStride];  // a 64 x 64 matrix in three parts
 
 // A tile's accumulator (column m, rows 4 q + r) into the matrix.

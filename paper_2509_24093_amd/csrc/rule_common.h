@@ -41,6 +41,7 @@ constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
 
 // Eight values of one lane (one part).
 union Frag {
+  uint4 all;
   uint32_t w[4];
   uint2 h[2];
   v8bf f;
@@ -91,6 +92,20 @@ __device__ __forceinline__ v4f mma(const Frag (&a)[NA], const Frag (&b)[NB], v4f
   return acc;
 }
 
+// acc[i] += A[i] B: the products of one accumulator follow each other only after all the
+// others', so that none waits for the one before (each takes 16 cycles and is done after 32).
+template <int NI, int NA, int NB>
+__device__ __forceinline__ void mma_all(const Frag (&a)[NI][NA], const Frag (&b)[NB], v4f (&acc)[NI]) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int p = 0; p < NA; ++p)
+      if (s - p >= 0 && s - p < NB) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i][p].f, b[s - p].f, acc[i], 0, 0, 0);
+      }
+}
 // Eight elements of a row from p on, n of them there (any n), zeros behind.
 template <class T>
 __device__ __forceinline__ void row8(const T* p, int n, float (&x)[8]) {
@@ -99,9 +114,9 @@ __device__ __forceinline__ void row8(const T* p, int n, float (&x)[8]) {
   raw.widen_to(x);
 }
 
-// Rows of 64 tokens in LDS, one array a part.  Row stride in elements: 8 bytes
-// beyond a multiple of 32 banks' words, so that 16 rows at one column take 32 banks.
-constexpr int row_stride(int KB) { return 32 * KB + 4; }
+// Rows of 64 tokens in LDS, one array a part.  Row stride in elements: an odd multiple of
+// four words, so that 16 rows' words at one column lie in 16 different groups of four banks.
+constexpr int row_stride(int KB) { return 32 * KB + 8; }
 
 __device__ __forceinline__ uint2 lds2(const bf16* p) { return *reinterpret_cast<const uint2*>(p); }
 
@@ -162,21 +177,43 @@ __device__ __forceinline__ constexpr bool triangle_has(int i, int kb) {
   return UPPER ? 2 * kb + 1 >= i : 2 * kb <= i;
 }
 
+// mma_all of a triangle's rows: those without a block in this half are left out.
+template <bool UPPER, int NB>
+__device__ __forceinline__ void mma_triangle(const uint2 (&t)[3][kBlocks][64], int kb, int lane, const Frag (&b)[NB],
+                                             v4f (&acc)[kTiles]) {
+  Frag f[kTiles][3];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+    if (triangle_has<UPPER>(i, kb)) triangle_frag<UPPER>(t, i, kb, lane, f[i]);
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+      if (s - p >= 0 && s - p < NB) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+          if (triangle_has<UPPER>(i, kb))
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i][p].f, b[s - p].f, acc[i], 0, 0, 0);
+      }
+}
+
 // The numbers of a token that its chunk's kernels need, made by rule_prepare_kernel:
 // x = beta, y = rk e^G, z = rk e^(G_end - G), w = scale rq e^G with G the sum of the
 // decays of the chunk up to the token, rk and rq the factors that norm key and query.
-// Second: x = rk, y = rq, z + w = G.
+// Second: x = rk, y = rq, z + w = G log2(e), so that a decay is one exponential of base 2 of
+// a difference rounded once.
 struct Token {
   float4 a, b;
 };
 __device__ __forceinline__ float decay_between(const float4& i, const float4& j) {
-  return __expf((i.z - j.z) + (i.w - j.w));
+  return __builtin_amdgcn_exp2f((i.z - j.z) + (i.w - j.w));
 }
 
 // A head's column (component, channel) in a token's row; columns past V: none.
 struct Column {
   int at;
   bool there;
+  Column() = default;
   __device__ __forceinline__ Column(int col, int V, int P, int C, int h) {
     there = col < V;
     const int k = there ? col / P : 0;
@@ -250,9 +287,7 @@ struct RowStage {
       }
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        uint2* to = reinterpret_cast<uint2*>(buf[i] + row * ST + c);
-        to[0] = f[i].h[0];
-        to[1] = f[i].h[1];
+        *reinterpret_cast<Frag*>(buf[i] + row * ST + c) = f[i];
       }
     }
   }
@@ -274,6 +309,20 @@ struct BlockStage {
       if (at < kBlocks * 64) put_block(t, at >> 6, at & 63, v[p].x, v[p].y, v[p].z, v[p].w);
     }
   }
+};
+
+// A chunk in LDS: its keys, queries, triangles and tokens.  Two of them where they fit: the
+// next one is filled while the waves work on this one, and they meet once a chunk.
+template <class T, int KB, bool QUERIES, bool INSIDE>
+struct Stage {
+  static constexpr int NP = kParts<T>, ST = row_stride(KB);
+  alignas(16) bf16 k[NP][kT * ST];
+  alignas(16) bf16 q[QUERIES ? NP : 1][QUERIES ? kT * ST : 8];
+  TriangleParts inv;
+  uint2 inside[INSIDE ? 3 : 1][INSIDE ? kBlocks : 1][INSIDE ? 64 : 1];
+  float4 token[kT];
+  static constexpr int kBytes = 2 * NP * kT * ST * (QUERIES ? 2 : 1) + (int)sizeof(TriangleParts) * (INSIDE ? 2 : 1) + 16 * kT + 64;
+  static constexpr int kCount = 2 * kBytes <= 160 * 1024 ? 2 : 1;
 };
 
 // The 16 values of a lane's column in a chunk: tokens 16 i + 4 q + r.  In place of a token

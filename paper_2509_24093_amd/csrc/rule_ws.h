@@ -12,7 +12,8 @@ struct RuleWs {
   float4* token;   // [unit][chunk][64][2]: see Token in rule_common.h
   float* whole;    // [unit][chunk]: decay of the whole chunk
   float4* inv;     // [unit][chunk][10 blocks][64 lanes]: (1 + A)^-1, rows
-  float4* invT;    // the same, columns (backward)
+  float4* inside;  // the same of P, rows; of the backward columns
+  float4* invT;    // (1 + A)^-1, columns (backward)
   float* state;    // [unit][chunk][DP][VP]: the state before every chunk (backward)
   float* gstate;   // [unit][chunk][DP][VP]: gradient of the state after every chunk
   float* value;    // [unit][chunk][64][VP]: what the tokens write, V'
@@ -48,6 +49,7 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
   take(w.token, count * kRuleChunk * 2);
   take(w.whole, count);
   take(w.inv, count * kRuleTriangle * 64);
+  take(w.inside, count * kRuleTriangle * 64);
   if (backward) {
     take(w.invT, count * kRuleTriangle * 64);
     take(w.state, count * 32 * w.KB * w.VP);
@@ -66,7 +68,7 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
   return w;
 }
 
-// (1 + A)^-1 and the numbers of every token, of all chunks at once.
+// (1 + A)^-1, P and the numbers of every token, of all chunks at once.
 hipError_t launch_rule_prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
 // The states from chunk to chunk; for the backward they and V' are kept and no output is formed.
 hipError_t launch_rule_states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
