@@ -51,6 +51,20 @@ __device__ __forceinline__ void load_or(const T* p, int n, float none, float (&v
   if (p) load_part<TAIL>(p, n, v);
 }
 
+// V elements at an offset in a tile, zeros where `there` is false (then the tile's first).
+template <bool TAIL, class T, int V>
+__device__ __forceinline__ void load_there(const T* tile, int at, int n, bool there, float (&v)[V]) {
+  if constexpr (TAIL) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    if (there) load_part<true>(tile + at, n, v);
+  } else {
+    load_vec(tile + (there ? at : 0), v);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = there ? v[e] : 0.f;
+  }
+}
+
 // silu(gate) of a block's tokens, one value a thread at a time, where several rows share it.
 template <class T>
 __device__ __forceinline__ void stage_gates(const T* gate, float* to, int n, int threads) {
@@ -125,16 +139,16 @@ __global__ void residual_rows_kernel(ResidualArgs a, RowShape sh) {
     }
   };
   const auto factors = [&](const float* from, float* to, int at) {
+    __syncthreads();
     degree_sums(from, to, toks, degs, a.K, sh.threads, [&](float s, int i, int l) {
       const float r = 1.f / __builtin_sqrtf(s / (float)((2 * l + 1) * a.C) + a.eps);
       if (stats) stats[(long long)(i / degs) * stats_of(a.L) + at + l] = r;
       return r;
     });
+    __syncthreads();
   };
   center(v, sums, 0);
-  __syncthreads();
   factors(sums, ru, 1);
-  __syncthreads();
   float sc[V];
   load_or<TAIL>(col ? a.scale ? a.scale + c : nullptr : nullptr, left, 1.f, sc);
   T* ro = static_cast<T*>(a.r) + base;
@@ -152,9 +166,7 @@ __global__ void residual_rows_kernel(ResidualArgs a, RowShape sh) {
     store_part<TAIL>(ro + (long long)r * a.C + c, left, v[i]);
   }
   center(v, sums2, a.L + 2);
-  __syncthreads();
   factors(sums2, rr, a.L + 3);
-  __syncthreads();
   T* y = static_cast<T*>(a.y) + base;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -171,126 +183,165 @@ __global__ void residual_rows_kernel(ResidualArgs a, RowShape sh) {
   }
 }
 
-// Block b takes tiles b, b + gridDim.x, ... of sh.tokens tokens.  Dynamic LDS: sums of rows
-// and degrees, silu(gate) and the rows' products for the gate's gradient while the tiles run;
-// then the staging of the parameters' sums.  Partial sums of block b: part[b][gw of L + 1
-// degrees, Q of L + 1 degrees, gb][C].
+// Block b takes tiles b, b + gridDim.x, ... of sh.tokens tokens; the next tile's gates are
+// staged, and its statistics, behind this one's first sums, so that the threads meet twice a tile.  Dynamic LDS: sums of rows (twice), silu(gate) (of two tiles) and
+// the rows' products for the gate's gradient while the tiles run; then the staging of the
+// parameters' sums.  Partial sums of block b: part[b][gw of L + 1 degrees, Q of L + 1 degrees,
+// gb][C].  131072 tokens of L=6 C=32 in fp32, 4.9 GB: 1.80 ms with five meetings and nothing
+// asked for ahead.
 constexpr int kResidualRowThreads = 512;
 
-template <class T, int V, int R, bool TAIL>
-__global__ __launch_bounds__(kResidualRowThreads) void residual_rows_bwd_kernel(ResidualBwdArgs g, RowShape sh,
-                                                                                long long tiles) {
+template <class T, int V, int R, int MAXT, bool TAIL>
+__global__ __launch_bounds__(MAXT, R * V <= 8 ? 3 : 2) void residual_rows_bwd_kernel(ResidualBwdArgs g, RowShape sh,
+                                                                                      long long tiles) {
   extern __shared__ float lds[];
   const ResidualArgs& a = g.a;
   const int tid = threadIdx.x, per = sh.threads / sh.lanes;
   const int j = tid & (sh.lanes - 1), rg = tid / sh.lanes;
   const int c = j * V, left = a.C - c, degs = a.L + 1, ns = stats_of(a.L);
-  const bool col = left > 0;
+  const bool col = left > 0, shared = a.gate && a.K > 1;
+  const int rowsum = sh.tokens * a.K, gated = sh.tokens * a.C;
   float* sums = lds;
-  float* ds = sums + sh.tokens * a.K;
-  float* gates = ds + sh.tokens * degs;
-  float* prod = gates + sh.tokens * a.C;  // [rows][C]; both where K > 1
-  float gw[R][V], gq[R][V], gb[V], sc[V];
+  float* gates = sums + 2 * rowsum;
+  float* stats = gates + (a.K > 1 ? 2 * gated : 0);  // of two tiles
+  float* prod = stats + 2 * sh.tokens * ns;          // [rows][C]; the gates too only where K > 1
+  float* slices = prod + rowsum * a.C;               // of prod's sums over a token's rows, [slice][gated]
+  const int count = max(1, min(8, sh.threads / gated));
+  float gw[R][V], gq[R][V], gb[V], f[R][V], w[R][V];  // f: scale post_weight
   int tok[R], comp[R], deg[R];
+  float share[R];  // of an element in its degree's mean
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = i * per + rg;
     tok[i] = divide(r, sh.magic);
     comp[i] = r - tok[i] * a.K;
     deg[i] = degree_of(comp[i]);
+    share[i] = 1.f / (float)((2 * deg[i] + 1) * a.C);
 #pragma unroll
     for (int e = 0; e < V; ++e) gw[i][e] = gq[i][e] = 0.f;
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) gb[e] = 0.f;
-  load_or<TAIL>(col && a.scale ? a.scale + c : nullptr, left, 1.f, sc);
-  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    float sc[V];
+    const int at = deg[i] * a.C + c;
+    const bool on = col && tok[i] < sh.tokens;
+    load_or<TAIL>(on && a.scale ? a.scale + c : nullptr, left, 1.f, sc);
+    load_or<TAIL>(on && a.post_weight ? a.post_weight + at : nullptr, left, 1.f, f[i]);
+    load_or<TAIL>(on && a.weight ? a.weight + at : nullptr, left, 1.f, w[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[i][e] *= sc[e];
+  }
+  const auto stage = [&](long long tile, int half) {
+    const long long t0 = tile * sh.tokens;
+    const int toks = (int)min((long long)sh.tokens, a.tokens - t0);
+    for (int i = tid; i < toks * ns; i += sh.threads) stats[half * sh.tokens * ns + i] = a.stats[t0 * ns + i];
+    if (shared) stage_gates(static_cast<const T*>(a.gate) + t0 * a.C, gates + half * gated, toks * a.C, sh.threads);
+  };
+  if (blockIdx.x < tiles) stage(blockIdx.x, 0);
+  __syncthreads();
+  int half = 0;
+  // the gate's gradient of a tile, a slice of the rows a thread: the slices are added one
+  // barrier later, in the next tile
+  const auto gate_out = [&](long long tile) {
+    const long long t0 = tile * sh.tokens;
+    const int n = (int)min((long long)sh.tokens, a.tokens - t0) * a.C;
+    for (int o = tid; o < n; o += sh.threads) {
+      float s = 0.f;
+      for (int i = 0; i < count; ++i) s += slices[i * gated + o];
+      const long long at = t0 * a.C + o;
+      static_cast<T*>(g.ggate)[at] = (T)(s * silu_slope(widen(static_cast<const T*>(a.gate)[at])));
+    }
+  };
+  const bool gates_wanted = g.ggate && a.K > 1;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, half ^= 1) {
     const long long t0 = tile * sh.tokens, base = t0 * a.K * a.C;
     const int toks = (int)min((long long)sh.tokens, a.tokens - t0);
-    float h[R][V], k[R][V], gy[R][V], G[R][V], ru[R], rr[R], mu[R], mr[R];
+    const T* gate = a.gate ? static_cast<const T*>(a.gate) + t0 * a.C : nullptr;
+    bool there[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) there[i] = col && tok[i] < toks;
+    const auto gate_of = [&](int i, float (&s)[V]) {
+      if (TAIL || !shared) {
+        gates_of<TAIL>(there[i] ? gate : nullptr, gates + half * gated, a.K, tok[i], a.C, c, s);
+      } else {
+        load_vec(gates + half * gated + (there[i] ? tok[i] * a.C + c : 0), s);
+      }
+    };
+    float h[R][V], k[R][V], gy[R][V], G[R][V], fu[R], fr[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
+      const int at = (i * per + rg) * a.C + c;
+      load_there<TAIL>(static_cast<const T*>(a.u) + base, at, left, there[i], h[i]);
+      load_there<TAIL>(static_cast<const T*>(a.x) + base, at, left, there[i], k[i]);
+      load_there<TAIL>(static_cast<const T*>(g.gy) + base, at, left, there[i], gy[i]);
+      load_there<TAIL>(static_cast<const T*>(g.gr ? g.gr : g.gy) + base, at, left, there[i] && g.gr, G[i]);
+    }
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[i][e] = k[i][e] = gy[i][e] = G[i][e] = 0.f;
-      ru[i] = rr[i] = mu[i] = mr[i] = 0.f;
-      if (col && tok[i] < toks) {
-        const long long at = base + (long long)(i * per + rg) * a.C + c;
-        load_part<TAIL>(static_cast<const T*>(a.u) + at, left, h[i]);
-        load_part<TAIL>(static_cast<const T*>(a.x) + at, left, k[i]);
-        load_part<TAIL>(static_cast<const T*>(g.gy) + at, left, gy[i]);
-        if (g.gr) load_part<TAIL>(static_cast<const T*>(g.gr) + at, left, G[i]);
-        const float* st = a.stats + (t0 + tok[i]) * ns;
-        ru[i] = st[1 + deg[i]];
-        rr[i] = st[a.L + 3 + deg[i]];
-        if (comp[i] == 0) {
-          mu[i] = st[0];
-          mr[i] = st[a.L + 2];
-        }
+    for (int i = 0; i < R; ++i) {
+      const float* st = stats + half * sh.tokens * ns + (there[i] ? tok[i] * ns : 0);
+      const float m = comp[i] == 0 ? st[0] : 0.f, m2 = comp[i] == 0 ? st[a.L + 2] : 0.f;
+      fu[i] = there[i] ? st[1 + deg[i]] : 0.f;  // zero: nothing of a lane without a vector remains
+      fr[i] = there[i] ? st[a.L + 3 + deg[i]] : 0.f;
+      float s[V];
+      gate_of(i, s);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float x = (h[i][e] - m) * fu[i], y = (fmaf(x, s[e] * f[i][e], k[i][e]) - m2) * fr[i];
+        h[i][e] = there[i] ? x : 0.f;
+        k[i][e] = there[i] ? y : 0.f;
       }
     }
-    const T* gate = a.gate ? static_cast<const T*>(a.gate) + t0 * a.C : nullptr;
-    if (gate && a.K > 1) stage_gates(gate, gates, toks * a.C, sh.threads);
-    __syncthreads();  // also: the tile before has read its products and sums
-    const auto gate_of = [&](int i, float (&s)[V]) {
-      gates_of<TAIL>(col && tok[i] < toks ? gate : nullptr, gates, a.K, tok[i], a.C, c, s);
-    };
-    const auto post_of = [&](int i, float (&p)[V]) {
-      load_or<TAIL>(a.post_weight && col ? a.post_weight + deg[i] * a.C + c : nullptr, left, 1.f, p);
-    };
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      float w[V], p[V], s[V];
-      gate_of(i, s);
-      post_of(i, p);
-      load_or<TAIL>(a.weight && col ? a.weight + deg[i] * a.C + c : nullptr, left, 1.f, w);
       float q = 0.f, sum = 0.f;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        h[i][e] = (h[i][e] - mu[i]) * ru[i];
-        k[i][e] = (fmaf(h[i][e], p[e] * (s[e] * sc[e]), k[i][e]) - mr[i]) * rr[i];
         gw[i][e] = fmaf(gy[i][e], k[i][e], gw[i][e]);
         if (comp[i] == 0) gb[e] += gy[i][e];
-        gy[i][e] *= w[e];
+        gy[i][e] *= w[i][e];
         q = fmaf(gy[i][e], k[i][e], q);
         sum += gy[i][e];
       }
       q = group_sum(q, sh.lanes);
       if (comp[i] == 0) {
-        sum = group_sum(sum, sh.lanes) / (float)a.C;
+        sum = group_sum(sum, sh.lanes) * share[i];
 #pragma unroll
         for (int e = 0; e < V; ++e) gy[i][e] -= sum;
       }
       if (j == 0 && tok[i] < toks) sums[i * per + rg] = q;
     }
-    const auto means = [&] {
-      __syncthreads();
-      degree_sums(sums, ds, toks, degs, a.K, sh.threads,
-                  [&](float s, int, int l) { return s / (float)((2 * l + 1) * a.C); });
-      __syncthreads();
+    // the mean over a row's degree, added by the row's lanes
+    const auto mean_of = [&](int i, const float* from) {
+      float s = 0.f;
+      if (tok[i] < toks)
+        for (int m = j; m < 2 * deg[i] + 1; m += sh.lanes) s += from[tok[i] * a.K + deg[i] * deg[i] + m];
+      return group_sum(s, sh.lanes) * share[i];
     };
-    means();
+    __syncthreads();
+    if (gates_wanted && tile != blockIdx.x) gate_out(tile - gridDim.x);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const bool there = col && tok[i] < toks;
-      const float d = there ? ds[tok[i] * degs + deg[i]] : 0.f;
-      float p[V], s[V], o[V];
+      const bool on = there[i];
+      const float d = mean_of(i, sums);
+      float s[V], o[V];
       gate_of(i, s);
-      post_of(i, p);
 #pragma unroll
-      for (int e = 0; e < V; ++e) G[i][e] = fmaf(rr[i], fmaf(-k[i][e], d, gy[i][e]), G[i][e]);
-      if (there && g.gx)
+      for (int e = 0; e < V; ++e) G[i][e] = fmaf(fr[i], fmaf(-k[i][e], d, gy[i][e]), G[i][e]);
+      if (on && g.gx)
         store_part<TAIL>(static_cast<T*>(g.gx) + base + (long long)(i * per + rg) * a.C + c, left, G[i]);
       float q = 0.f, sum = 0.f;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float gh = TAIL && e >= left ? 0.f : G[i][e] * h[i][e];
         gq[i][e] = fmaf(gh, s[e], gq[i][e]);
-        o[e] = gh * (sc[e] * p[e]);
-        k[i][e] = TAIL && e >= left ? 0.f : G[i][e] * (p[e] * (s[e] * sc[e]));  // p of the header
+        o[e] = gh * f[i][e];
+        k[i][e] = TAIL && e >= left ? 0.f : G[i][e] * (s[e] * f[i][e]);  // p of the header
         q = fmaf(k[i][e], h[i][e], q);
         sum += k[i][e];
       }
-      if (there && g.ggate) {
+      if (on && g.ggate) {
         if (a.K > 1) {
 #pragma unroll
           for (int e = 0; e < V; ++e)
@@ -306,36 +357,39 @@ __global__ __launch_bounds__(kResidualRowThreads) void residual_rows_bwd_kernel(
       }
       q = group_sum(q, sh.lanes);
       if (comp[i] == 0) {
-        sum = group_sum(sum, sh.lanes) / (float)a.C;
+        sum = group_sum(sum, sh.lanes) * share[i];
 #pragma unroll
         for (int e = 0; e < V; ++e) k[i][e] -= sum;
       }
-      if (j == 0 && tok[i] < toks) sums[i * per + rg] = q;
+      if (j == 0 && tok[i] < toks) sums[rowsum + i * per + rg] = q;
     }
-    means();
+    if (tile + gridDim.x < tiles) stage(tile + gridDim.x, half ^ 1);
+    __syncthreads();
     if (g.gu) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        if (!col || tok[i] >= toks) continue;
-        const float d = ds[tok[i] * degs + deg[i]];
+        const float d = mean_of(i, sums + rowsum);
+        if (!there[i]) continue;
         float o[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = ru[i] * fmaf(-h[i][e], d, k[i][e]);
+        for (int e = 0; e < V; ++e) o[e] = fu[i] * fmaf(-h[i][e], d, k[i][e]);
         store_part<TAIL>(static_cast<T*>(g.gu) + base + (long long)(i * per + rg) * a.C + c, left, o);
       }
     }
-    if (g.ggate && a.K > 1) {
-      for (int o = tid; o < toks * a.C; o += sh.threads) {
-        const int t = o / a.C, ch = o - t * a.C;
-        const float* p = prod + t * a.K * a.C + ch;
+    if (gates_wanted) {
+      for (int i = tid; i < count * gated; i += sh.threads) {
+        const int slice = i / gated, o = i - slice * gated, t = o / a.C;
         float s = 0.f;
-        for (int m = 0; m < a.K; ++m) s += p[m * a.C];
-        const long long at = (t0 + t) * a.C + ch;
-        static_cast<T*>(g.ggate)[at] = (T)(s * silu_slope(widen(static_cast<const T*>(a.gate)[at])));
+        for (int m = slice; m < a.K; m += count) s += prod[(t * a.K + m) * a.C + o - t * a.C];
+        slices[i] = s;
       }
     }
-    // The next tile writes gates, which nobody has read since the last barrier; everything
-    // else behind a barrier of its own.
+    // The next tile writes the first sums, which nobody has read since the last barrier, then
+    // everything else behind its own first.
+  }
+  if (gates_wanted && blockIdx.x < tiles) {
+    __syncthreads();
+    gate_out(blockIdx.x + (tiles - 1 - blockIdx.x) / gridDim.x * gridDim.x);
   }
   if (!g.part) return;
   float* part = g.part + (long long)blockIdx.x * (2 * degs + 1) * a.C;
@@ -445,9 +499,10 @@ __global__ __launch_bounds__(MAXT) void residual_wide_kernel(ResidualArgs a) {
   }
 }
 
-// Block `slot` takes tokens slot, slot + gridDim.x, ...; partial sums part[slot][gw, Q, gb][C].
+// Block `slot` takes tokens slot, slot + gridDim.x, ..., each asked for while the one before is
+// computed; partial sums part[slot][gw, Q, gb][C].
 template <class T, int V, int R, int MAXT, bool TAIL>
-__global__ __launch_bounds__(MAXT) void residual_wide_bwd_kernel(ResidualBwdArgs g) {
+__global__ __launch_bounds__(MAXT, MAXT == 1024 ? 4 : 2) void residual_wide_bwd_kernel(ResidualBwdArgs g) {
   __shared__ float lds[32];
   const ResidualArgs& a = g.a;
   const int tid = threadIdx.x, threads = blockDim.x, n = a.C;
@@ -456,22 +511,39 @@ __global__ __launch_bounds__(MAXT) void residual_wide_bwd_kernel(ResidualBwdArgs
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) gw[i][e] = gq[i][e] = gb[i][e] = 0.f;
-  for (long long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+  Raw<T, V> hr[R], kr[R], yr[R], Gr[R], zr[R];
+  float4 st;
+  const auto fetch = [&](long long t) {
     const long long base = t * n;
-    const float mu = a.stats[t * 4], ru = a.stats[t * 4 + 1], mr = a.stats[t * 4 + 2], rr = a.stats[t * 4 + 3];
-    float h[R][V], k[R][V], y[R][V], G[R][V], z[R][V];
+    st = reinterpret_cast<const float4*>(a.stats)[t];  // mean of u, ru, mean of r, rr
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int e0 = (i * threads + tid) * V;
+      if (e0 >= n) continue;
+      hr[i].template load_part<TAIL>(static_cast<const T*>(a.u) + base + e0, n - e0);
+      kr[i].template load_part<TAIL>(static_cast<const T*>(a.x) + base + e0, n - e0);
+      yr[i].template load_part<TAIL>(static_cast<const T*>(g.gy) + base + e0, n - e0);
+      if (g.gr) Gr[i].template load_part<TAIL>(static_cast<const T*>(g.gr) + base + e0, n - e0);
+      if (a.gate) zr[i].template load_part<TAIL>(static_cast<const T*>(a.gate) + base + e0, n - e0);
+    }
+  };
+  if (blockIdx.x < a.tokens) fetch(blockIdx.x);
+  for (long long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+    const long long base = t * n;
+    const float mu = st.x, ru = st.y, mr = st.z, rr = st.w;
+    float h[R][V], k[R][V], y[R][V], G[R][V], z[R][V];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
 #pragma unroll
       for (int e = 0; e < V; ++e) h[i][e] = k[i][e] = y[i][e] = G[i][e] = z[i][e] = 0.f;
-      if (e0 >= n) continue;
-      load_part<TAIL>(static_cast<const T*>(a.u) + base + e0, n - e0, h[i]);
-      load_part<TAIL>(static_cast<const T*>(a.x) + base + e0, n - e0, k[i]);
-      load_part<TAIL>(static_cast<const T*>(g.gy) + base + e0, n - e0, y[i]);
-      if (g.gr) load_part<TAIL>(static_cast<const T*>(g.gr) + base + e0, n - e0, G[i]);
-      if (a.gate) load_part<TAIL>(static_cast<const T*>(a.gate) + base + e0, n - e0, z[i]);
+      if ((i * threads + tid) * V >= n) continue;
+      hr[i].widen_to(h[i]);
+      kr[i].widen_to(k[i]);
+      yr[i].widen_to(y[i]);
+      if (g.gr) Gr[i].widen_to(G[i]);
+      if (a.gate) zr[i].widen_to(z[i]);
     }
+    if (t + gridDim.x < a.tokens) fetch(t + gridDim.x);
     float q = 0.f, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -742,7 +814,7 @@ __global__ __launch_bounds__(64 * kResidualSlices) void residual_sum_kernel(Resi
 constexpr int kFwdPasses = 4;
 constexpr int bwd_passes(int V) { return 16 / V; }
 constexpr int kRowValues = 8192;    // of one array in the backward's tiles: 32 KiB of products
-constexpr int kRowBlocks = 1024, kChannelBlocks = 512;
+constexpr int kRowBlocks = 768, kChannelBlocks = 512;  // of 256 threads: three a CU are resident
 
 enum class Kind { kRows, kWide, kChannels };
 struct Form {
@@ -768,12 +840,13 @@ Form residual_form(int type, int C, int L, bool backward) {
 }
 
 size_t rows_lds(const RowShape& sh, int K, int L, int C, bool gate) {
-  return ((size_t)sh.tokens * (2 * K + 2 * (L + 1)) + (gate && K > 1 ? (size_t)sh.tokens * C : 0)) * sizeof(float);
+  return ((size_t)sh.tokens * 2 * (K + L + 1) + (gate && K > 1 ? (size_t)sh.tokens * C : 0)) * sizeof(float);
 }
 size_t rows_bwd_lds(const RowShape& sh, int K, int L, int C) {
   const size_t rows = (size_t)(sh.threads / sh.lanes) * sh.passes;
-  const size_t shared = K > 1 ? sh.tokens * (size_t)(K + 1) * C : 0;
-  return std::max(sh.tokens * (size_t)(K + L + 1) + shared, rows * C) * sizeof(float);
+  const int slices = std::max(1, std::min(8, sh.threads / (sh.tokens * C)));
+  const size_t shared = K > 1 ? sh.tokens * (size_t)(K + 2 + slices) * C : 0;
+  return std::max(sh.tokens * (size_t)(2 * (K + stats_of(L))) + shared, rows * C) * sizeof(float);
 }
 int residual_blocks(const Form& f, long long tokens) {
   if (f.kind == Kind::kRows) {
@@ -811,11 +884,15 @@ hipError_t wide_backward(const WideShape& w, F f) {
 template <class T, int V, bool TAIL>
 hipError_t residual_any(const ResidualArgs& a, const Form& f, hipStream_t s) {
   if (f.kind == Kind::kRows) {
-    const long long blocks = (a.tokens + f.row.tokens - 1) / f.row.tokens;
-    const size_t lds = rows_lds(f.row, a.K, a.L, a.C, a.gate != nullptr);
-    if (!launch_fits(blocks, f.row.threads) || lds > 160 * 1024) return hipErrorInvalidConfiguration;
+    // few tokens: a CU each, rather than blocks filled to the last lane (64 tokens of L=2 C=4:
+    // 12 us in two blocks, five in 64)
+    RowShape row = f.row;
+    row.tokens = (int)std::min<long long>(row.tokens, (a.tokens + 255) / 256);
+    const long long blocks = (a.tokens + row.tokens - 1) / row.tokens;
+    const size_t lds = rows_lds(row, a.K, a.L, a.C, a.gate != nullptr);
+    if (!launch_fits(blocks, row.threads) || lds > 160 * 1024) return hipErrorInvalidConfiguration;
     const auto run = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(f.row.threads), lds, s, a, f.row);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(row.threads), lds, s, a, row);
       return hipGetLastError();
     };
     return f.row.passes == 2 ? run(residual_rows_kernel<T, V, 2, TAIL>) : run(residual_rows_kernel<T, V, 4, TAIL>);
@@ -840,8 +917,12 @@ hipError_t residual_any(const ResidualBwdArgs& g, const Form& f, hipStream_t s) 
       hipLaunchKernelGGL(kernel, dim3(blocks), dim3(f.row.threads), lds, s, g, f.row, tiles);
       return hipGetLastError();
     };
-    if (f.row.passes == 2) return run(residual_rows_bwd_kernel<T, V, 2, TAIL>);
-    return run(residual_rows_bwd_kernel<T, V, bwd_passes(V), TAIL>);
+    constexpr int R = bwd_passes(V);  // as many in every block of more than 256 threads
+    if constexpr (R > 2) {
+      if (f.row.passes == 2) return run(residual_rows_bwd_kernel<T, V, 2, 256, TAIL>);
+    }
+    return f.row.threads <= 256 ? run(residual_rows_bwd_kernel<T, V, R, 256, TAIL>)
+                                : run(residual_rows_bwd_kernel<T, V, R, 512, TAIL>);
   }
   return wide_backward<T>(f.wide, [&](auto shape) {
     constexpr int R = decltype(shape)::kVecs, MAXT = decltype(shape)::kThreads;

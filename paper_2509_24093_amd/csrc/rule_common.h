@@ -232,13 +232,6 @@ __device__ __forceinline__ T& place(T* base, uint32_t bytes) {
   typedef typename std::conditional<std::is_const<T>::value, const char, char>::type Byte;
   return *reinterpret_cast<T*>(reinterpret_cast<Byte*>(base) + bytes);
 }
-// x as a number the compiler knows nothing of: what is computed from it stays where it is,
-// instead of waiting in registers for every turn of a loop.
-__device__ __forceinline__ int afresh(int x) {
-  asm volatile("" : "+s"(x));
-  return x;
-}
-
 // A chunk's key or query rows, tokens >= 1 of them.
 template <class T, int KB, int THREADS>
 struct RowStage {

@@ -125,6 +125,13 @@ __device__ __forceinline__ void store_part(T* p, int n, const float (&v)[V]) {
     if (i < n) p[i] = (T)v[i];
 }
 
+// x as a number the compiler knows nothing of: what is computed from it stays where it is,
+// instead of waiting in registers for every turn of a loop.
+__device__ __forceinline__ int afresh(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));

@@ -298,18 +298,23 @@ def checkpoint_unpack(codes, scales, dtype=None, out=None):
 
 
 def _list_of(name, tensors, device):
-    """Type codes, sizes and addresses of a list of contiguous GPU tensors."""
+    """Type codes, sizes and addresses of a list of contiguous GPU tensors.  A
+    list of few tensors spends its call's time here: cheap queries, and the
+    explanation only for a list that is refused."""
     import torch
-    codes, counts, addresses = [], [], []
+    _dtype_code(name, torch.float32)
+    try:
+        if all([t.is_contiguous() and t.get_device() == device for t in tensors]):
+            return ([_codes[t.dtype] for t in tensors], [t.numel() for t in tensors], [t.data_ptr() for t in tensors])
+    except (AttributeError, KeyError):
+        pass
     for i, t in enumerate(tensors):
         if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
             raise ValueError(f"{name}[{i}] must be a contiguous GPU tensor")
         if t.get_device() != device:
             raise ValueError(f"{name}[{i}] is on GPU {t.get_device()}, which is not current")
-        codes.append(_dtype_code(f"{name}[{i}]", t.dtype))
-        counts.append(t.numel())
-        addresses.append(t.data_ptr())
-    return codes, counts, addresses
+        _dtype_code(f"{name}[{i}]", t.dtype)
+    raise ValueError(f"{name} must be tensors")
 
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None):
