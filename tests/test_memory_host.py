@@ -186,7 +186,7 @@ size = lib.cgconv_clip_workspace(3, counts)
 assert lib.cgconv_clip(3, (ctypes.c_int32 * 3)(0, 1, 0), counts, (ctypes.c_void_p * 3)(big(0), big(1), big(2)),
                        (ctypes.c_void_p * 3)(big(3), big(4), big(5)), 1.0, 0.0, ptr(0), ptr(1), size, None) == 0
 for grid, block, lds, allowed in launches():
-    assert grid[0] <= 2048 + 3
+    assert grid[0] <= 16384 + 3
 """)
 
 
