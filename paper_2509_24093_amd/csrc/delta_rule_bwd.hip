@@ -227,35 +227,31 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
 
 // ---- gradients of keys, queries, decays and betas -------------------------------------------
 
-// Eight fp32 values of a row as an operand.
-__device__ __forceinline__ void wide_frag(const float* p, Frag (&f)[3]) {
-  float x[8];
-  load_vec(p, x);
-  split8(x, f);
-}
-
-// Eight columns from col on of a chunk's token (row: its first token), zeros where there is
-// no column or no token.  Where eight columns of a head are neighbours in memory (P a
-// multiple of eight) they are one load; what is not there is read from a place that is.
+// Eight columns from col on of a chunk's token (row: its first token), a slice ahead of their
+// use; zeros where there is no column or no token.  Where eight columns of a head are neighbours
+// in memory (P a multiple of eight) they are one load; what is not there is read from a place
+// that is.
 template <class T>
-__device__ __forceinline__ void columns8(const T* row, int t, int tokens, int stride, int col, int V, int P, int C,
-                                         int h, float (&x)[8]) {
-  const T* from = row + (long long)min(t, tokens - 1) * stride;
-  if (P % 8 == 0) {
-    const Column c(col, V, P, C, h);
-    load_vec(from + c.at, x);
-    const bool there = c.there && t < tokens;
+struct SliceStage {
+  Raw<T, 8> raw;
+  __device__ __forceinline__ void load(const T* row, int t, int tokens, int stride, int col, int V, int P, int C,
+                                       int h) {
+    const T* from = row + (long long)min(t, tokens - 1) * stride;
+    if (P % 8 == 0) {
+      raw.load(from + Column(col, V, P, C, h).at);
+    } else {
+      T x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = there ? x[e] : 0.f;
-    return;
+      for (int e = 0; e < 8; ++e) x[e] = from[Column(col + e, V, P, C, h).at];
+      __builtin_memcpy(raw.w, x, sizeof x);
+    }
   }
+  __device__ __forceinline__ void get(bool there, int col, int V, float (&x)[8]) const {
+    raw.widen_to(x);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const Column c(col + e, V, P, C, h);
-    const float y = widen(from[c.at]);
-    x[e] = c.there && t < tokens ? y : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = there && col + e < V ? x[e] : 0.f;
   }
-}
+};
 
 constexpr int kMStride = kT + 8;  // as row_stride
 typedef bf16 Square[3][kT * kMStride];  // a 64 x 64 matrix in three parts
@@ -275,17 +271,45 @@ __device__ __forceinline__ void put_tile(Square& s, int i, int j, int m, int q, 
   }
 }
 
-// Block (chunk, sequence and key head), the heads that share the key one after the other.
-// Wave w owns the tiles w, w + 4 of 16 key components (rows of S and gS) for all tokens, and
-// of the 64 x 64 matrices the tiles of row w.
+// 32 columns of a chunk's V', gY and gO, in parts.
+template <class T>
+struct Slice {
+  static constexpr int ST = row_stride(1);
+  alignas(16) bf16 value[3][kT * ST], gvalue[3][kT * ST], gy[kParts<T>][kT * ST];
+};
+
+// What a block of rule_grads_kernel shares.  The slices make room for the matrices M1 and beta
+// M2; two of each where they fit, so that the waves meet once a slice, or once for both.
 template <class T, int KB>
-__global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs ws) {
-  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, NT = (DT + 3) / 4;
-  __shared__ __attribute__((aligned(16))) bf16 kbuf[NP][kT * ST];
-  __shared__ __attribute__((aligned(16))) bf16 qbuf[NP][kT * ST];
-  __shared__ __attribute__((aligned(16))) Square mat;
-  __shared__ float4 ta[kT], tb[kT];
-  __shared__ float dots[3][4][kT], behind[4][kT], direct[kT], dleft[kT], whole_dot[4];
+struct GradsSpace {
+  static constexpr int NP = kParts<T>, ST = row_stride(KB);
+  alignas(16) bf16 k[NP][kT * ST];
+  alignas(16) bf16 q[NP][kT * ST];
+  float4 ta[kT], tb[kT];
+  float dots[3][8][kT], behind[8][kT], direct[kT], dleft[kT], whole_dot[8];
+  static constexpr int kLeft = 160 * 1024 - 4 * NP * kT * ST - 32 * kT - 4 * kT * 34 - 64;
+  static constexpr int kSlices = 2 * (int)sizeof(Slice<T>) <= kLeft ? 2 : 1;
+  static constexpr int kSquares = 2 * (int)sizeof(Square) <= kLeft ? 2 : 1;
+  union {
+    Slice<T> slice[kSlices];
+    Square mat[kSquares];
+  };
+};
+
+// Block (chunk, sequence and key head) of eight waves, the heads that share the key one after
+// the other.  Wave w owns the tile of the 16 key components from 16 w on (rows of S and gS) for
+// all tokens; of the 64 x 64 matrices wave w < 4 has the row of tiles w of M1, wave w + 4 that
+// of M2.
+template <class T, int KB>
+__global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs ws) {
+  typedef GradsSpace<T, KB> Space;
+  constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, SS = Slice<T>::ST;
+  __shared__ Space space;
+  auto& kbuf = space.k;
+  auto& qbuf = space.q;
+  auto& ta = space.ta;
+  auto& tb = space.tb;
+  auto& dots = space.dots;
   const RuleArgs& a = g.a;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
   const int chunk = blockIdx.x, b = blockIdx.y / a.n.Hk, hk = blockIdx.y - b * a.n.Hk;
@@ -298,12 +322,12 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
   T* gk = g.gk ? static_cast<T*>(g.gk) + key0 : nullptr;
   const auto gate_at = [&](int t, int h) { return ((long long)b * N + t0 + t) * a.n.H + h; };
   if (tokens == 0) {
-    for (int i = tid; i < here * D; i += 256) {
+    for (int i = tid; i < here * D; i += 512) {
       const int at = (i / D) * stride + i % D;
       if (gq) gq[at] = (T)0.f;
       if (gk) gk[at] = (T)0.f;
     }
-    for (int i = tid; i < here * each; i += 256) {
+    for (int i = tid; i < here * each; i += 512) {
       const long long at = gate_at(i / each, hk * each + i % each);
       if (g.gdecay) g.gdecay[at] = 0.f;
       if (g.gbeta) g.gbeta[at] = 0.f;
@@ -311,13 +335,12 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     return;
   }
   {
-    RowStage<T, KB, 256> s;
-    s.load(static_cast<const T*>(a.k) + key0, stride, tokens, D, tid);
-    s.store(kbuf, tokens, D, tid);
-    s.load(static_cast<const T*>(a.q) + key0, stride, tokens, D, tid);
-    s.store(qbuf, tokens, D, tid);
+    RowStage<T, KB, 512> k, q;
+    k.load(static_cast<const T*>(a.k) + key0, stride, tokens, D, tid);
+    q.load(static_cast<const T*>(a.q) + key0, stride, tokens, D, tid);
+    k.store(kbuf, tokens, D, tid);
+    q.store(qbuf, tokens, D, tid);
   }
-  for (int i = tid; i < 3 * kT * kMStride / 2; i += 256) reinterpret_cast<uint32_t*>(&mat)[i] = 0;  // above the diagonal
   // an element of the keys or queries as stored
   const auto element = [&](const bf16 (&buf)[NP][kT * ST], int t, int d) {
     float x = 0.f;
@@ -325,109 +348,112 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     for (int p = NP - 1; p >= 0; --p) x += (float)buf[p][t * ST + d];
     return x;
   };
-  v4f totq[kTiles][NT], totk[kTiles][NT];
+  const bool owner = wave < DT, second = wave >= 4;  // has key components; has a row of M2
+  const int row = wave & 3, own = 16 * wave + m;
+  const int st = (tid & 255) >> 2, sc = (tid & 3) * 8;  // token and columns of a slice that a thread brings
+  v4f totq[kTiles], totk[kTiles];
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-    for (int n = 0; n < NT; ++n) totq[i][n] = totk[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < kTiles; ++i) totq[i] = totk[i] = v4f{0.f, 0.f, 0.f, 0.f};
 
   for (int e = 0; e < each; ++e) {
     const int h = hk * each + e, unit = b * a.n.H + h;
     const long long at = (long long)unit * ws.chunks + chunk;
-    const float* S = ws.state + at * (32 * KB) * ws.VP;
-    const float* gS = ws.gstate + at * (32 * KB) * ws.VP;
-    const float* val = ws.value + at * kT * ws.VP;
-    const float* gval = ws.gvalue + at * kT * ws.VP;
-    const T* gy = static_cast<const T*>(g.gy) + ((long long)b * N + t0) * KC;
-    const T* v = static_cast<const T*>(a.v) + ((long long)b * N + t0) * KC;
+    const long long state0 = (at * (32 * KB) + (owner ? own : 0)) * ws.VP + 4 * q;
+    const float* wide = (second ? ws.value : ws.gvalue) + (at * kT + st) * ws.VP + sc;
+    const T* rows = static_cast<const T*>(second ? g.gy : a.v) + ((long long)b * N + t0) * KC;
     const float whole = ws.whole[at];
     __syncthreads();  // the head before has been read
     if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = ws.token[at * 2 * kT + tid];
 
-    // S gO, S gY, gS V' over the columns, and <S, gS>
-    v4f aq[kTiles][NT], al[kTiles][NT], ar[kTiles][NT];
-    float both = 0.f;
+    // S gO, S gY, gS V' over the columns, <S, gS>, gO V'^T or gY V'^T of the own row of tiles, and gY.v
+    v4f aq[kTiles], al[kTiles], ar[kTiles], w[kTiles];
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
+    for (int i = 0; i < kTiles; ++i) aq[i] = al[i] = ar[i] = w[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    float both = 0.f, yv = 0.f, wx[8], sx[8], gx[8];
+    SliceStage<T> narrow;
+    const auto fetch = [&](int v0) {
+      load_vec(wide + v0, wx);
+      narrow.load(rows, st, tokens, KC, v0 + sc, ws.V, P, C, h);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) aq[i][n] = al[i][n] = ar[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
-    if (wave < DT) {
-      for (int v0 = 8 * q; v0 < ws.VP; v0 += 32) {
-        Frag fs[NT][3], fg[NT][3];
+      for (int half = 0; half < 2; ++half) {
+        const v4f x = *reinterpret_cast<const v4f*>(ws.state + state0 + v0 + 16 * half);
+        const v4f y = *reinterpret_cast<const v4f*>(ws.gstate + state0 + v0 + 16 * half);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if (wave + 4 * n >= DT) continue;
-          float x[8], y[8];
-          const long long row = (long long)(16 * (wave + 4 * n) + m) * ws.VP + v0;
-          load_vec(S + row, x);
-          load_vec(gS + row, y);
-#pragma unroll
-          for (int c = 0; c < 8; ++c) both = fmaf(x[c], y[c], both);
-          split8(x, fs[n]);
-          split8(y, fg[n]);
-        }
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          const int t = 16 * i + m;
-          float x[8];
-          Frag fo[NP], fy[3], fv[3];
-          columns8(gy, t, tokens, KC, v0, ws.V, P, C, h, x);
-          parts8<T>(x, fo);
-          wide_frag(gval + (long long)t * ws.VP + v0, fy);
-          wide_frag(val + (long long)t * ws.VP + v0, fv);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            if (wave + 4 * n >= DT) continue;
-            aq[i][n] = mma(fo, fs[n], aq[i][n]);
-            al[i][n] = mma(fy, fs[n], al[i][n]);
-            ar[i][n] = mma(fv, fg[n], ar[i][n]);
-          }
+        for (int r = 0; r < 4; ++r) {
+          sx[4 * half + r] = x[r];
+          gx[4 * half + r] = y[r];
         }
       }
-    }
-    // gO V'^T and gY V'^T of the own row of tiles, and gY.v of its tokens
-    v4f mo[kTiles], my[kTiles];
-    float yv = 0.f;
+    };
+    fetch(0);
+    for (int v0 = 0, n = 0; v0 < ws.VP; v0 += 32, ++n) {
+      auto& slice = space.slice[n & (Space::kSlices - 1)];
+      if (Space::kSlices == 1 && n) __syncthreads();  // the one before has been read
+      {
+        float x[8];
+        Frag f[3];
+        narrow.get(st < tokens, v0 + sc, ws.V, x);
+        split8(wx, f);
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) mo[j] = my[j] = v4f{0.f, 0.f, 0.f, 0.f};
-    for (int v0 = 8 * q; v0 < ws.VP; v0 += 32) {
-      const int t = 16 * wave + m;
-      float x[8], y[8];
-      Frag fo[NP], fy[3];
-      load_vec(gval + (long long)t * ws.VP + v0, y);
-      split8(y, fy);
-      columns8(v, t, tokens, KC, v0, ws.V, P, C, h, x);
+        for (int p = 0; p < 3; ++p)
+          *reinterpret_cast<Frag*>((second ? slice.value : slice.gvalue)[p] + st * SS + sc) = f[p];
+        if (second) {
+          Frag o[NP];
+          parts8<T>(x, o);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) yv = fmaf(x[c], y[c], yv);
-      columns8(gy, t, tokens, KC, v0, ws.V, P, C, h, x);
-      parts8<T>(x, fo);
+          for (int p = 0; p < NP; ++p) *reinterpret_cast<Frag*>(slice.gy[p] + st * SS + sc) = o[p];
+        } else {
 #pragma unroll
-      for (int j = 0; j < kTiles; ++j) {
-        if (j > wave) continue;
-        Frag fv[3];
-        wide_frag(val + (long long)(16 * j + m) * ws.VP + v0, fv);
-        mo[j] = mma(fo, fv, mo[j]);
-        my[j] = mma(fy, fv, my[j]);
+          for (int c = 0; c < 8; ++c) yv = fmaf(x[c], wx[c], yv);
+        }
+      }
+      Frag fs[3], fg[3];
+      if (owner) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) both = fmaf(sx[c], gx[c], both);
+      }
+      split8(sx, fs);
+      split8(gx, fg);
+      if (v0 + 32 < ws.VP) fetch(v0 + 32);
+      __syncthreads();  // the slice is there
+      Frag fv[kTiles][3];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) rows_frag<3, SS>(slice.value, i, 0, m, q, fv[i]);
+      if (owner) mma_all(fv, fg, ar);
+      if (second) {
+        Frag f[3];
+        rows_frag<3, SS>(slice.gvalue, row, 0, m, q, f);
+        mma_each(f, fv, w);
+      } else {
+        Frag f[NP];
+        rows_frag<NP, SS>(slice.gy, row, 0, m, q, f);
+        mma_each(f, fv, w);
+      }
+      if (owner) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) rows_frag<3, SS>(slice.gvalue, i, 0, m, q, fv[i]);
+        mma_all(fv, fs, al);
+        Frag fo[kTiles][NP];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) rows_frag<NP, SS>(slice.gy, i, 0, m, q, fo[i]);
+        mma_all(fo, fs, aq);
       }
     }
-    yv += __shfl_xor(yv, 16);
-    yv += __shfl_xor(yv, 32);
-    if (q == 0) direct[16 * wave + m] = yv;
-    __syncthreads();  // the tokens' numbers are there, and the matrix has been read
+    yv = group_sum(yv, 4);
+    if (!second && (lane & 3) == 0) space.direct[st] = yv;
+    // M1 or M2 (the tiles past the diagonal are not used)
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) {
-      if (j > wave) continue;
+      if (j > row) continue;
       const int u = 16 * j + m;
       const float4 other = tb[u];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int t = 16 * wave + 4 * q + r;
+        const int t = 16 * row + 4 * q + r;
         const float4 me = tb[t];
-        const float f = other.x * decay_between(me, other);
-        mo[j][r] = t >= u ? mo[j][r] * f * (a.scale * me.y) : 0.f;
-        my[j][r] = t > u ? -my[j][r] * f * me.x : 0.f;
+        const float f = other.x * decay_between(me, other) * (second ? -me.x : a.scale * me.y);
+        w[j][r] = t > u || (t == u && !second) ? w[j][r] * f : 0.f;
       }
-      put_tile(mat, wave, j, m, q, mo[j]);
     }
     // what the state gives, before the tokens' share: its part of q.Uq, k.UL, k.UR
 #pragma unroll
@@ -437,17 +463,14 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
         const int t = 16 * i + 4 * q + r;
         const float4 tok = ta[t];
         float x = 0.f, y = 0.f, z = 0.f;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          aq[i][n][r] *= tok.w;
-          al[i][n][r] *= -tok.y;
-          ar[i][n][r] *= tok.z;
-          if (wave + 4 * n >= DT) continue;
-          const int d = 16 * (wave + 4 * n) + m;
-          const float ke = element(kbuf, t, d);
-          x = fmaf(element(qbuf, t, d), aq[i][n][r], x);
-          y = fmaf(ke, al[i][n][r], y);
-          z = fmaf(ke, ar[i][n][r], z);
+        if (owner) {
+          const float ke = element(kbuf, t, own), qo = tok.w * aq[i][r], ko = -tok.y * al[i][r];
+          const float kr = tok.z * ar[i][r];
+          x = element(qbuf, t, own) * qo;
+          y = ke * ko;
+          z = ke * kr;
+          totq[i][r] += qo;
+          totk[i][r] += fmaf(tok.x, ko, kr);
         }
         x = group_sum(x, 16);
         y = group_sum(y, 16);
@@ -459,30 +482,30 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
         }
       }
     both = group_sum(both, 64);
-    if (lane == 0) whole_dot[wave] = both;
-    // the tokens' share, of the own row of tiles: sums over j up to a column, then over i behind it
+    if (lane == 0) space.whole_dot[wave] = both;
+    // the tokens' share, of the own row of tiles: sums over j up to a column, then over i behind
+    // it; that of M2 times beta, as M2 is used from here on
     {
       v4f left{0.f, 0.f, 0.f, 0.f}, before{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < kTiles; ++j) {
         float column = 0.f;
-        if (j <= wave) {
-          v4f qk{0.f, 0.f, 0.f, 0.f}, kk{0.f, 0.f, 0.f, 0.f};
+        if (j <= row) {
+          v4f p{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) {
             Frag f[NP], fj[NP];
             rows_frag<NP, ST>(kbuf, j, kb, m, q, fj);
-            rows_frag<NP, ST>(qbuf, wave, kb, m, q, f);
-            qk = mma(f, fj, qk);
-            rows_frag<NP, ST>(kbuf, wave, kb, m, q, f);
-            kk = mma(f, fj, kk);
+            rows_frag<NP, ST>(second ? kbuf : qbuf, row, kb, m, q, f);
+            p = mma(f, fj, p);
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int t = 16 * wave + 4 * q + r;
-            const float l = my[j][r] * kk[r];
-            left[r] += l;
-            float x = t > 16 * j + m ? fmaf(mo[j][r], qk[r], ta[t].x * l) : 0.f;
+            const int t = 16 * row + 4 * q + r;
+            const float beta = second ? ta[t].x : 1.f;
+            left[r] = fmaf(w[j][r], p[r], left[r]);
+            w[j][r] *= beta;
+            float x = t > 16 * j + m ? w[j][r] * p[r] : 0.f;
             x += dpp<0x111>(x);  // from the lanes 1, 2, 4, 8 below, zero from outside the 16
             x += dpp<0x112>(x);
             x += dpp<0x114>(x);
@@ -494,93 +517,57 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
         }
         column += __shfl_xor(column, 16);
         column += __shfl_xor(column, 32);
-        if (q == 0) behind[wave][16 * j + m] = column;
+        if (q == 0) space.behind[wave][16 * j + m] = column;
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float x = group_sum(left[r], 16);
-        if (m == 0) dleft[16 * wave + 4 * q + r] = x;
+        if (second && m == 0) space.dleft[16 * row + 4 * q + r] = x;
       }
     }
-    __syncthreads();  // M1 is there
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (wave + 4 * n >= DT) continue;
+    for (int j = 0; j < kTiles; ++j)
+      if (j > row) w[j] = v4f{0.f, 0.f, 0.f, 0.f};
+    // Uq += M1 k, U += M1^T q + beta M2 k + (beta M2)^T k; of the tiles past the diagonal only the
+    // neighbour of an even row's own is read
+    const auto put = [&](Square& mat) {
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j)
+        if (j <= row || (j == row + 1 && row % 2 == 0)) put_tile(mat, row, j, m, q, w[j]);
+    };
+    const auto add = [&](const Square& mat, v4f (&down)[kTiles], const bf16 (&other)[NP][kT * ST]) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        Frag fk[NP], fq[NP], f[3];
-        columns_frag<NP, ST>(kbuf, wave + 4 * n, kb, m, q, fk);
-        columns_frag<NP, ST>(qbuf, wave + 4 * n, kb, m, q, fq);
+        Frag fk[NP], fo[NP], f[3];
+        columns_frag<NP, ST>(kbuf, wave, kb, m, q, fk);
+        columns_frag<NP, ST>(other, wave, kb, m, q, fo);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           if (triangle_has<false>(i, kb)) {
             rows_frag<3, kMStride>(mat, i, kb, m, q, f);
-            aq[i][n] = mma(f, fk, aq[i][n]);
+            down[i] = mma(f, fk, down[i]);
           }
           if (triangle_has<true>(i, kb)) {
             columns_frag<3, kMStride>(mat, i, kb, m, q, f);
-            ar[i][n] = mma(f, fq, ar[i][n]);
+            totk[i] = mma(f, fo, totk[i]);
           }
         }
       }
+    };
+    __syncthreads();  // the slices have been read
+    if (!second || Space::kSquares == 2) put(space.mat[second ? Space::kSquares - 1 : 0]);
+    __syncthreads();  // M1 is there
+    if (owner) add(space.mat[0], totq, qbuf);
+    if (Space::kSquares == 1) {
+      __syncthreads();
+      if (second) put(space.mat[0]);
+      __syncthreads();
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kTiles; ++j)
-      if (j <= wave) put_tile(mat, wave, j, m, q, my[j]);
-    __syncthreads();  // M2 is there
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (wave + 4 * n >= DT) continue;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        Frag fk[NP], f[3];
-        columns_frag<NP, ST>(kbuf, wave + 4 * n, kb, m, q, fk);
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-          if (triangle_has<false>(i, kb)) {
-            rows_frag<3, kMStride>(mat, i, kb, m, q, f);
-            al[i][n] = mma(f, fk, al[i][n]);
-          }
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kTiles; ++j)
-      if (j <= wave) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) my[j][r] *= ta[16 * wave + 4 * q + r].x;
-        put_tile(mat, wave, j, m, q, my[j]);
-      }
-    __syncthreads();  // beta M2 is there
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (wave + 4 * n >= DT) continue;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        Frag fk[NP], f[3];
-        columns_frag<NP, ST>(kbuf, wave + 4 * n, kb, m, q, fk);
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-          if (triangle_has<true>(i, kb)) {
-            columns_frag<3, kMStride>(mat, i, kb, m, q, f);
-            ar[i][n] = mma(f, fk, ar[i][n]);
-          }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float beta = ta[16 * i + 4 * q + r].x;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          totq[i][n][r] += aq[i][n][r];
-          totk[i][n][r] += fmaf(beta, al[i][n][r], ar[i][n][r]);
-        }
-      }
+    if (owner) add(space.mat[Space::kSquares - 1], totk, kbuf);
     if (wave == 0) {
-      const auto over = [&](const float (&x)[4][kT], int t) { return (x[0][t] + x[1][t]) + (x[2][t] + x[3][t]); };
+      const auto over = [&](const float (&x)[8][kT], int t) {
+        return ((x[0][t] + x[1][t]) + (x[2][t] + x[3][t])) + ((x[4][t] + x[5][t]) + (x[6][t] + x[7][t]));
+      };
       const float left = over(dots[1], lane);
       float from = fmaf(ta[lane].x, left, over(dots[0], lane));  // summed from the token on
       float until = over(dots[2], lane);                         // summed up to the token
@@ -591,60 +578,59 @@ __global__ __launch_bounds__(256) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
         if (lane >= o) until += y;
       }
       until = __shfl_up(until, 1);
-      const float s = whole * ((whole_dot[0] + whole_dot[1]) + (whole_dot[2] + whole_dot[3])) + from +
-                      (lane ? until + over(behind, lane - 1) : 0.f);
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss += space.whole_dot[i];
+      const float s = whole * ss + from + (lane ? until + over(space.behind, lane - 1) : 0.f);
       if (lane < here) {
         const long long to = gate_at(lane, h);
         if (g.gdecay) g.gdecay[to] = lane < tokens ? s : 0.f;
-        if (g.gbeta) g.gbeta[to] = lane < tokens ? left + dleft[lane] + direct[lane] : 0.f;
+        if (g.gbeta) g.gbeta[to] = lane < tokens ? left + space.dleft[lane] + space.direct[lane] : 0.f;
       }
     }
   }
   // through the norms of key and query, and out
   if (a.normalize) {
+    __syncthreads();  // the last head's dots have been read
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int t = 16 * i + 4 * q + r;
         float x = 0.f, y = 0.f;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if (wave + 4 * n >= DT) continue;
-          const int d = 16 * (wave + 4 * n) + m;
-          x = fmaf(element(qbuf, t, d), totq[i][n][r], x);
-          y = fmaf(element(kbuf, t, d), totk[i][n][r], y);
+        if (owner) {
+          x = element(qbuf, t, own) * totq[i][r];
+          y = element(kbuf, t, own) * totk[i][r];
         }
         x = group_sum(x, 16);
         y = group_sum(y, 16);
-        if (i == 0 && r == 0) __syncthreads();  // the last head's dots have been read
         if (m == 0) {
           dots[0][wave][t] = x;
           dots[1][wave][t] = y;
         }
       }
     __syncthreads();
+    if (tid < 2 * kT) {
+      const int t = tid >> 1, k = tid & 1;
+      float x = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x += dots[k][i][t];
+      const float f = k ? tb[t].x : tb[t].y;
+      (k ? space.dleft : space.direct)[t] = f * f * x;
+    }
+    __syncthreads();
   }
+  if (!owner || own >= D) return;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int t = 16 * i + 4 * q + r;
-      float x = 0.f, y = 0.f;
-      if (a.normalize) {
-        const float4 f = tb[t];
-        x = f.y * f.y * ((dots[0][0][t] + dots[0][1][t]) + (dots[0][2][t] + dots[0][3][t]));
-        y = f.x * f.x * ((dots[1][0][t] + dots[1][1][t]) + (dots[1][2][t] + dots[1][3][t]));
-      }
       if (t >= here) continue;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int d = 16 * (wave + 4 * n) + m;
-        if (d >= D) continue;
-        const bool there = t < tokens;
-        if (gq) gq[t * stride + d] = there ? (T)fmaf(-x, element(qbuf, t, d), totq[i][n][r]) : (T)0.f;
-        if (gk) gk[t * stride + d] = there ? (T)fmaf(-y, element(kbuf, t, d), totk[i][n][r]) : (T)0.f;
-      }
+      const float x = a.normalize ? space.direct[t] : 0.f, y = a.normalize ? space.dleft[t] : 0.f;
+      const bool there = t < tokens;
+      if (gq) gq[t * stride + own] = there ? (T)fmaf(-x, element(qbuf, t, own), totq[i][r]) : (T)0.f;
+      if (gk) gk[t * stride + own] = there ? (T)fmaf(-y, element(kbuf, t, own), totk[i][r]) : (T)0.f;
     }
 }
 
@@ -663,7 +649,7 @@ hipError_t backward(const RuleBwdArgs& g, const RuleWs& w, hipStream_t s) {
   }
   e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, false>, 4) : walk(rule_reverse_kernel<T, KB, 8, false>, 8);
   if (e != hipSuccess || !(g.gq || g.gk || g.gdecay || g.gbeta)) return e;
-  hipLaunchKernelGGL((rule_grads_kernel<T, KB>), dim3(w.chunks, g.a.n.B * g.a.n.Hk), dim3(256), 0, s, g, w);
+  hipLaunchKernelGGL((rule_grads_kernel<T, KB>), dim3(w.chunks, g.a.n.B * g.a.n.Hk), dim3(512), 0, s, g, w);
   return hipGetLastError();
 }
 

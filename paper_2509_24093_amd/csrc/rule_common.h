@@ -106,14 +106,19 @@ __device__ __forceinline__ void mma_all(const Frag (&a)[NI][NA], const Frag (&b)
           acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i][p].f, b[s - p].f, acc[i], 0, 0, 0);
       }
 }
-// Eight elements of a row from p on, n of them there (any n), zeros behind.
-template <class T>
-__device__ __forceinline__ void row8(const T* p, int n, float (&x)[8]) {
-  Raw<T, 8> raw;
-  raw.template load_part<true>(p, n);
-  raw.widen_to(x);
+// acc[j] += A B[j], in the same order.
+template <int NJ, int NA, int NB>
+__device__ __forceinline__ void mma_each(const Frag (&a)[NA], const Frag (&b)[NJ][NB], v4f (&acc)[NJ]) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int p = 0; p < NA; ++p)
+      if (s - p >= 0 && s - p < NB) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[p].f, b[j][s - p].f, acc[j], 0, 0, 0);
+      }
 }
-
 // Rows of 64 tokens in LDS, one array a part.  Row stride in elements: an odd multiple of
 // four words, so that 16 rows' words at one column lie in 16 different groups of four banks.
 constexpr int row_stride(int KB) { return 32 * KB + 8; }
