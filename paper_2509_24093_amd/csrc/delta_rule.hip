@@ -55,7 +55,8 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
   auto& qbuf = reinterpret_cast<bf16(*)[NP][kT * ST]>(space)[1];
   float* tri = reinterpret_cast<float*>(space);
   float* inv = tri + kT * kRow;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int m = lane & 15, q = lane >> 4;
   const int chunk = blockIdx.x, unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H;
   const int t0 = chunk * kT, tokens = min(tokens_of(a, b) - t0, kT);
   if (tokens <= 0) return;
@@ -248,7 +249,8 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
   typedef Stage<T, KB, kOut, kOut> Buffer;
   constexpr int ST = Buffer::ST;
   __shared__ Buffer buffers[Buffer::kCount];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
   const int first = (blockIdx.x * NW + wave) * 16 * CT;

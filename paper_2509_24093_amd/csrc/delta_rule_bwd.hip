@@ -49,7 +49,8 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
   constexpr int ST = Buffer::ST;
   __shared__ Buffer buffers[Buffer::kCount];
   const RuleArgs& a = g.a;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
   const int col = (blockIdx.x * NW + wave) * 16 + m;
@@ -228,21 +229,19 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
 // ---- gradients of keys, queries, decays and betas -------------------------------------------
 
 // Eight columns from col on of a chunk's token (row: its first token), a slice ahead of their
-// use; zeros where there is no column or no token.  Where eight columns of a head are neighbours
-// in memory (P a multiple of eight) they are one load; what is not there is read from a place
-// that is.
-template <class T>
+// use; zeros where there is no column or no token.  PACKED: eight columns of a head are neighbours
+// in memory (P a multiple of eight), one load; what is not there is read from a place that is.
+template <class T, bool PACKED>
 struct SliceStage {
   Raw<T, 8> raw;
-  __device__ __forceinline__ void load(const T* row, int t, int tokens, int stride, int col, int V, int P, int C,
-                                       int h) {
-    const T* from = row + (long long)min(t, tokens - 1) * stride;
-    if (P % 8 == 0) {
-      raw.load(from + Column(col, V, P, C, h).at);
+  // at: bytes of the token's row from the base
+  __device__ __forceinline__ void load(const T* base, uint32_t at, int col, int V, int P, int C, int h) {
+    if constexpr (PACKED) {
+      raw.load(&place(base, at + Column(col, V, P, C, h).at * (int)sizeof(T)));
     } else {
       T x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = from[Column(col + e, V, P, C, h).at];
+      for (int e = 0; e < 8; ++e) x[e] = place(base, at + Column(col + e, V, P, C, h).at * (int)sizeof(T));
       __builtin_memcpy(raw.w, x, sizeof x);
     }
   }
@@ -300,7 +299,7 @@ struct GradsSpace {
 // the other.  Wave w owns the tile of the 16 key components from 16 w on (rows of S and gS) for
 // all tokens; of the 64 x 64 matrices wave w < 4 has the row of tiles w of M1, wave w + 4 that
 // of M2.
-template <class T, int KB>
+template <class T, int KB, bool PACKED>
 __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs ws) {
   typedef GradsSpace<T, KB> Space;
   constexpr int NP = kParts<T>, ST = row_stride(KB), DT = 2 * KB, SS = Slice<T>::ST;
@@ -311,7 +310,8 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
   auto& tb = space.tb;
   auto& dots = space.dots;
   const RuleArgs& a = g.a;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int m = lane & 15, q = lane >> 4;
   const int chunk = blockIdx.x, b = blockIdx.y / a.n.Hk, hk = blockIdx.y - b * a.n.Hk;
   const int each = a.n.H / a.n.Hk, P = a.n.C / a.n.H;
   const int D = a.n.D, C = a.n.C, KC = a.n.K * C, N = a.n.N;
@@ -356,10 +356,14 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
   for (int i = 0; i < kTiles; ++i) totq[i] = totk[i] = v4f{0.f, 0.f, 0.f, 0.f};
 
   for (int e = 0; e < each; ++e) {
+    const int lane = afresh_lane(tid & 63), m = lane & 15, q = lane >> 4, own = 16 * wave + m;
     const int h = hk * each + e, unit = b * a.n.H + h;
     const long long at = (long long)unit * ws.chunks + chunk;
-    const long long state0 = (at * (32 * KB) + (owner ? own : 0)) * ws.VP + 4 * q;
-    const float* wide = (second ? ws.value : ws.gvalue) + (at * kT + st) * ws.VP + sc;
+    const float* S = ws.state + at * (32 * KB) * ws.VP;
+    const float* gS = ws.gstate + at * (32 * KB) * ws.VP;
+    const float* wide = (second ? ws.value : ws.gvalue) + at * kT * ws.VP;
+    const uint32_t state_at = 4 * (__umul24(owner ? own : 0, ws.VP) + 4 * q), wide_at = 4 * (__umul24(st, ws.VP) + sc);
+    const uint32_t row_at = __umul24(min(st, tokens - 1), KC * (int)sizeof(T));
     const T* rows = static_cast<const T*>(second ? g.gy : a.v) + ((long long)b * N + t0) * KC;
     const float whole = ws.whole[at];
     __syncthreads();  // the head before has been read
@@ -369,20 +373,18 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     v4f aq[kTiles], al[kTiles], ar[kTiles], w[kTiles];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) aq[i] = al[i] = ar[i] = w[i] = v4f{0.f, 0.f, 0.f, 0.f};
-    float both = 0.f, yv = 0.f, wx[8], sx[8], gx[8];
-    SliceStage<T> narrow;
+    float both = 0.f, yv = 0.f;
+    Raw<float, 8> wide_raw;
+    v4f sx[2], gx[2];
+    SliceStage<T, PACKED> narrow;
+    // asked for a slice ahead, the last one twice: a branch here would wait for it
     const auto fetch = [&](int v0) {
-      load_vec(wide + v0, wx);
-      narrow.load(rows, st, tokens, KC, v0 + sc, ws.V, P, C, h);
+      wide_raw.load(&place(wide, wide_at + 4 * v0));
+      narrow.load(rows, row_at, v0 + sc, ws.V, P, C, h);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const v4f x = *reinterpret_cast<const v4f*>(ws.state + state0 + v0 + 16 * half);
-        const v4f y = *reinterpret_cast<const v4f*>(ws.gstate + state0 + v0 + 16 * half);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          sx[4 * half + r] = x[r];
-          gx[4 * half + r] = y[r];
-        }
+        sx[half] = place(reinterpret_cast<const v4f*>(S), state_at + 4 * (v0 + 16 * half));
+        gx[half] = place(reinterpret_cast<const v4f*>(gS), state_at + 4 * (v0 + 16 * half));
       }
     };
     fetch(0);
@@ -390,8 +392,9 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
       auto& slice = space.slice[n & (Space::kSlices - 1)];
       if (Space::kSlices == 1 && n) __syncthreads();  // the one before has been read
       {
-        float x[8];
+        float x[8], wx[8];
         Frag f[3];
+        wide_raw.widen_to(wx);
         narrow.get(st < tokens, v0 + sc, ws.V, x);
         split8(wx, f);
 #pragma unroll
@@ -410,11 +413,11 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
       Frag fs[3], fg[3];
       if (owner) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) both = fmaf(sx[c], gx[c], both);
+        for (int c = 0; c < 8; ++c) both = fmaf(sx[c / 4][c % 4], gx[c / 4][c % 4], both);
       }
-      split8(sx, fs);
-      split8(gx, fg);
-      if (v0 + 32 < ws.VP) fetch(v0 + 32);
+      split_tiles(sx[0], sx[1], fs);
+      split_tiles(gx[0], gx[1], fg);
+      fetch(min(v0 + 32, ws.VP - 32));
       __syncthreads();  // the slice is there
       Frag fv[kTiles][3];
 #pragma unroll
@@ -649,7 +652,11 @@ hipError_t backward(const RuleBwdArgs& g, const RuleWs& w, hipStream_t s) {
   }
   e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, false>, 4) : walk(rule_reverse_kernel<T, KB, 8, false>, 8);
   if (e != hipSuccess || !(g.gq || g.gk || g.gdecay || g.gbeta)) return e;
-  hipLaunchKernelGGL((rule_grads_kernel<T, KB>), dim3(w.chunks, g.a.n.B * g.a.n.Hk), dim3(512), 0, s, g, w);
+  const dim3 grid(w.chunks, g.a.n.B * g.a.n.Hk);
+  if (g.a.n.C / g.a.n.H % 8 == 0)
+    hipLaunchKernelGGL((rule_grads_kernel<T, KB, true>), grid, dim3(512), 0, s, g, w);
+  else
+    hipLaunchKernelGGL((rule_grads_kernel<T, KB, false>), grid, dim3(512), 0, s, g, w);
   return hipGetLastError();
 }
 

@@ -19,7 +19,8 @@ template <int KB, bool REVERSE>
 __global__ __launch_bounds__(256) void rule_join_kernel(const float* first, RuleWs ws, RuleSizes n) {
   constexpr int DT = 2 * KB, NT = (DT + 3) / 4, DP = 32 * KB;
   __shared__ v4f S[DT][64];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, m = lane & 15, q = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / n.H, h = unit - b * n.H, col = blockIdx.x * 16 + m;
   const Column column(col, ws.V, n.C / n.H, n.C, h);
   const long long KC = (long long)n.K * n.C;

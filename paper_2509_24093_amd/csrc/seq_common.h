@@ -131,6 +131,10 @@ __device__ __forceinline__ int afresh(int x) {
   asm volatile("" : "+s"(x));
   return x;
 }
+__device__ __forceinline__ int afresh_lane(int x) {  // x differs from lane to lane
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
