@@ -322,6 +322,7 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
     }
   }
   for (int c = begin; c < end; ++c) {
+    const int lane = afresh_lane(tid & 63), m = lane & 15, q = lane >> 4;
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
     Buffer& buf = buffers[(c - begin) & (Buffer::kCount - 1)];

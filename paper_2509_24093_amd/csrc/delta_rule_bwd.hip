@@ -112,6 +112,7 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
     }
   }
   for (int c = end - 1; c >= begin; --c) {
+    const int lane = afresh_lane(tid & 63), m = lane & 15, q = lane >> 4;
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
     Buffer& buf = buffers[(end - 1 - c) & (Buffer::kCount - 1)];
