@@ -236,29 +236,30 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
 enum Walk {
   kOutputs,  // the outputs, and the last state
   kKeep,     // the state before every chunk and V', for the backward
-  kSpan,     // of a segment of the chunks: its last state from zero, and from every unit
-             // vector with no values written, which is the segment's matrix
+  kSpan,     // of every segment of the chunks but the last: its last state, of the first from the
+             // given one, of others from zero, and of these also from every unit vector with no
+             // values written, which is the segment's matrix
 };
 
-// Block (group of 16 NW CT columns, unit, segment); a wave has CT tiles of 16 side by side.  The columns of kSpan are the VP of the
+// Block (group of 16 NW columns, unit, segment).  The columns of kSpan are the VP of the
 // values, then those of the matrix.
-template <class T, int KB, int NW, int CT, int WALK>
+template <class T, int KB, int NW, int WALK>
 __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs ws) {
   constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * NW;
   constexpr bool kOut = WALK == kOutputs;
   typedef Stage<T, KB, kOut, kOut> Buffer;
   constexpr int ST = Buffer::ST;
   __shared__ Buffer buffers[Buffer::kCount];
+  __shared__ float turn[WALK == kSpan ? NW : 1][16][20];  // of the matrix: a tile, read along its rows
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int first = (blockIdx.x * NW + wave) * 16 * CT;
-  const bool active = first < (kOut ? ws.V : WALK == kKeep ? ws.VP : ws.VP + 32 * KB);
+  const int first = (blockIdx.x * NW + wave) * 16;
   const bool matrix = WALK == kSpan && first >= ws.VP;
-  Column column[CT];
-#pragma unroll
-  for (int t = 0; t < CT; ++t) column[t] = Column(first + 16 * t + m, ws.V, C / a.n.H, C, h);
+  const bool active = first < (kOut ? ws.V : WALK == kKeep ? ws.VP : ws.VP + 32 * KB) && !(matrix && seg == 0);
+  if (WALK == kSpan && seg == 0 && (int)blockIdx.x * NW * 16 >= ws.VP) return;
+  const Column column(first + m, ws.V, C / a.n.H, C, h);
   const int length = tokens_of(a, b);
   const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
   const int end = min((length + kT - 1) / kT, last);
@@ -269,29 +270,28 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
   T* y = static_cast<T*>(a.y) + (kOut ? (long long)b * N * KC : 0);
   const long long start = ((long long)unit * ws.segments + seg) * (32 * KB);  // row of a segment's state
 
-  v4f S[CT][DT];
+  v4f S[DT];
 #pragma unroll
-  for (int t = 0; t < CT; ++t)
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * d + 4 * q + r, col = first + 16 * t + m;
-        float x = 0.f;
-        if (WALK == kSpan) {
-          x = matrix && row == col - ws.VP ? 1.f : 0.f;
-        } else if (seg > 0) {
-          if (col < ws.VP) x = ws.start[(start + row) * ws.VP + col];
-        } else if (a.state_in && column[t].there && row < D) {
-          x = a.state_in[((long long)b * D + row) * KC + column[t].at];
-        }
-        S[t][d][r] = x;
+    for (int r = 0; r < 4; ++r) {
+      const int row = 16 * d + 4 * q + r, col = first + m;
+      float x = 0.f;
+      if (matrix) {
+        x = row == col - ws.VP ? 1.f : 0.f;
+      } else if (WALK == kSpan && seg > 0) {
+      } else if (seg > 0) {
+        if (col < ws.VP) x = ws.start[(start + row) * ws.VP + col];
+      } else if (a.state_in && column.there && row < D) {
+        x = a.state_in[((long long)b * D + row) * KC + column.at];
       }
+      S[d][r] = x;
+    }
 
   RowStage<T, KB, kThreads> sk, sq;
   BlockStage<kThreads> si, sp;
   float4 st;
-  ColumnStage<T> sv[CT];
+  ColumnStage<T> sv;
   const auto fetch = [&](int c) {
     const int tokens = min(length - c * kT, kT);
     const long long at = (long long)unit * ws.chunks + c;
@@ -310,8 +310,7 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
     if (tid < kT) to.token[tid] = st;
   };
   const auto fetch_values = [&](int c) {
-#pragma unroll
-    for (int t = 0; t < CT; ++t) sv[t].load(v + (long long)c * kT * KC, KC, min(length - c * kT, kT), column[t], q);
+    sv.load(v + (long long)c * kT * KC, KC, min(length - c * kT, kT), column, q);
   };
   if (begin < end) {
     fetch(begin);
@@ -338,32 +337,25 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
     const auto& inv = buf.inv;
     const auto& inside = buf.inside;
     const float4* ta = buf.token;
-    v4f X[CT][kTiles], O[CT][kTiles];
+    v4f X[kTiles], O[kTiles];
     if (active) {
       if constexpr (WALK == kKeep) {
-#pragma unroll
-        for (int t = 0; t < CT; ++t)
-          store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, first + 16 * t + m, q, S[t]);
+        store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, first + m, q, S);
       }
 #pragma unroll
-      for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) X[t][i] = O[t][i] = v4f{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < kTiles; ++i) X[i] = O[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        Frag s[CT][3];
-#pragma unroll
-        for (int t = 0; t < CT; ++t) split_tiles(S[t][2 * kb], S[t][2 * kb + 1], s[t]);
+        Frag s[3];
+        split_tiles(S[2 * kb], S[2 * kb + 1], s);
         Frag f[kTiles][NP];
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) rows_frag<NP, ST>(kbuf, i, kb, m, q, f[i]);
-#pragma unroll
-        for (int t = 0; t < CT; ++t) mma_all(f, s[t], X[t]);
+        mma_all(f, s, X);
         if constexpr (kOut) {
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) rows_frag<NP, ST>(qbuf, i, kb, m, q, f[i]);
-#pragma unroll
-          for (int t = 0; t < CT; ++t) mma_all(f, s[t], O[t]);
+          mma_all(f, s, O);
         }
       }
       // Y, then V' = (1 + A)^-1 Y
@@ -372,25 +364,17 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float4 tok = ta[16 * i + 4 * q + r];
-#pragma unroll
-          for (int t = 0; t < CT; ++t) {
-            X[t][i][r] = tok.x * fmaf(-tok.y, X[t][i][r], sv[t].get(i, r, column[t]));
-            O[t][i][r] *= tok.w;
-          }
+          X[i][r] = tok.x * fmaf(-tok.y, X[i][r], sv.get(i, r, column));
+          if constexpr (kOut) O[i][r] *= tok.w;
         }
       if (c + 1 < end) fetch_values(c + 1);
-      Frag fy[CT][2][3];
+      Frag fy[2][3];
 #pragma unroll
-      for (int t = 0; t < CT; ++t)
+      for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fy[kb]);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) split_tiles(X[t][2 * kb], X[t][2 * kb + 1], fy[t][kb]);
+      for (int i = 0; i < kTiles; ++i) X[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < CT; ++t) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) X[t][i] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inv, kb, lane, fy[t][kb], X[t]);
-      }
+      for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inv, kb, lane, fy[kb], X);
     }
     if (Buffer::kCount == 2 && c + 1 < end) {
       put(c + 1, buffers[(c + 1 - begin) & 1]);
@@ -398,81 +382,85 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
     }
     if (!active) continue;
     if constexpr (WALK == kKeep) {
-#pragma unroll
-      for (int t = 0; t < CT; ++t) store_tiles(ws.value + at * kT * ws.VP, ws.VP, first + 16 * t + m, q, X[t]);
+      store_tiles(ws.value + at * kT * ws.VP, ws.VP, first + m, q, X);
     }
     if constexpr (kOut) {
-      Frag fv[CT][2][3];
+      Frag fv[2][3];
 #pragma unroll
-      for (int t = 0; t < CT; ++t)
+      for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fv[kb]);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) split_tiles(X[t][2 * kb], X[t][2 * kb + 1], fv[t][kb]);
-#pragma unroll
-      for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inside, kb, lane, fv[t][kb], O[t]);
-#pragma unroll
-      for (int t = 0; t < CT; ++t)
-        store_column(y + (long long)c * kT * KC, KC, N - c * kT, tokens, column[t], q, O[t]);
+      for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inside, kb, lane, fv[kb], O);
+      store_column(y + (long long)c * kT * KC, KC, N - c * kT, tokens, column, q, O);
     }
     // S <- e^{G_end} S + K^T (e^{G_end - G} rk V')
-    Frag fz[CT][2][3];
+    Frag fz[2][3];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float z = ta[16 * i + 4 * q + r].z;
-#pragma unroll
-        for (int t = 0; t < CT; ++t) X[t][i][r] *= z;
+        X[i][r] *= ta[16 * i + 4 * q + r].z;
       }
 #pragma unroll
-    for (int t = 0; t < CT; ++t)
+    for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fz[kb]);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) split_tiles(X[t][2 * kb], X[t][2 * kb + 1], fz[t][kb]);
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int t = 0; t < CT; ++t)
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][d][r] *= whole;
+      for (int r = 0; r < 4; ++r) S[d][r] *= whole;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       Frag f[DT][NP];
 #pragma unroll
       for (int d = 0; d < DT; ++d) columns_frag<NP, ST>(kbuf, d, kb, m, q, f[d]);
-#pragma unroll
-      for (int t = 0; t < CT; ++t) mma_all(f, fz[t][kb], S[t]);
+      mma_all(f, fz[kb], S);
     }
   }
   if constexpr (WALK == kSpan) {
     if (!active) return;
+    const int col = first + m;
+    if (!matrix) {
+      store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S);
+    } else {
+      const int j = (first - ws.VP) / 16;  // the matrix's columns from 16 j on
+      const long long at = ((long long)unit * ws.segments + seg) * (DT * KB * 3 * 64);
+      auto& tile = turn[wave];
 #pragma unroll
-    for (int t = 0; t < CT; ++t) {
-      const int col = first + 16 * t + m;
-      if (!matrix) {
-        store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S[t]);
-      } else {
-        float* to = ws.span_matrix + (start + col - ws.VP) * (32 * KB) + 4 * q;  // its columns are rows here
+      for (int d = 0; d < DT; ++d) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<v4f*>(to + 16 * d) = S[t][d];
+        for (int r = 0; r < 4; ++r) tile[4 * q + r][m] = S[d][r];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const v4f x = *reinterpret_cast<const v4f*>(&tile[m][4 * q]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        uint2 part[3];
+        split2(x[0], x[1], part[0].x, part[1].x, part[2].x);
+        split2(x[2], x[3], part[0].y, part[1].y, part[2].y);
+        uint4* to = ws.span_matrix + at + ((d * KB + j / 2) * 3) * 64 + lane;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) reinterpret_cast<uint2*>(to + 64 * p)[j & 1] = part[p];
+      }
+      if (ws.span_matrixT) {
+        uint4* to = ws.span_matrixT + at + (j * KB * 3) * 64 + lane;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          Frag f[3];
+          split_tiles(S[2 * kb], S[2 * kb + 1], f);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) to[64 * (3 * kb + p)] = f[p].all;
+        }
       }
     }
   }
   if constexpr (kOut) {
+    if (!column.there) return;
+    const long long stop = min((long long)last * kT, (long long)N);
+    for (long long n = (long long)max(end, begin) * kT + q; n < stop; n += 4) y[n * KC + column.at] = (T)0.f;
+    if (!a.state_out || last != ws.chunks) return;
 #pragma unroll
-    for (int t = 0; t < CT; ++t) {
-      if (!column[t].there) continue;
-      const long long stop = min((long long)last * kT, (long long)N);
-      for (long long n = (long long)max(end, begin) * kT + q; n < stop; n += 4) y[n * KC + column[t].at] = (T)0.f;
-      if (!a.state_out || last != ws.chunks) continue;
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * d + 4 * q + r;
-          if (row < D) a.state_out[((long long)b * D + row) * KC + column[t].at] = S[t][d][r];
-        }
-    }
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * d + 4 * q + r;
+        if (row < D) a.state_out[((long long)b * D + row) * KC + column.at] = S[d][r];
+      }
   }
 }
 
@@ -597,28 +585,29 @@ hipError_t prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_
   });
 }
 
-template <class T, int NW, int CT, int WALK>
+template <class T, int NW, int WALK>
 hipError_t walk(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
-  constexpr int kColumns = 16 * NW * CT;
+  constexpr int kColumns = 16 * NW;
   const int columns = WALK == kOutputs ? w.V : WALK == kKeep ? w.VP : w.VP + 32 * w.KB;
-  const dim3 grid((columns + kColumns - 1) / kColumns, w.units, w.segments);
+  const dim3 grid((columns + kColumns - 1) / kColumns, w.units, WALK == kSpan ? w.segments - 1 : w.segments);
   return by_width(w.KB, [&](auto kb) {
-    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, NW, CT, WALK>), grid, dim3(64 * NW), 0, s, a, w);
+    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, NW, WALK>), grid, dim3(64 * NW), 0, s, a, w);
     return hipGetLastError();
   });
 }
 
 template <class T, int WALK>
 hipError_t walk_any(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
-  if (WALK != kSpan && w.V <= 64) return walk<T, 4, 1, WALK>(a, w, s);
-  return walk<T, 8, 1, WALK>(a, w, s);
+  if constexpr (WALK != kSpan)
+    if (w.V <= 64) return walk<T, 4, WALK>(a, w, s);
+  return walk<T, 8, WALK>(a, w, s);
 }
 
 template <class T>
 hipError_t states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s) {
   if (w.segments > 1) {
     hipError_t e = walk_any<T, kSpan>(a, w, s);
-    if (e == hipSuccess) e = launch_rule_join(a.state_in, w, a.n, false, s);
+    if (e == hipSuccess) e = launch_rule_join(w, false, s);
     if (e != hipSuccess) return e;
   }
   return backward ? walk_any<T, kKeep>(a, w, s) : walk_any<T, kOutputs>(a, w, s);

@@ -40,8 +40,8 @@ __device__ __forceinline__ int tokens_of(const RuleArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.n.N) : a.n.N;
 }
 
-// Block (group of 16 NW columns, unit, segment).  SPAN: only what the segment adds to the
-// state's gradient.
+// Block (group of 16 NW columns, unit, segment).  SPAN: of every segment but the first only
+// the gradient of the state before it, of the last from the given one, of others from zero.
 template <class T, int KB, int NW, bool SPAN>
 __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
   constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * NW;
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
   const RuleArgs& a = g.a;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int m = lane & 15, q = lane >> 4;
-  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
+  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z + SPAN;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
   const int col = (blockIdx.x * NW + wave) * 16 + m;
   const bool active = (blockIdx.x * NW + wave) * 16 < ws.VP;
@@ -73,9 +73,8 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
     for (int r = 0; r < 4; ++r) {
       const int row = 16 * d + 4 * q + r;
       float x = 0.f;
-      if (SPAN) {
-      } else if (ws.segments > 1) {
-        if (active) x = ws.start[(start + row) * ws.VP + col];
+      if (seg + 1 < ws.segments) {
+        if (!SPAN && active) x = ws.start[(start + row) * ws.VP + col];
       } else if (g.gstate && column.there && row < D) {
         x = g.gstate[((long long)b * D + row) * KC + column.at];
       }
@@ -640,18 +639,19 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
 
 template <class T, int KB>
 hipError_t backward(const RuleBwdArgs& g, const RuleWs& w, hipStream_t s) {
-  const auto walk = [&](auto kernel, int waves) {
-    hipLaunchKernelGGL(kernel, dim3((w.VP + 16 * waves - 1) / (16 * waves), w.units, w.segments), dim3(64 * waves), 0, s,
-                       g, w);
+  const auto walk = [&](auto kernel, int waves, int segments) {
+    hipLaunchKernelGGL(kernel, dim3((w.VP + 16 * waves - 1) / (16 * waves), w.units, segments), dim3(64 * waves), 0, s, g, w);
     return hipGetLastError();
   };
   hipError_t e = hipSuccess;
   if (w.segments > 1) {
-    e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, true>, 4) : walk(rule_reverse_kernel<T, KB, 8, true>, 8);
-    if (e == hipSuccess) e = launch_rule_join(g.gstate, w, g.a.n, true, s);
+    e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, true>, 4, w.segments - 1)
+                  : walk(rule_reverse_kernel<T, KB, 8, true>, 8, w.segments - 1);
+    if (e == hipSuccess) e = launch_rule_join(w, true, s);
     if (e != hipSuccess) return e;
   }
-  e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, false>, 4) : walk(rule_reverse_kernel<T, KB, 8, false>, 8);
+  e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, false>, 4, w.segments)
+                : walk(rule_reverse_kernel<T, KB, 8, false>, 8, w.segments);
   if (e != hipSuccess || !(g.gq || g.gk || g.gdecay || g.gbeta)) return e;
   const dim3 grid(w.chunks, g.a.n.B * g.a.n.Hk);
   if (g.a.n.C / g.a.n.H % 8 == 0)

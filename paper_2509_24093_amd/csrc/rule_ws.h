@@ -18,9 +18,12 @@ struct RuleWs {
   float* gstate;   // [unit][chunk][DP][VP]: gradient of the state after every chunk
   float* value;    // [unit][chunk][64][VP]: what the tokens write, V'
   float* gvalue;   // [unit][chunk][64][VP]: its gradient through (1 + A)^-T, dY
-  float* start;        // [unit][segment][DP][VP]: the state before every segment (its gradient behind it)
-  float* span_state;   // [unit][segment][DP][VP]: what a segment adds to the state
-  float* span_matrix;  // [unit][segment][DP][DP]: and by what it multiplies it, columns as rows
+  float* start;       // [unit][segment][DP][VP]: the state before every segment (its gradient behind it)
+  float* span_state;  // [unit][segment][DP][VP]: what a segment adds to the state
+  // and by what it multiplies it, as the join's operand: [unit][segment][DP / 16 tiles of rows]
+  // [DP / 32][3 parts][64 lanes]; and its transpose (backward)
+  uint4* span_matrix;
+  uint4* span_matrixT;
   int units, chunks, KB, V, VP;  // DP = 32 KB; VP: V in whole tiles of 32
   int segments, span;            // the chunks in segments of `span`, walked at once
 };
@@ -62,7 +65,9 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
   if (w.segments > 1) {
     take(w.start, (size_t)w.units * w.segments * 32 * w.KB * w.VP);
     take(w.span_state, (size_t)w.units * w.segments * 32 * w.KB * w.VP);
-    take(w.span_matrix, (size_t)w.units * w.segments * 1024 * w.KB * w.KB);
+    const size_t matrix = (size_t)w.units * w.segments * 2 * w.KB * w.KB * 3 * 64;
+    take(w.span_matrix, matrix);
+    if (backward) take(w.span_matrixT, matrix);
   }
   if (bytes) *bytes = at;
   return w;
@@ -72,8 +77,8 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
 hipError_t launch_rule_prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
 // The states from chunk to chunk; for the backward they and V' are kept and no output is formed.
 hipError_t launch_rule_states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s);
-// From what every segment adds and multiplies by, the state before every segment, or in
-// reverse the gradient of the state behind it; `first`: [B][D][K][C] or nullptr (zeros).
-hipError_t launch_rule_join(const float* first, const RuleWs& w, const RuleSizes& n, bool reverse, hipStream_t s);
+// From what every segment adds and multiplies by, the state before every segment but the
+// first, or in reverse the gradient of the state behind every one but the last.
+hipError_t launch_rule_join(const RuleWs& w, bool reverse, hipStream_t s);
 
 }  // namespace cgconv
