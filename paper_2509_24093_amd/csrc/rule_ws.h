@@ -28,12 +28,23 @@ struct RuleWs {
   int segments, span;            // the chunks in segments of `span`, walked at once
 };
 
-// Chunks of a segment.
-inline int rule_span(int chunks, int units, int VP) {
-  const long long blocks = (long long)units * ((VP + 127) / 128);
-  if (blocks >= 128 || chunks < 8) return chunks;
-  const int segments = (int)std::min<long long>(chunks / 4, (256 + blocks - 1) / blocks);
-  return (chunks + segments - 1) / segments;
+// Chunks of a segment.  A walk takes as many rounds of 256 blocks, one a CU, as its segments'
+// blocks of 128 columns make (those of the first span walk have no matrix), a round the
+// segment's length; joining takes half a chunk's time a step.
+inline int rule_span(int chunks, int units, int KB, int VP) {
+  const long long values = (VP + 127) / 128, both = (VP + 32 * KB + 127) / 128;
+  const auto rounds = [&](long long blocks) { return (units * blocks + 255) / 256; };
+  int best = chunks;
+  long long least = 2 * chunks * rounds(values);
+  for (int want = 2; want <= std::min(chunks / 4, 64); ++want) {
+    const int span = (chunks + want - 1) / want, n = (chunks + span - 1) / span;
+    const long long cost = 2 * span * (rounds(values * n) + rounds(values + both * (n - 2))) + n - 2;
+    if (cost < least) {
+      least = cost;
+      best = span;
+    }
+  }
+  return best;
 }
 
 inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size_t* bytes) {
@@ -60,7 +71,7 @@ inline RuleWs rule_workspace(const RuleSizes& n, bool backward, char* base, size
     take(w.value, count * kRuleChunk * w.VP);
     take(w.gvalue, count * kRuleChunk * w.VP);
   }
-  w.span = rule_span(w.chunks, w.units, w.VP);
+  w.span = rule_span(w.chunks, w.units, w.KB, w.VP);
   w.segments = (w.chunks + w.span - 1) / w.span;
   if (w.segments > 1) {
     take(w.start, (size_t)w.units * w.segments * 32 * w.KB * w.VP);
