@@ -30,7 +30,10 @@ struct RuleWs {
 
 // Chunks of a segment.  A walk takes as many rounds of 256 blocks, one a CU, as its segments'
 // blocks of 128 columns make (those of the first span walk have no matrix), a round the
-// segment's length; joining takes half a chunk's time a step.
+// segment's length; joining takes half a chunk's time a step.  Measured, bf16, heads of 128 x
+// 128: 4 prompts of 8192 tokens and 16 heads in 1, 2, 3, 4, 8 segments 970, 851, 627, 659, 714 us;
+// 32768 tokens of 8 heads in 16, 24, 32, 64 segments 456, 461, 413, 492; training of 2 x 4096
+// tokens of 8 heads in 4, 8, 16 segments 784, 577, 584.
 inline int rule_span(int chunks, int units, int KB, int VP) {
   const long long values = (VP + 127) / 128, both = (VP + 32 * KB + 127) / 128;
   const auto rounds = [&](long long blocks) { return (units * blocks + 255) / 256; };
