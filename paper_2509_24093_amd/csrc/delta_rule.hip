@@ -242,29 +242,30 @@ enum Walk {
              // values written, which is the segment's matrix
 };
 
-// Block (group of 16 NW columns, unit, segment).  The columns of kSpan are the VP of the
+// Block (128 columns, unit, segment).  The columns of kSpan are the VP of the
 // values, then those of the matrix.  A wave's chunk is a chain of products, each waiting for
 // the one before, so it is bound by latency: with heads of 128 x 128 and eight waves a block,
 // a chunk of 64 tokens takes 8.6 us with its outputs, 5.3 without; the matrix cores are busy 29%
 // of the time, the vector units 40%, the LDS 36%.  More of a state's columns in a wave (32: 860
-// us of a prompt instead of 688) or fewer waves that share a chunk (four: 1061) are slower;
-// a chunk in LDS ahead, and products of one accumulator apart, took 740 to 688.
-template <class T, int KB, int NW, int WALK>
-__global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs ws) {
-  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * NW;
+// us of a prompt instead of 688) or fewer waves that share a chunk (four: 1061, and for heads of
+// 64 columns, which occupy no more, 195 us instead of 174) are slower; a chunk in LDS ahead, and
+// products of one accumulator apart, took 740 to 688.
+template <class T, int KB, int WALK>
+__global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a, RuleWs ws) {
+  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * kWalkWaves;
   constexpr bool kOut = WALK == kOutputs;
   typedef Stage<T, KB, kOut, kOut> Buffer;
   constexpr int ST = Buffer::ST;
   __shared__ Buffer buffers[Buffer::kCount];
-  __shared__ float turn[WALK == kSpan ? NW : 1][16][20];  // of the matrix: a tile, read along its rows
+  __shared__ float turn[WALK == kSpan ? kWalkWaves : 1][16][20];  // of the matrix: a tile, read along its rows
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int first = (blockIdx.x * NW + wave) * 16;
+  const int first = (blockIdx.x * kWalkWaves + wave) * 16;
   const bool matrix = WALK == kSpan && first >= ws.VP;
   const bool active = first < (kOut ? ws.V : WALK == kKeep ? ws.VP : ws.VP + 32 * KB) && !(matrix && seg == 0);
-  if (WALK == kSpan && seg == 0 && (int)blockIdx.x * NW * 16 >= ws.VP) return;
+  if (WALK == kSpan && seg == 0 && (int)blockIdx.x * kWalkWaves * 16 >= ws.VP) return;
   const Column column(first + m, ws.V, C / a.n.H, C, h);
   const int length = tokens_of(a, b);
   const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
@@ -472,14 +473,15 @@ __global__ __launch_bounds__(64 * NW) void rule_state_kernel(RuleArgs a, RuleWs 
 
 // ---- one token ---------------------------------------------------------------------------
 
-// Block (group of columns, unit): LANES vectors of VC columns side by side, 256 / LANES
-// rows of the state at a time, all of a thread's rows in registers, so the state is read
-// once and written once (bound by its bytes; of few sequences by the latency of one
-// chain load - sum - store).  Both sums over the rows come first:
+// Block (group of columns, unit): 16 vectors of VC columns side by side, 16 rows of the state at
+// a time, all of a thread's rows in registers, so the state is read once and written once.  Bound
+// by its bytes: 64 sequences of 16 heads of 128 x 128, 134 MB, 25.9 us, 5.2 TB/s (38 in blocks of
+// 16 columns); of few sequences by the latency of one chain load - sum - store (one sequence
+// 4.5 us, as in blocks of 16 columns).  Both sums over the rows come first:
 //   y = scale (e^g qn.S + (qn.kn) u),   u = beta (v - e^g kn.S),   S <- e^g S + kn u.
-template <class T, int VC, int LANES>
+template <class T, int VC>
 __global__ __launch_bounds__(256) void rule_step_kernel(RuleArgs a, int V) {
-  constexpr int kGroups = 256 / LANES, kRows = kRuleMaxDim / kGroups;
+  constexpr int LANES = 16, kGroups = 256 / LANES, kRows = kRuleMaxDim / kGroups;
   __shared__ float kn[kRuleMaxDim], qn[kRuleMaxDim], dots[4][3];
   __shared__ float part[4][2][LANES * VC];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -591,32 +593,25 @@ hipError_t prepare(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_
   });
 }
 
-template <class T, int NW, int WALK>
+template <class T, int WALK>
 hipError_t walk(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
-  constexpr int kColumns = 16 * NW;
+  constexpr int kColumns = 16 * kWalkWaves;
   const int columns = WALK == kOutputs ? w.V : WALK == kKeep ? w.VP : w.VP + 32 * w.KB;
   const dim3 grid((columns + kColumns - 1) / kColumns, w.units, WALK == kSpan ? w.segments - 1 : w.segments);
   return by_width(w.KB, [&](auto kb) {
-    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, NW, WALK>), grid, dim3(64 * NW), 0, s, a, w);
+    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, WALK>), grid, dim3(64 * kWalkWaves), 0, s, a, w);
     return hipGetLastError();
   });
-}
-
-template <class T, int WALK>
-hipError_t walk_any(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
-  if constexpr (WALK != kSpan)
-    if (w.V <= 64) return walk<T, 4, WALK>(a, w, s);
-  return walk<T, 8, WALK>(a, w, s);
 }
 
 template <class T>
 hipError_t states(const RuleArgs& a, const RuleWs& w, bool backward, hipStream_t s) {
   if (w.segments > 1) {
-    hipError_t e = walk_any<T, kSpan>(a, w, s);
+    hipError_t e = walk<T, kSpan>(a, w, s);
     if (e == hipSuccess) e = launch_rule_join(w, false, s);
     if (e != hipSuccess) return e;
   }
-  return backward ? walk_any<T, kKeep>(a, w, s) : walk_any<T, kOutputs>(a, w, s);
+  return backward ? walk<T, kKeep>(a, w, s) : walk<T, kOutputs>(a, w, s);
 }
 
 template <class T>
@@ -626,12 +621,7 @@ hipError_t step(const RuleArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3((V + columns - 1) / columns, units), dim3(256), 0, s, a, V);
     return hipGetLastError();
   };
-  if (P % 4 == 0) {
-    // 64 columns a block, or 16 where those leave CUs without one
-    if ((long long)((V + 63) / 64) * units >= 256) return run(rule_step_kernel<T, 4, 16>, 64);
-    return run(rule_step_kernel<T, 4, 4>, 16);
-  }
-  return run(rule_step_kernel<T, 1, 16>, 16);
+  return P % 4 == 0 ? run(rule_step_kernel<T, 4>, 64) : run(rule_step_kernel<T, 1>, 16);
 }
 
 }  // namespace

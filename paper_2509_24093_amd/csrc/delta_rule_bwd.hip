@@ -40,12 +40,12 @@ __device__ __forceinline__ int tokens_of(const RuleArgs& a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.n.N) : a.n.N;
 }
 
-// Block (group of 16 NW columns, unit, segment).  SPAN: of every segment but the first only
+// Block (128 columns, unit, segment).  SPAN: of every segment but the first only
 // the gradient of the state before it, of the last from the given one, of others from zero.
 // Bound as the forward's walk: a chunk of a 128 x 128 head takes 10 us, 7.3 with SPAN.
-template <class T, int KB, int NW, bool SPAN>
-__global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
-  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * NW;
+template <class T, int KB, bool SPAN>
+__global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
+  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * kWalkWaves;
   typedef Stage<T, KB, true, true> Buffer;  // the transposed triangles
   constexpr int ST = Buffer::ST;
   __shared__ Buffer buffers[Buffer::kCount];
@@ -54,8 +54,8 @@ __global__ __launch_bounds__(64 * NW) void rule_reverse_kernel(RuleBwdArgs g, Ru
   const int m = lane & 15, q = lane >> 4;
   const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z + SPAN;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int col = (blockIdx.x * NW + wave) * 16 + m;
-  const bool active = (blockIdx.x * NW + wave) * 16 < ws.VP;
+  const int col = (blockIdx.x * kWalkWaves + wave) * 16 + m;
+  const bool active = (blockIdx.x * kWalkWaves + wave) * 16 < ws.VP;
   const Column column(col, ws.V, C / a.n.H, C, h);
   const int length = tokens_of(a, b);
   const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
@@ -643,19 +643,19 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
 
 template <class T, int KB>
 hipError_t backward(const RuleBwdArgs& g, const RuleWs& w, hipStream_t s) {
-  const auto walk = [&](auto kernel, int waves, int segments) {
-    hipLaunchKernelGGL(kernel, dim3((w.VP + 16 * waves - 1) / (16 * waves), w.units, segments), dim3(64 * waves), 0, s, g, w);
+  constexpr int kColumns = 16 * kWalkWaves;
+  const auto walk = [&](auto kernel, int segments) {
+    hipLaunchKernelGGL(kernel, dim3((w.VP + kColumns - 1) / kColumns, w.units, segments), dim3(64 * kWalkWaves), 0, s, g,
+                       w);
     return hipGetLastError();
   };
   hipError_t e = hipSuccess;
   if (w.segments > 1) {
-    e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, true>, 4, w.segments - 1)
-                  : walk(rule_reverse_kernel<T, KB, 8, true>, 8, w.segments - 1);
+    e = walk(rule_reverse_kernel<T, KB, true>, w.segments - 1);
     if (e == hipSuccess) e = launch_rule_join(w, true, s);
     if (e != hipSuccess) return e;
   }
-  e = w.V <= 64 ? walk(rule_reverse_kernel<T, KB, 4, false>, 4, w.segments)
-                : walk(rule_reverse_kernel<T, KB, 8, false>, 8, w.segments);
+  e = walk(rule_reverse_kernel<T, KB, false>, w.segments);
   if (e != hipSuccess || !(g.gq || g.gk || g.gdecay || g.gbeta)) return e;
   const dim3 grid(w.chunks, g.a.n.B * g.a.n.Hk);
   if (g.a.n.C / g.a.n.H % 8 == 0)

@@ -31,6 +31,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr int kT = kRuleChunk;          // tokens of a chunk: four tiles of 16
 constexpr int kTiles = kT / 16;
+constexpr int kWalkWaves = 8;           // of a block that walks the chunks, 16 columns each
 constexpr int kBlocks = kRuleTriangle;  // 16 x 16 blocks on and below the diagonal of kT x kT
 __host__ __device__ constexpr int block_of(int i, int j) { return i * (i + 1) / 2 + j; }
 __host__ __device__ constexpr int row_of(int block) { return block < 1 ? 0 : block < 3 ? 1 : block < 6 ? 2 : 3; }
