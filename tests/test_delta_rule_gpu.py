@@ -31,7 +31,8 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(1, 1, 0, 1, 1, 1, 1), (2, 5, 0, 6, 3, 1, 4), (1, 64, 0, 16, 1, 1, 32), (1, 65, 0, 16, 1, 1, 33),
           (2, 63, 2, 6, 2, 2, 24), (3, 130, 1, 12, 4, 2, 7), (1, 200, 0, 160, 4, 2, 64), (1, 129, 0, 130, 1, 1, 128),
           (1, 100, 3, 4, 1, 1, 96), (2, 37, 0, 72, 9, 3, 65), (1, 70, 0, 300, 1, 1, 40), (1, 80, 4, 16, 2, 1, 16),
-          (2, 1000, 0, 24, 2, 1, 20), (1, 700, 0, 144, 1, 1, 100)]
+          (2, 1000, 0, 24, 2, 1, 20), (1, 700, 0, 144, 1, 1, 100), (1, 1100, 0, 144, 1, 1, 100), (1, 1030, 0, 40, 1, 1, 64),
+          (2, 1090, 1, 24, 2, 1, 90), (1, 2100, 0, 16, 1, 1, 32)]
 
 
 def _inputs(shape, dtype, seed, ragged=False):
