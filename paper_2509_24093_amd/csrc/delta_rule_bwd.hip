@@ -278,6 +278,15 @@ struct Slice {
   alignas(16) bf16 value[3][kT * ST], gvalue[3][kT * ST], gy[kParts<T>][kT * ST];
 };
 
+// Operand with a slice's rows 16 i + m: lane group q has the columns 8 q .. 8 q + 7, as it has of
+// the other operand's rows.
+template <int NP, int N>
+__device__ __forceinline__ void slice_frag(const bf16 (&buf)[NP][N], int i, int m, int q, Frag (&f)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+    f[p].all = *reinterpret_cast<const uint4*>(buf[p] + (16 * i + m) * (N / kT) + 8 * q);
+}
+
 // What a block of rule_grads_kernel shares.  The slices make room for the matrices M1 and beta
 // M2; two of each where they fit, so that the waves meet once a slice, or once for both.
 template <class T, int KB>
@@ -299,8 +308,8 @@ struct GradsSpace {
 // Block (chunk, sequence and key head) of eight waves, the heads that share the key one after
 // the other.  Wave w owns the tile of the 16 key components from 16 w on (rows of S and gS) for
 // all tokens; of the 64 x 64 matrices wave w < 4 has the row of tiles w of M1, wave w + 4 that
-// of M2.  1024 chunks of 128 x 128 heads in bf16: 147 us, four rounds of blocks (a block's
-// accumulators fill the registers of a CU), 0.23 GB at 1.6 TB/s; half of the time is waiting,
+// of M2.  1024 chunks of 128 x 128 heads in bf16: 134 us, four rounds of blocks (a block's
+// accumulators fill the registers of a CU), 0.23 GB at 1.7 TB/s; half of the time is waiting,
 // for the slices' loads and at the meetings, and the LDS is busy 42%.  With four waves that read
 // and split the columns each for itself 313 us, with branches around the slices' loads 228.
 template <class T, int KB, bool PACKED>
@@ -366,12 +375,11 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     const float* S = ws.state + at * (32 * KB) * ws.VP;
     const float* gS = ws.gstate + at * (32 * KB) * ws.VP;
     const float* wide = (second ? ws.value : ws.gvalue) + at * kT * ws.VP;
-    const uint32_t state_at = 4 * (__umul24(owner ? own : 0, ws.VP) + 4 * q), wide_at = 4 * (__umul24(st, ws.VP) + sc);
+    const uint32_t state_at = 4 * (__umul24(owner ? own : 0, ws.VP) + 8 * q), wide_at = 4 * (__umul24(st, ws.VP) + sc);
     const uint32_t row_at = __umul24(min(st, tokens - 1), KC * (int)sizeof(T));
     const T* rows = static_cast<const T*>(second ? g.gy : a.v) + ((long long)b * N + t0) * KC;
     const float whole = ws.whole[at];
-    __syncthreads();  // the head before has been read
-    if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = ws.token[at * 2 * kT + tid];
+    const float4 token = ws.token[at * 2 * kT + (tid & (2 * kT - 1))];
 
     // S gO, S gY, gS V' over the columns, <S, gS>, gO V'^T or gY V'^T of the own row of tiles, and gY.v
     v4f aq[kTiles], al[kTiles], ar[kTiles], w[kTiles];
@@ -379,19 +387,18 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     for (int i = 0; i < kTiles; ++i) aq[i] = al[i] = ar[i] = w[i] = v4f{0.f, 0.f, 0.f, 0.f};
     float both = 0.f, yv = 0.f;
     Raw<float, 8> wide_raw;
-    v4f sx[2], gx[2];
+    Raw<float, 8> state_raw, gstate_raw;
     SliceStage<T, PACKED> narrow;
     // asked for a slice ahead, the last one twice: a branch here would wait for it
     const auto fetch = [&](int v0) {
       wide_raw.load(&place(wide, wide_at + 4 * v0));
       narrow.load(rows, row_at, v0 + sc, ws.V, P, C, h);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        sx[half] = place(reinterpret_cast<const v4f*>(S), state_at + 4 * (v0 + 16 * half));
-        gx[half] = place(reinterpret_cast<const v4f*>(gS), state_at + 4 * (v0 + 16 * half));
-      }
+      state_raw.load(&place(S, state_at + 4 * v0));
+      gstate_raw.load(&place(gS, state_at + 4 * v0));
     };
     fetch(0);
+    __syncthreads();  // the head before has been read
+    if (tid < 2 * kT) (tid & 1 ? tb : ta)[tid >> 1] = token;
     for (int v0 = 0, n = 0; v0 < ws.VP; v0 += 32, ++n) {
       auto& slice = space.slice[n & (Space::kSlices - 1)];
       if (Space::kSlices == 1 && n) __syncthreads();  // the one before has been read
@@ -415,34 +422,39 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
         }
       }
       Frag fs[3], fg[3];
-      if (owner) {
+      {
+        float x[8], y[8];
+        state_raw.widen_to(x);
+        gstate_raw.widen_to(y);
+        if (owner) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) both = fmaf(sx[c / 4][c % 4], gx[c / 4][c % 4], both);
+          for (int c = 0; c < 8; ++c) both = fmaf(x[c], y[c], both);
+        }
+        split8(x, fs);
+        split8(y, fg);
       }
-      split_tiles(sx[0], sx[1], fs);
-      split_tiles(gx[0], gx[1], fg);
       fetch(min(v0 + 32, ws.VP - 32));
       __syncthreads();  // the slice is there
       Frag fv[kTiles][3];
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) rows_frag<3, SS>(slice.value, i, 0, m, q, fv[i]);
+      for (int i = 0; i < kTiles; ++i) slice_frag(slice.value, i, m, q, fv[i]);
       if (owner) mma_all(fv, fg, ar);
       if (second) {
         Frag f[3];
-        rows_frag<3, SS>(slice.gvalue, row, 0, m, q, f);
+        slice_frag(slice.gvalue, row, m, q, f);
         mma_each(f, fv, w);
       } else {
         Frag f[NP];
-        rows_frag<NP, SS>(slice.gy, row, 0, m, q, f);
+        slice_frag(slice.gy, row, m, q, f);
         mma_each(f, fv, w);
       }
       if (owner) {
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) rows_frag<3, SS>(slice.gvalue, i, 0, m, q, fv[i]);
+        for (int i = 0; i < kTiles; ++i) slice_frag(slice.gvalue, i, m, q, fv[i]);
         mma_all(fv, fs, al);
         Frag fo[kTiles][NP];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) rows_frag<NP, SS>(slice.gy, i, 0, m, q, fo[i]);
+        for (int i = 0; i < kTiles; ++i) slice_frag(slice.gy, i, m, q, fo[i]);
         mma_all(fo, fs, aq);
       }
     }
@@ -627,18 +639,68 @@ __global__ __launch_bounds__(512) void rule_grads_kernel(RuleBwdArgs g, RuleWs w
     }
     __syncthreads();
   }
-  if (!owner || own >= D) return;
-#pragma unroll
-  for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = 16 * i + 4 * q + r;
-      if (t >= here) continue;
-      const float x = a.normalize ? space.direct[t] : 0.f, y = a.normalize ? space.dleft[t] : 0.f;
-      const bool there = t < tokens;
-      if (gq) gq[t * stride + own] = there ? (T)fmaf(-x, element(qbuf, t, own), totq[i][r]) : (T)0.f;
-      if (gk) gk[t * stride + own] = there ? (T)fmaf(-y, element(kbuf, t, own), totk[i][r]) : (T)0.f;
+  const auto results = [&](int i, int r, float& gqi, float& gki) {
+    const int t = 16 * i + 4 * q + r;
+    gqi = totq[i][r];
+    gki = totk[i][r];
+    if (a.normalize) {
+      gqi = fmaf(-space.direct[t], element(qbuf, t, own), gqi);
+      gki = fmaf(-space.dleft[t], element(kbuf, t, own), gki);
     }
+    if (t >= tokens) gqi = gki = 0.f;
+  };
+  if constexpr (NP == 1) {
+    // in the place of the keys and queries, from where whole rows go out, rather than in 2-byte
+    // stores of a wave's 16 components
+    if (owner) {
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = (16 * i + 4 * q + r) * ST + own;
+          float x, y;
+          results(i, r, x, y);
+          qbuf[0][at] = (bf16)x;
+          kbuf[0][at] = (bf16)y;
+        }
+    }
+    __syncthreads();
+    const auto store_raw = [](T* to, const bf16* from) {
+      Raw<T, 8> piece;
+      __builtin_memcpy(piece.w, __builtin_assume_aligned(from, 16), 16);
+#pragma unroll
+      for (int i = 0; i < Words<T, 8>::kWords; ++i) reinterpret_cast<typename Words<T, 8>::Unaligned*>(to)[i] = piece.w[i];
+    };
+    const auto out = [&](T* to, const bf16* from) {
+      if (!to) return;
+      if (D % 8 == 0) {
+        const int pieces = D / 8;
+        for (int i = tid; i < here * pieces; i += 512) {
+          const int t = i / pieces, c = (i - t * pieces) * 8;
+          store_raw(to + t * stride + c, from + t * ST + c);
+        }
+      } else {
+        for (int i = tid; i < here * D; i += 512) {
+          const int t = i / D, c = i - t * D;
+          to[t * stride + c] = from[t * ST + c];
+        }
+      }
+    };
+    out(gq, qbuf[0]);
+    out(gk, kbuf[0]);
+  } else if (owner && own < D) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * i + 4 * q + r;
+        float x, y;
+        results(i, r, x, y);
+        if (t >= here) continue;
+        if (gq) gq[t * stride + own] = x;
+        if (gk) gk[t * stride + own] = y;
+      }
+  }
 }
 
 template <class T, int KB>
