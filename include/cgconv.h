@@ -619,9 +619,10 @@ int cgconv_unpack8(int32_t dtype, int64_t rows, int64_t C, const int8_t* codes, 
  * squares are added in 64 bits and in a fixed order; norm (device, one float) receives the
  * norm, an output is rounded once.  An infinity in a gradient makes the norm infinite and
  * the factor zero (0 x infinity is NaN); a NaN makes everything NaN.  max_norm, eps >= 0;
- * max_norm infinite: only the norm.  workspace: device, 8-byte aligned, of
- * cgconv_clip_workspace(n, counts) bytes (a negative status where the list is refused); its
- * use by two calls at once is the caller's to avoid.  No plan.
+ * max_norm infinite: only the norm, whatever it is; a norm and eps of zero: the factor is 1.
+ * workspace: device, 8-byte aligned, of cgconv_clip_workspace(n, counts) bytes (a negative
+ * status where the list is refused); its use by two calls at once is the caller's to avoid.
+ * No plan.
  */
 #define CGCONV_CLIP_TENSORS (1 << 20)
 int64_t cgconv_clip_workspace(int64_t n, const int64_t* counts);

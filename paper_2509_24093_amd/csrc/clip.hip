@@ -135,7 +135,9 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(Batch b, const
   const double total = sqrt(add_sums(part, n, lds));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
   if (b.n == 0) return;
-  const double ratio = (double)max_norm / (total + (double)eps);
+  // without a limit, or with nothing but zeros and no eps, the values stay
+  const double under = total + (double)eps;
+  const double ratio = max_norm == __builtin_inff() || under == 0.0 ? 1.0 : (double)max_norm / under;
   const float factor = ratio >= 1.0 ? 1.f : (float)ratio;  // a NaN stays one
   long long from, to;
   const int t = find(b, blockIdx.x, from, to);

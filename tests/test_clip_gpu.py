@@ -98,6 +98,22 @@ def test_extremes():
     assert math.isnan(float(P.clip_gradients(g, 1.0, out=out))) and all(torch.isnan(x).all() for x in out)
 
 
+def test_no_limit_and_nothing_to_scale():
+    """Without a limit the values stay, whatever their norm; zeros stay without eps too."""
+    torch = torch_gpu()
+    import paper_2509_24093_amd as P
+    for odd in (math.inf, math.nan):
+        g = [torch.ones(10, device="cuda"), torch.ones(10, device="cuda", dtype=torch.bfloat16)]
+        g[0][3] = odd
+        held, out = [x.clone() for x in g], [torch.zeros_like(x) for x in g]
+        for to in (None, out):
+            norm = float(P.clip_gradients(g, math.inf, out=to))
+            assert norm == odd or math.isnan(norm) and math.isnan(odd)
+            assert all(torch.equal(a.nan_to_num(7.0, 8.0), b.nan_to_num(7.0, 8.0)) for a, b in zip(to or g, held))
+    zero = [torch.zeros(100, device="cuda")]
+    assert float(P.clip_gradients(zero, 0.0, eps=0.0)) == 0 and (zero[0] == 0).all()
+
+
 def test_same_result_every_time_and_in_a_graph():
     torch = torch_gpu()
     import paper_2509_24093_amd as P
