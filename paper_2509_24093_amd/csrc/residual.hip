@@ -845,6 +845,19 @@ Form residual_form(int type, int C, int L, bool backward) {
   const int K = (L + 1) * (L + 1);
   Form f{Kind::kRows, type == SEQ_BF16 ? 8 : 4, false};
   f.tail = C % f.v != 0;
+  if (backward) {
+    // Two rows of four channels a thread where a token of them fits a block of 256, so that three
+    // waves share a SIMD: 65536 tokens of L=2 C=64 in fp32 238 us, 444 with four rows; in bf16
+    // 202, 242 with eight channels; 32768 of L=6 C=32 in bf16 289, 341.  In blocks of 512, of
+    // which a CU holds one, they are slower (32768 of L=4 C=128 in bf16 981, 603 with eight
+    // channels in 256).
+    f.row = row_shape(C, K, 4, 2, 256, kRowValues, 1.0);
+    if (f.row.tokens) {
+      f.v = 4;
+      f.tail = C % 4 != 0;
+      return f;
+    }
+  }
   f.row = backward ? row_shape(C, K, f.v, bwd_passes(f.v), kResidualRowThreads, kRowValues, 1.0)
                    : row_shape(C, K, f.v, kFwdPasses, 1024, 1024 * 32, 0.1);
   if (f.row.tokens) return f;
@@ -931,23 +944,31 @@ hipError_t residual_any(const ResidualBwdArgs& g, const Form& f, hipStream_t s) 
       hipLaunchKernelGGL(kernel, dim3(blocks), dim3(f.row.threads), lds, s, g, f.row, tiles);
       return hipGetLastError();
     };
-    constexpr int R = bwd_passes(V);  // as many in every block of more than 256 threads
-    if constexpr (R > 2) {
+    if constexpr (V == 4) {
       if (f.row.passes == 2) return run(residual_rows_bwd_kernel<T, V, 2, 256, TAIL>);
     }
-    return f.row.threads <= 256 ? run(residual_rows_bwd_kernel<T, V, R, 256, TAIL>)
-                                : run(residual_rows_bwd_kernel<T, V, R, 512, TAIL>);
+    if constexpr (V * sizeof(T) == 16) {
+      constexpr int R = bwd_passes(V);
+      return f.row.threads <= 256 ? run(residual_rows_bwd_kernel<T, V, R, 256, TAIL>)
+                                  : run(residual_rows_bwd_kernel<T, V, R, 512, TAIL>);
+    }
   }
-  return wide_backward<T>(f.wide, [&](auto shape) {
-    constexpr int R = decltype(shape)::kVecs, MAXT = decltype(shape)::kThreads;
-    hipLaunchKernelGGL((residual_wide_bwd_kernel<T, V, R, MAXT, TAIL>), dim3(blocks), dim3(f.wide.threads), 0, s, g);
-    return hipGetLastError();
-  });
+  if constexpr (V * sizeof(T) == 16) {
+    return wide_backward<T>(f.wide, [&](auto shape) {
+      constexpr int R = decltype(shape)::kVecs, MAXT = decltype(shape)::kThreads;
+      hipLaunchKernelGGL((residual_wide_bwd_kernel<T, V, R, MAXT, TAIL>), dim3(blocks), dim3(f.wide.threads), 0, s, g);
+      return hipGetLastError();
+    });
+  }
+  return hipErrorInvalidValue;
 }
 
 template <class T, class Args>
 hipError_t residual_typed(const Args& a, const Form& f, hipStream_t s) {
   constexpr int V = 16 / (int)sizeof(T);
+  if constexpr (V > 4 && std::is_same<Args, ResidualBwdArgs>::value) {
+    if (f.v == 4) return f.tail ? residual_any<T, 4, true>(a, f, s) : residual_any<T, 4, false>(a, f, s);
+  }
   return f.tail ? residual_any<T, V, true>(a, f, s) : residual_any<T, V, false>(a, f, s);
 }
 
