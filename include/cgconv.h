@@ -575,6 +575,12 @@ int cgconv_seq_scan_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
  * v, y [batch][K][C], decay, beta [batch][heads]), the state in place.  The backward
  * takes the gradients of y and of the final state (or NULL: zeros); any of its outputs
  * may be NULL, not all; tokens behind a length get zeros.  All sums have a fixed order.
+ * What is not finite counts as NaN and reaches what the formula takes it to: of a value its
+ * column, of a key, decay or beta its head, each from its token on and with the state, of a
+ * query its head at its token; tokens before it, and other columns and heads, are bit by bit as
+ * without it.  In the backward a value or a column of state_in reaches no gradient of a value
+ * or of state_in, and a gradient of y none of a later token and none of another query; a key,
+ * query, decay or beta may make every gradient of its key head and sequence NaN.
  */
 cgconv_seq_plan_t cgconv_seq_plan_create_rule(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states,
                                               int32_t heads, int32_t key_heads, int32_t key_dim, int32_t backward);

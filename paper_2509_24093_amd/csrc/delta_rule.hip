@@ -52,6 +52,7 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
   __shared__ float4 tok[kT];  // beta, rk; the second of Token's z, w
   __shared__ float rq[kT];
   __shared__ double sum[kT];
+  __shared__ int odd;  // first row of A that is not finite
   auto& kbuf = reinterpret_cast<bf16(*)[NP][kT * ST]>(space)[0];
   auto& qbuf = reinterpret_cast<bf16(*)[NP][kT * ST]>(space)[1];
   float* tri = reinterpret_cast<float*>(space);
@@ -83,6 +84,7 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
   }
   sk.store(kbuf, tokens, D, tid);
   sq.store(qbuf, tokens, D, tid);
+  if (tid == 0) odd = kT;
   __syncthreads();
   const int t = 16 * wave + m;
   // products of all pairs on and below the diagonal: kk and (forward) qk with rows j and the own
@@ -124,6 +126,7 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
   __syncthreads();
   const float4 me = tok[t];
   const float sq_ = a.scale * (BACKWARD ? 1.f : rq[t]);
+  float zero = 0.f;  // NaN if the lane has an entry of A that is not finite
 #pragma unroll
   for (int j = 0; j < kTiles; ++j) {
     v4f p = pq[j];
@@ -133,7 +136,9 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
         const int u = 16 * j + 4 * q + r;
         const float4 other = tok[u];
         const float f = decay_between(me, other) * other.y;
-        tri[t * kRow + u] = t > u ? me.x * me.y * f * kk[j][r] : 0.f;
+        const float x = t > u ? me.x * me.y * f * kk[j][r] : 0.f;
+        tri[t * kRow + u] = x;
+        zero = fmaf(x, 0.f, zero);
         if (!BACKWARD) p[r] = t >= u ? p[r] * f * sq_ : 0.f;
       }
       if (!BACKWARD)
@@ -148,7 +153,15 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
       ws.inside[(at * kBlocks + block_of(j, wave)) * 64 + lane] = make_float4(p[0], p[1], p[2], p[3]);
     }
   }
+  if (zero != 0.f) atomicMin(&odd, t);  // the least of them, in whatever order
   __syncthreads();
+  // Rows of A from the first that is not finite on stay out of the products, whose zeros would
+  // take them to the rows before; those of the inverse are NaN left of the diagonal.
+  const int bad = __builtin_amdgcn_readfirstlane(odd);
+  if (bad < kT) {
+    for (int i = tid; i < (kT - bad) * kT; i += 256) tri[(bad + i / kT) * kRow + i % kT] = 0.f;
+    __syncthreads();
+  }
   // Diagonal blocks: the inverse of blocks twice as large, X <- X - X C X with C the part of A
   // that joins two of them.  X is held as it accumulates and transposed: the one is an operand
   // of the other's products as it is.
@@ -211,12 +224,19 @@ __global__ __launch_bounds__(256) void rule_prepare_kernel(RuleArgs a, RuleWs ws
   }
   for (int n = wave; n < kBlocks; n += 4) {
     const int i = row_of(n), j = n - block_of(i, 0);
-    const float* p = inv + (16 * i + m) * kRow + 16 * j + 4 * q;
-    ws.inv[(at * kBlocks + n) * 64 + lane] = make_float4(p[0], p[1], p[2], p[3]);
-    if (BACKWARD) {
-      const float* c = inv + (16 * i + 4 * q) * kRow + 16 * j + m;
-      ws.invT[(at * kBlocks + n) * 64 + lane] = make_float4(c[0], c[kRow], c[2 * kRow], c[3 * kRow]);
-    }
+    // a lane's four entries from (row, column) on, down or along the row
+    const auto entries = [&](int row, int column, int down) {
+      const float* p = inv + row * kRow + column;
+      float4 x = down ? make_float4(p[0], p[kRow], p[2 * kRow], p[3 * kRow]) : make_float4(p[0], p[1], p[2], p[3]);
+      if (bad < kT) {
+        const auto lost = [&](int e) { return row + e * down >= bad && column + e * !down < row + e * down; };
+        const float nan = __builtin_nanf("");
+        x = make_float4(lost(0) ? nan : x.x, lost(1) ? nan : x.y, lost(2) ? nan : x.z, lost(3) ? nan : x.w);
+      }
+      return x;
+    };
+    ws.inv[(at * kBlocks + n) * 64 + lane] = entries(16 * i + m, 16 * j + 4 * q, 0);
+    if (BACKWARD) ws.invT[(at * kBlocks + n) * 64 + lane] = entries(16 * i + 4 * q, 16 * j + m, 1);
   }
   if (wave == 0) {
     const float4 x = tok[lane];
@@ -250,22 +270,42 @@ enum Walk {
 // us of a prompt instead of 688) or fewer waves that share a chunk (four: 1061, and for heads of
 // 64 columns, which occupy no more, 195 us instead of 174) are slower; a chunk in LDS ahead, and
 // products of one accumulator apart, took 740 to 688.
+//
+// CAREFUL: what is not finite stays out of the triangles' products.  Returns whether a column of
+// the last state is not finite, so that the segment is to be walked again with care; of kSpan
+// nothing else is wanted than that the column is.
 template <class T, int KB, int WALK>
-__global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a, RuleWs ws) {
+struct WalkSpace {
+  typedef Stage<T, KB, WALK == kOutputs, WALK == kOutputs> Buffer;
+  Buffer buffers[Buffer::kCount];
+  int again;
+};
+template <class T, int KB, int WALK>
+__device__ __forceinline__ WalkSpace<T, KB, WALK>& walk_space() {
+  __shared__ WalkSpace<T, KB, WALK> space;
+  return space;
+}
+
+template <class T, int KB, int WALK, bool CAREFUL>
+__device__ __forceinline__ bool rule_walk(const RuleArgs& a, const RuleWs& ws) {
   constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * kWalkWaves;
   constexpr bool kOut = WALK == kOutputs;
-  typedef Stage<T, KB, kOut, kOut> Buffer;
+  typedef typename WalkSpace<T, KB, WALK>::Buffer Buffer;
   constexpr int ST = Buffer::ST;
-  __shared__ Buffer buffers[Buffer::kCount];
+  auto& space = walk_space<T, KB, WALK>();
+  auto& buffers = space.buffers;
   __shared__ float turn[WALK == kSpan ? kWalkWaves : 1][16][20];  // of the matrix: a tile, read along its rows
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  // of a second walk the numbers are made anew, rather than held in registers through the first
+  const auto lane_number = [](int x) { return CAREFUL ? afresh_lane(x) : x; };
+  const auto block_number = [](int x) { return CAREFUL ? afresh(x) : x; };
+  const int tid = lane_number(threadIdx.x), wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int m = lane & 15, q = lane >> 4;
-  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z;
+  const int unit = block_number(blockIdx.y), b = unit / a.n.H, h = unit - b * a.n.H, seg = block_number(blockIdx.z);
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int first = (blockIdx.x * kWalkWaves + wave) * 16;
+  const int first = (block_number(blockIdx.x) * kWalkWaves + wave) * 16;
   const bool matrix = WALK == kSpan && first >= ws.VP;
   const bool active = first < (kOut ? ws.V : WALK == kKeep ? ws.VP : ws.VP + 32 * KB) && !(matrix && seg == 0);
-  if (WALK == kSpan && seg == 0 && (int)blockIdx.x * kWalkWaves * 16 >= ws.VP) return;
+  if (WALK == kSpan && seg == 0 && (int)blockIdx.x * kWalkWaves * 16 >= ws.VP) return false;
   const Column column(first + m, ws.V, C / a.n.H, C, h);
   const int length = tokens_of(a, b);
   const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
@@ -319,6 +359,7 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
   const auto fetch_values = [&](int c) {
     sv.load(v + (long long)c * kT * KC, KC, min(length - c * kT, kT), column, q);
   };
+  if (WALK != kSpan && !CAREFUL && tid == 0) space.again = 0;
   if (begin < end) {
     fetch(begin);
     fetch_values(begin);
@@ -345,6 +386,7 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
     const auto& inside = buf.inside;
     const float4* ta = buf.token;
     v4f X[kTiles], O[kTiles];
+    int odd = kT;  // the first place in the lane's column that is not finite
     if (active) {
       if constexpr (WALK == kKeep) {
         store_tiles(ws.state + at * (32 * KB) * ws.VP, ws.VP, first + m, q, S);
@@ -366,18 +408,25 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
         }
       }
       // Y, then V' = (1 + A)^-1 Y
+      v4f beta[kTiles];
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float4 tok = ta[16 * i + 4 * q + r];
-          X[i][r] = tok.x * fmaf(-tok.y, X[i][r], sv.get(i, r, column));
+          X[i][r] = fmaf(-tok.y, X[i][r], sv.get(i, r, column));
+          beta[i][r] = tok.x;
           if constexpr (kOut) O[i][r] *= tok.w;
         }
       if (c + 1 < end) fetch_values(c + 1);
+      if constexpr (CAREFUL) {
+        odd = min(first_odd<false>(X, q), first_odd<false>(beta, q));
+        put_from<false>(X, odd, q, 0.f);
+        put_from<false>(beta, odd, q, 0.f);
+      }
       Frag fy[2][3];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fy[kb]);
+      for (int kb = 0; kb < 2; ++kb) split_products(X[2 * kb], beta[2 * kb], X[2 * kb + 1], beta[2 * kb + 1], fy[kb]);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) X[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -388,6 +437,10 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
       if (c + 2 < end) fetch(c + 2);
     }
     if (!active) continue;
+    if constexpr (CAREFUL) {
+      if (kOut) odd = min(odd, first_odd<false>(X, q));  // the inverse has more
+      put_from<false>(X, odd, q, kOut ? 0.f : __builtin_nanf(""));
+    }
     if constexpr (WALK == kKeep) {
       store_tiles(ws.value + at * kT * ws.VP, ws.VP, first + m, q, X);
     }
@@ -397,18 +450,21 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
       for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fv[kb]);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) mma_triangle<false>(inside, kb, lane, fv[kb], O);
+      if constexpr (CAREFUL) {
+        put_from<false>(O, odd, q, __builtin_nanf(""));
+        put_from<false>(X, odd, q, __builtin_nanf(""));
+      }
       store_column(y + (long long)c * kT * KC, KC, N - c * kT, tokens, column, q, O);
     }
     // S <- e^{G_end} S + K^T (e^{G_end - G} rk V')
     Frag fz[2][3];
+    v4f late[kTiles];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        X[i][r] *= ta[16 * i + 4 * q + r].z;
-      }
+      for (int r = 0; r < 4; ++r) late[i][r] = ta[16 * i + 4 * q + r].z;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fz[kb]);
+    for (int kb = 0; kb < 2; ++kb) split_products(X[2 * kb], late[2 * kb], X[2 * kb + 1], late[2 * kb + 1], fz[kb]);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -421,8 +477,14 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
       mma_all(f, fz[kb], S);
     }
   }
+  bool again = false;
+  if (WALK != kSpan && !CAREFUL && begin < end) {
+    if (any_odd(S)) space.again = 1;
+    __syncthreads();
+    again = __builtin_amdgcn_readfirstlane(space.again) != 0;
+  }
   if constexpr (WALK == kSpan) {
-    if (!active) return;
+    if (!active) return false;
     const int col = first + m;
     if (!matrix) {
       store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S);
@@ -457,10 +519,10 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
     }
   }
   if constexpr (kOut) {
-    if (!column.there) return;
+    if (!column.there) return again;
     const long long stop = min((long long)last * kT, (long long)N);
     for (long long n = (long long)max(end, begin) * kT + q; n < stop; n += 4) y[n * KC + column.at] = (T)0.f;
-    if (!a.state_out || last != ws.chunks) return;
+    if (!a.state_out || last != ws.chunks) return again;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -468,6 +530,22 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(RuleArgs a,
         const int row = 16 * d + 4 * q + r;
         if (row < D) a.state_out[((long long)b * D + row) * KC + column.at] = S[d][r];
       }
+  }
+  return again;
+}
+
+struct WalkArgs {
+  RuleArgs a;
+  RuleWs ws;
+};
+template <class T, int KB, int WALK>
+__global__ __launch_bounds__(64 * kWalkWaves) void rule_state_kernel(WalkArgs w) {
+  const bool again = rule_walk<T, KB, WALK, false>(w.a, w.ws);
+  if constexpr (WALK != kSpan) {
+    if (again) {
+      const auto once_more = argument_anew<WalkArgs>();
+      rule_walk<T, KB, WALK, true>(once_more.a, once_more.ws);
+    }
   }
 }
 
@@ -599,7 +677,8 @@ hipError_t walk(const RuleArgs& a, const RuleWs& w, hipStream_t s) {
   const int columns = WALK == kOutputs ? w.V : WALK == kKeep ? w.VP : w.VP + 32 * w.KB;
   const dim3 grid((columns + kColumns - 1) / kColumns, w.units, WALK == kSpan ? w.segments - 1 : w.segments);
   return by_width(w.KB, [&](auto kb) {
-    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, WALK>), grid, dim3(64 * kWalkWaves), 0, s, a, w);
+    hipLaunchKernelGGL((rule_state_kernel<T, decltype(kb)::value, WALK>), grid, dim3(64 * kWalkWaves), 0, s,
+                       WalkArgs{a, w});
     return hipGetLastError();
   });
 }

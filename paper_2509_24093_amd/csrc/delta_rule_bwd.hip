@@ -43,19 +43,35 @@ __device__ __forceinline__ int tokens_of(const RuleArgs& a, int b) {
 // Block (128 columns, unit, segment).  SPAN: of every segment but the first only
 // the gradient of the state before it, of the last from the given one, of others from zero.
 // Bound as the forward's walk: a chunk of a 128 x 128 head takes 10 us, 7.3 with SPAN.
-template <class T, int KB, bool SPAN>
-__global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdArgs g, RuleWs ws) {
-  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * kWalkWaves;
+// CAREFUL and what it returns: as rule_walk, of the first gradient of the state.
+template <class T, int KB>
+struct ReverseSpace {
   typedef Stage<T, KB, true, true> Buffer;  // the transposed triangles
+  Buffer buffers[Buffer::kCount];
+  int again;
+};
+template <class T, int KB>
+__device__ __forceinline__ ReverseSpace<T, KB>& reverse_space() {
+  __shared__ ReverseSpace<T, KB> space;
+  return space;
+}
+
+template <class T, int KB, bool SPAN, bool CAREFUL>
+__device__ __forceinline__ bool rule_reverse(const RuleBwdArgs& g, const RuleWs& ws) {
+  constexpr int NP = kParts<T>, DT = 2 * KB, kThreads = 64 * kWalkWaves;
+  typedef typename ReverseSpace<T, KB>::Buffer Buffer;
   constexpr int ST = Buffer::ST;
-  __shared__ Buffer buffers[Buffer::kCount];
+  auto& space = reverse_space<T, KB>();
+  auto& buffers = space.buffers;
   const RuleArgs& a = g.a;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const auto lane_number = [](int x) { return CAREFUL ? afresh_lane(x) : x; };
+  const auto block_number = [](int x) { return CAREFUL ? afresh(x) : x; };
+  const int tid = lane_number(threadIdx.x), wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int m = lane & 15, q = lane >> 4;
-  const int unit = blockIdx.y, b = unit / a.n.H, h = unit - b * a.n.H, seg = blockIdx.z + SPAN;
+  const int unit = block_number(blockIdx.y), b = unit / a.n.H, h = unit - b * a.n.H, seg = block_number(blockIdx.z) + SPAN;
   const int D = a.n.D, hk = h / (a.n.H / a.n.Hk), C = a.n.C, KC = a.n.K * C, N = a.n.N;
-  const int col = (blockIdx.x * kWalkWaves + wave) * 16 + m;
-  const bool active = (blockIdx.x * kWalkWaves + wave) * 16 < ws.VP;
+  const int first = (block_number(blockIdx.x) * kWalkWaves + wave) * 16, col = first + m;
+  const bool active = first < ws.VP;
   const Column column(col, ws.V, C / a.n.H, C, h);
   const int length = tokens_of(a, b);
   const int begin = seg * ws.span, last = min(begin + ws.span, ws.chunks);  // of the segment
@@ -103,6 +119,7 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdAr
     sp.store(to.inside, tid);
     if (tid < kT) to.token[tid] = st;
   };
+  if (!SPAN && !CAREFUL && tid == 0) space.again = 0;
   if (begin < end) {
     fetch(end - 1);
     so.load(gy + (long long)(end - 1) * kT * KC, KC, min(length - (end - 1) * kT, kT), column, q);
@@ -153,6 +170,20 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdAr
     }
     if (!active) continue;
     // gV', gY
+    int odd = kT;  // the first place in the lane's column that is not finite, from the last token back
+    if constexpr (CAREFUL) {
+      v4f o[kTiles];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[i][r] = so.get(i, r, column);
+      odd = first_odd<true>(o, q);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (place_of<true>(i, r, q) >= odd) so.v[i][r] = (T)0.f;
+    }
     Frag fo[2][NP];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -163,6 +194,10 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdAr
     }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) mma_triangle<true>(inside, kb, lane, fo[kb], X);
+    if constexpr (CAREFUL) {
+      odd = min(odd, first_odd<true>(X, q));  // the state's gradient and P have more
+      put_from<true>(X, odd, q, 0.f);
+    }
     Frag fx[2][3];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) split_tiles(X[2 * kb], X[2 * kb + 1], fx[kb]);
@@ -170,6 +205,7 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdAr
     for (int i = 0; i < kTiles; ++i) X[i] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) mma_triangle<true>(inv, kb, lane, fx[kb], X);
+    if constexpr (CAREFUL) put_from<true>(X, odd, q, __builtin_nanf(""));
     if (!SPAN) store_tiles(ws.gvalue + at * kT * ws.VP, ws.VP, col, q, X);
     // gS <- e^{G_end} gS + Q^T (o gO) - K^T (a gv)
     v4f o[kTiles];
@@ -208,16 +244,22 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdAr
       mma_all(f, fz[kb], S);
     }
   }
+  bool again = false;
+  if (!SPAN && !CAREFUL && begin < end) {
+    if (any_odd(S)) space.again = 1;
+    __syncthreads();
+    again = __builtin_amdgcn_readfirstlane(space.again) != 0;
+  }
   if constexpr (SPAN) {
     if (active) store_tiles(ws.span_state + start * ws.VP, ws.VP, col, q, S);
-    return;
+    return false;
   }
-  if (!column.there) return;
+  if (!column.there) return again;
   if (gv) {
     const long long stop = min((long long)last * kT, (long long)N);
     for (long long t = (long long)max(end, begin) * kT + q; t < stop; t += 4) gv[t * KC + column.at] = (T)0.f;
   }
-  if (!g.gstate_in || seg > 0) return;
+  if (!g.gstate_in || seg > 0) return again;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -225,6 +267,22 @@ __global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(RuleBwdAr
       const int row = 16 * d + 4 * q + r;
       if (row < D) g.gstate_in[((long long)b * D + row) * KC + column.at] = S[d][r];
     }
+  return again;
+}
+
+struct ReverseArgs {
+  RuleBwdArgs g;
+  RuleWs ws;
+};
+template <class T, int KB, bool SPAN>
+__global__ __launch_bounds__(64 * kWalkWaves) void rule_reverse_kernel(ReverseArgs r) {
+  const bool again = rule_reverse<T, KB, SPAN, false>(r.g, r.ws);
+  if constexpr (!SPAN) {
+    if (again) {
+      const auto once_more = argument_anew<ReverseArgs>();
+      rule_reverse<T, KB, SPAN, true>(once_more.g, once_more.ws);
+    }
+  }
 }
 
 // ---- gradients of keys, queries, decays and betas -------------------------------------------
@@ -707,8 +765,8 @@ template <class T, int KB>
 hipError_t backward(const RuleBwdArgs& g, const RuleWs& w, hipStream_t s) {
   constexpr int kColumns = 16 * kWalkWaves;
   const auto walk = [&](auto kernel, int segments) {
-    hipLaunchKernelGGL(kernel, dim3((w.VP + kColumns - 1) / kColumns, w.units, segments), dim3(64 * kWalkWaves), 0, s, g,
-                       w);
+    hipLaunchKernelGGL(kernel, dim3((w.VP + kColumns - 1) / kColumns, w.units, segments), dim3(64 * kWalkWaves), 0, s,
+                       ReverseArgs{g, w});
     return hipGetLastError();
   };
   hipError_t e = hipSuccess;

@@ -66,6 +66,23 @@ __device__ __forceinline__ void split8(const float (&x)[8], Frag (&f)[3]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) split2(x[2 * e], x[2 * e + 1], f[0].w[e], f[1].w[e], f[2].w[e]);
 }
+// The parts of products x y: what is left of the first part is that of the exact product.
+__device__ __forceinline__ void split_products(const v4f& xa, const v4f& ya, const v4f& xb, const v4f& yb, Frag (&f)[3]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float rest[2];
+    uint32_t top[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float x = (e < 2 ? xa : xb)[2 * (e & 1) + i], y = (e < 2 ? ya : yb)[2 * (e & 1) + i];
+      top[i] = __float_as_uint(x * y);
+      rest[i] = fmaf(x, y, -__uint_as_float(top[i] & 0xFFFF0000u));
+    }
+    f[0].w[e] = __builtin_amdgcn_perm(top[1], top[0], 0x07060302);
+    f[1].w[e] = top_halves(rest[0], rest[1]);
+    f[2].w[e] = top_halves(without_top(rest[0]), without_top(rest[1]));
+  }
+}
 __device__ __forceinline__ void split_tiles(const v4f& a, const v4f& b, Frag (&f)[3]) {
   const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   split8(x, f);
@@ -201,6 +218,60 @@ __device__ __forceinline__ void mma_triangle(const uint2 (&t)[3][kBlocks][64], i
           if (triangle_has<UPPER>(i, kb))
             acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i][p].f, b[s - p].f, acc[i], 0, 0, 0);
       }
+}
+
+// A triangle's zeros let nothing through but what is not finite: 0 x NaN is NaN.  So where
+// there is such a value, before a product with a triangle a column's values from the first one
+// on (of a transposed triangle: up to the last one) give way to zeros, and afterwards the
+// results from there on are NaN, as the formula has them; the others are those of finite values
+// bit by bit.  An infinity counts as a NaN: split into parts it is one.  What is not finite
+// never leaves a column of the state, so the walks look at the last one of a segment, and
+// repeat the segment in this way if there is any: looking at every chunk's values instead took
+// prompts of heads of 128 x 128 from 622 to 686 us.
+template <int TILES>
+__device__ __forceinline__ bool any_odd(const v4f (&x)[TILES]) {  // in any lane of the wave
+  float z = 0.f;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) z = fmaf(x[i][r], 0.f, z);
+  return __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+}
+// A place in the order of a triangle's products: tokens, or from the last one back.
+template <bool UPPER>
+__device__ __forceinline__ int place_of(int i, int r, int q) {
+  return UPPER ? kT - 1 - (16 * i + 4 * q + r) : 16 * i + 4 * q + r;
+}
+// The first place whose value in the lane's column is not finite, kT if there is none.
+template <bool UPPER>
+__device__ __forceinline__ int first_odd(const v4f (&x)[kTiles], int q) {
+  int at = kT;
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (!(__builtin_fabsf(x[i][r]) < __builtin_inff())) at = min(at, place_of<UPPER>(i, r, q));
+  at = min(at, __shfl_xor(at, 16));
+  return min(at, __shfl_xor(at, 32));
+}
+// x from a place on.
+template <bool UPPER>
+__device__ __forceinline__ void put_from(v4f (&x)[kTiles], int at, int q, float value) {
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[i][r] = place_of<UPPER>(i, r, q) >= at ? value : x[i][r];
+}
+
+// The only argument of a kernel, read once more: what a second part of the kernel needs of it is
+// then not held in registers through the first.
+template <class A>
+__device__ __forceinline__ A argument_anew() {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  A a;
+  __builtin_memcpy(&a, (const void*)p, sizeof a);
+  return a;
 }
 
 // The numbers of a token that its chunk's kernels need, made by rule_prepare_kernel:
