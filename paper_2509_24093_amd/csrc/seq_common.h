@@ -128,7 +128,6 @@ __device__ __forceinline__ void store_part(T* p, int n, const float (&v)[V]) {
 // x as a number the compiler knows nothing of: what is computed from it stays where it is,
 // instead of waiting in registers for every turn of a loop.
 __device__ __forceinline__ int afresh(int x) {
-  x = __builtin_amdgcn_readfirstlane(x);
   asm volatile("" : "+s"(x));
   return x;
 }
