@@ -34,8 +34,10 @@ namespace cgconv {
 
 namespace {
 
-// 1 / (1 + e^-z) within two units of the last place: a power of 2 whose argument's rounding is
-// made up for, and a reciprocal with one Newton step.  With expf and a division, which are twice
+// 1 / (1 + e^-z) within two units of the last place down to z = -87 (3.83 half units with silu's own
+// product over 2.9e5 gates, tests/test_residual_rows_gpu.py), zero or below 2^-125 under it: a
+// power of 2 whose argument is reduced with log2(e) in two parts, as Cody and Waite do it, so that
+// its rounding is made up for, and a reciprocal with one step of Newton's method.  With expf and a division, which are twice
 // the instructions, the wide rows' backward is bound by them (16384 tokens of 4096: 331 us, so
 // 271), and the rows' forward waits for its tokens' gates (131072 of L=6 C=32: 712 us, so 627).
 __device__ __forceinline__ float sigmoid(float z) {
