@@ -480,7 +480,9 @@ int cgconv_seq_norm_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
  * factor); post_weight, weight [L_max+1][C], scale and bias [C], fp32, may be NULL (ones,
  * zeros); eps >= 0.  y is of the r that has not been rounded to dtype.  stats
  * [batch][N][2 (L_max+2)], fp32, or NULL: mean of u, 1 / deviation of its degrees, mean of
- * r, 1 / deviation of its degrees, for the backward.  The backward takes the gradients
+ * r, 1 / deviation of its degrees, for the backward.  Both norms are always taken (without a
+ * post_weight u is normed with a weight of ones), and both take the mean of the invariants
+ * away.  The backward takes the gradients
  * of r (or NULL: zeros) and y; any of its outputs may be NULL, not all.  The sums over
  * tokens have a fixed order.
  */
