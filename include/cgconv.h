@@ -582,7 +582,9 @@ int cgconv_seq_scan_backward(cgconv_seq_plan_t plan, int32_t dtype, const void* 
  * query its head at its token; tokens before it, and other columns and heads, are bit by bit as
  * without it.  In the backward a value or a column of state_in reaches no gradient of a value
  * or of state_in, and a gradient of y none of a later token and none of another query; a key,
- * query, decay or beta may make every gradient of its key head and sequence NaN.
+ * query, decay or beta may make every gradient of its key head and sequence NaN.  That is of
+ * inputs: where keys and betas beyond the above make the state grow out of fp32 within 64
+ * tokens, tokens shortly before may be NaN as well.
  */
 cgconv_seq_plan_t cgconv_seq_plan_create_rule(int64_t batch, int64_t N, int32_t L_max, int64_t C, int32_t states,
                                               int32_t heads, int32_t key_heads, int32_t key_dim, int32_t backward);
